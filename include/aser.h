@@ -261,6 +261,38 @@ int aser_forward(const void* X_f16, const float* s, const void* LA_f16, const vo
                  void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Gated feed-forward block (gate, up and down projection of a decoder layer's MLP, each quantized as above):
+ *     H = act(gate(X)) * up(X),   Y = down(H)
+ * GATE AND UP ARE STORED AS ONE PROJECTION OF N = 2 F CHANNELS THAT ALTERNATE: rows 2 i and 2 i + 1 of the weight that is packed
+ * (aser_pack_w4, aser_repack_w4), of w_scale and of L_B are channel i of gate and channel i of up.  They read one X with one
+ * s, and share one down projection L_A [r, K] (Algorithm 1 applied to the interleaved weight; factors that were made apart, of
+ * ranks r1 and r2, are used with L_A = [L_A1; L_A2] and an L_B whose even rows are [L_B1 | 0] and odd rows [0 | L_B2]).
+ * activation: ASER_ACT_SILU  g / (1 + exp(-g));  ASER_ACT_GELU_TANH  g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) / 2.
+ *
+ * aser_linear_w4a8_lr_glu -- aser_linear_w4a8_lr of that projection with the product in its epilogue:
+ *     G[m,i] = fp16(channel 2 i),  U[m,i] = fp16(channel 2 i + 1)      (exactly what aser_linear_w4a8_lr would store)
+ *     H[m,i] = fp16( act(G[m,i]) * U[m,i] )                            (fp32, one rounding)
+ * H_f16 [M, N / 2]; N % 16 == 0; workspace as for aser_linear_w4a8_lr.  r == 0 (T and L_B NULL) gives the plain product.
+ *
+ * aser_forward_ffn -- the whole block: activation step of X, the launch above, activation step of H, the down projection
+ * (K = F, so F % 128 == 0), four to six launches in all, each a programmatic dependent of the one before.  s_down [F] or NULL,
+ * LA_down [r_down, F], Wk_down / w_scale_down / LB_down of the [N, F] down projection.  The codes, scales, T and H of
+ * both steps are kept in the workspace: aser_forward_ffn_workspace_bytes(...) bytes, zeroed once with aser_workspace_init (0
+ * for unsupported shapes).  Calls that overlap in time, and graphs that may run at the same time, need a workspace each.  Y may not overlap X or the
+ * workspace.  Errors: every argument of every launch is checked before anything is enqueued.
+ */
+#define ASER_ACT_SILU       0
+#define ASER_ACT_GELU_TANH  1
+int aser_linear_w4a8_lr_glu(const int8_t* Xq, const float* a_scale, const void* Wk, const float* w_scale,
+                            const void* T_bf16, const void* LB_f16, int M, int N, int K, int r, int activation,
+                            void* H_f16, void* workspace, size_t workspace_bytes, void* stream);
+size_t aser_forward_ffn_workspace_bytes(int M, int K, int F, int N, int r, int r_down);
+int aser_forward_ffn(const void* X_f16, const float* s, const void* LA_f16, const void* Wk_gu, const float* w_scale_gu,
+                     const void* LB_gu_f16, const float* s_down, const void* LA_down_f16, const void* Wk_down,
+                     const float* w_scale_down, const void* LB_down_f16, int M, int K, int F, int N, int r, int r_down,
+                     int activation, void* Y_f16, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * aser_forward_shared -- the forward pass of n_layers layers that read the SAME activation X
  * and share the smoothing vector s (Algorithm 1 builds each layer's factors on its own; where
  * the layers' inputs and s coincide their activation work is identical): X is smoothed and

@@ -16,7 +16,7 @@ EXPORTED_SYMBOLS = (
     "aser_linear_w4a8_lr_cat", "aser_forward_shared_cat_workspace_bytes", "aser_forward_shared_cat",
     "aser_forward_shared_workspace_bytes", "aser_construct", "aser_construct_workspace_bytes", "aser_linear_w4a8_lr", "aser_linear_w4a8", "aser_linear_w4a8_lr_simt", "aser_linear_w4a8_lr_static",
     "aser_workspace_bytes", "aser_workspace_init", "aser_check_status", "aser_forward",
-    "aser_forward_host",
+    "aser_forward_host", "aser_linear_w4a8_lr_glu", "aser_forward_ffn_workspace_bytes", "aser_forward_ffn",
     "aser_last_error", "aser_version",
 )
 
@@ -63,6 +63,10 @@ lib.aser_check_status.argtypes = [_P, _P]
 lib.aser_forward.argtypes = [_P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _P, _P, _P, _P, _P, _Z, _P]
 lib.aser_forward_host.argtypes = [_P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P,
                                   _I, _I, _I, _I, _P, _Z, _P]
+lib.aser_linear_w4a8_lr_glu.argtypes = [_P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _P, _P, _Z, _P]
+lib.aser_forward_ffn_workspace_bytes.argtypes = [_I, _I, _I, _I, _I, _I]
+lib.aser_forward_ffn_workspace_bytes.restype = _Z
+lib.aser_forward_ffn.argtypes = [_P] * 11 + [_I] * 7 + [_P, _P, _Z, _P]
 lib.aser_construct_workspace_bytes.argtypes = [_I, _I, _I, _I, _I]
 lib.aser_construct_workspace_bytes.restype = _Z
 lib.aser_construct.argtypes = [_P, _P, _P, _I, _I, _I, _I, C.c_double, _I, _P, _P, _P, _P, _P, _P, _P, _I, _P, _Z, _P]
@@ -247,6 +251,36 @@ def linear_w4a8(Xq, a_scale, Wk, w_scale, N: int, ws: torch.Tensor, Y=None, acc_
     _chk(lib.aser_linear_w4a8(_ptr(Xq), _ptr(a_scale), _ptr(Wk), _ptr(w_scale), M, N, K, _ptr(Y),
                               _ptr(acc_debug), _ptr(ws), ws.numel(), _stream()), "aser_linear_w4a8")
     return Y
+
+
+ACTIVATIONS = {"silu": 0, "gelu_tanh": 1}
+
+
+def _activation(name) -> int:
+    if name not in ACTIVATIONS:
+        raise ValueError("activation must be one of %s, not %r" % (", ".join(sorted(ACTIVATIONS)), name))
+    return ACTIVATIONS[name]
+
+
+def interleave_gate_up(gate: torch.Tensor, up: torch.Tensor) -> torch.Tensor:
+    """Rows of gate and up in turn: the order in which aser_linear_w4a8_lr_glu takes weights [F, K], scales [F] and up
+    projections [F, r]."""
+    if gate.shape != up.shape:
+        raise ValueError("gate and up need the same shape")
+    return torch.stack([gate, up], dim=1).reshape(2 * gate.shape[0], *gate.shape[1:]).contiguous()
+
+
+def linear_w4a8_lr_glu(Xq, a_scale, Wk, w_scale, T, L_B, N: int, ws: torch.Tensor, activation: str = "silu", H=None):
+    """aser_linear_w4a8_lr_glu: H fp16 [M, N / 2] = act(gate) * up of a projection whose N channels are gate and up in
+    turn."""
+    M, K = Xq.shape
+    r = 0 if L_B is None else L_B.shape[1]
+    if H is None:
+        H = torch.empty((M, N // 2), dtype=torch.float16, device=Xq.device)
+    _chk(lib.aser_linear_w4a8_lr_glu(_ptr(Xq), _ptr(a_scale), _ptr(Wk), _ptr(w_scale), _ptr(T) if r else None,
+                                     _ptr(L_B) if r else None, M, N, K, r, _activation(activation), _ptr(H), _ptr(ws),
+                                     ws.numel(), _stream()), "aser_linear_w4a8_lr_glu")
+    return H
 
 
 def linear_w4a8_lr_simt(Xq, a_scale, Wq, w_scale, T, L_B, Y=None, acc_debug=None):
@@ -503,6 +537,67 @@ class AserSharedInputCat(AserSharedInput):
                                          _ptr(self.T) if self.r_total else None, _ptr(self.Y_cat),
                                          _ptr(self.ws), self.ws.numel(), _stream()), "aser_forward_shared_cat")
         return self._views(M)
+
+
+class AserGatedFFN:
+    """Gated feed-forward block of three ASER-quantized layers, Y = down(act(gate(X)) * up(X)), through
+    aser_forward_ffn; device-resident operands and a workspace for up to `max_tokens` tokens.
+
+    W_gate, W_up fp16 [F,K] with one smoothing vector s [K] (or None) and one pair of factors for both: L_A [r,K], L_B [2F,r]
+    whose first F rows are gate's (None for no low-rank term); W_down fp16 [N,F] with s_down [F], L_A_down [r',F],
+    L_B_down [N,r'].  The packed gate and up channels are stored in turn."""
+
+    def __init__(self, W_gate, W_up, s, L_A, L_B, W_down, s_down, L_A_down, L_B_down, max_tokens: int,
+                 activation: str = "silu"):
+        self.F, self.K = W_gate.shape
+        self.N = W_down.shape[0]
+        if W_up.shape != W_gate.shape or W_down.shape[1] != self.F:
+            raise ValueError("gate and up need the same shape, and down as many columns as they have rows")
+        if (L_A is None) != (L_B is None) or (L_A_down is None) != (L_B_down is None):
+            raise ValueError("L_A and L_B come together")
+        self.activation = _activation(activation)
+        self.max_tokens = max_tokens
+        self.r = 0 if L_A is None else L_A.shape[0]
+        self.r_down = 0 if L_A_down is None else L_A_down.shape[0]
+        for A, B, k, n, r, what in ((L_A, L_B, self.K, 2 * self.F, self.r, "gate and up"),
+                                    (L_A_down, L_B_down, self.F, self.N, self.r_down, "down")):
+            if r and (tuple(A.shape) != (r, k) or tuple(B.shape) != (n, r)):
+                raise ValueError("factors of %s: need L_A [%d, %d] and L_B [%d, %d]" % (what, r, k, n, r))
+        for v, k, name in ((s, self.K, "s"), (s_down, self.F, "s_down")):
+            if v is not None and (_dev(v, torch.float32, name).shape != (k,)):
+                raise ValueError("%s needs %d elements" % (name, k))
+        nbytes = int(lib.aser_forward_ffn_workspace_bytes(max_tokens, self.K, self.F, self.N, self.r, self.r_down))
+        if nbytes == 0:
+            raise ValueError("unsupported shapes for a feed-forward block")
+        dev = W_gate.device
+        self.s, self.s_down = s, s_down
+        self.Wq, self.w_scale = pack_w4(interleave_gate_up(W_gate, W_up), s)
+        self.Wk = repack_w4(self.Wq)
+        self.L_A = None if L_A is None else _dev(L_A, torch.float16, "L_A")
+        self.L_B = None if L_B is None else interleave_gate_up(*_dev(L_B, torch.float16, "L_B").chunk(2))
+        self.Wq_down, self.w_scale_down = pack_w4(_dev(W_down, torch.float16, "W_down"), s_down)
+        self.Wk_down = repack_w4(self.Wq_down)
+        self.L_A_down = None if L_A_down is None else _dev(L_A_down, torch.float16, "L_A_down")
+        self.L_B_down = None if L_B_down is None else _dev(L_B_down, torch.float16, "L_B_down")
+        self.Y = torch.empty((max_tokens, self.N), dtype=torch.float16, device=dev)
+        self.ws = torch.empty((nbytes,), dtype=torch.uint8, device=dev)
+        _chk(lib.aser_workspace_init(_ptr(self.ws), nbytes, _stream()), "aser_workspace_init")
+
+    def __call__(self, X: torch.Tensor) -> torch.Tensor:
+        """Y [M, N] (a view of a preallocated buffer) of X fp16 [M, K], M up to max_tokens."""
+        if X.dtype != torch.float16 or not X.is_cuda or not X.is_contiguous() or X.dim() != 2 or X.shape[1] != self.K:
+            raise TypeError("X: need a contiguous CUDA tensor of torch.float16, [M, %d]" % self.K)
+        M = X.shape[0]
+        if M > self.max_tokens:
+            raise ValueError("%d tokens, but the block was made for %d" % (M, self.max_tokens))
+        rc = lib.aser_forward_ffn(X.data_ptr(), _ptr(self.s), _ptr(self.L_A), self.Wk.data_ptr(), self.w_scale.data_ptr(),
+                                  _ptr(self.L_B), _ptr(self.s_down), _ptr(self.L_A_down), self.Wk_down.data_ptr(),
+                                  self.w_scale_down.data_ptr(), _ptr(self.L_B_down), M, self.K, self.F, self.N, self.r,
+                                  self.r_down, self.activation, self.Y.data_ptr(), self.ws.data_ptr(), self.ws.numel(),
+                                  _stream())
+        if rc != 0:
+            raise AserError(rc, "aser_forward_ffn")
+        return self.Y[:M]
 
 
 def forward_host(layer: AserLinear, X_host: torch.Tensor, Y_host: torch.Tensor):

@@ -92,7 +92,7 @@ int check_device() {
 int linear_common(const int8_t* Xq, const float* a_scale, const void* Wk, const float* w_scale,
                   const void* T_bf16, const void* LB_f16, int M, int N, int K, int r, void* Y_f16,
                   int32_t* acc_debug, void* workspace, size_t workspace_bytes, void* stream,
-                  bool overlap_prev = false, int ldt = 0, CatSplit cat = CatSplit()) {
+                  bool overlap_prev = false, int ldt = 0, CatSplit cat = CatSplit(), const GluForm* glu = nullptr) {
     if (!shape_ok(M, N, K, r)) return fail(ASER_ERR_SHAPE, "unsupported M, N, K or r");
     if (r > 0 && ldt != 0 && (ldt < r || ldt % 8 != 0))
         return fail(ASER_ERR_SHAPE, "ldt must be a multiple of 8 and at least r");
@@ -117,26 +117,54 @@ int linear_common(const int8_t* Xq, const float* a_scale, const void* Wk, const 
                                     static_cast<const __nv_bfloat16*>(T_bf16),
                                     static_cast<const __half*>(LB_f16), M, N, K, r,
                                     static_cast<__half*>(Y_f16), acc_debug,
-                                    static_cast<cudaStream_t>(stream), overlap_prev, ldt, cat);
+                                    static_cast<cudaStream_t>(stream), overlap_prev, ldt, cat, glu);
     const bool split = linear_split_prefers(M, N, K);
-    if (split || linear_pair_prefers(M, N, K, cat)) {
+    if (split || linear_pair_prefers(M, N, K, cat, glu != nullptr)) {
         rc = linear_tc_check(M, N, K, r, workspace_bytes);      // the limits are the same for all three kernels
         if (rc != ASER_OK) return rc;
         if (split)
             return launch_linear_split(Xq, a_scale, static_cast<const uint8_t*>(Wk), w_scale,
                                        static_cast<const __nv_bfloat16*>(T_bf16), static_cast<const __half*>(LB_f16),
                                        M, N, K, r, static_cast<__half*>(Y_f16), acc_debug, workspace,
-                                       static_cast<cudaStream_t>(stream), overlap_prev, ldt, cat);
+                                       static_cast<cudaStream_t>(stream), overlap_prev, ldt, cat, glu);
         return launch_linear_pair(Xq, a_scale, static_cast<const uint8_t*>(Wk), w_scale,
                                   static_cast<const __nv_bfloat16*>(T_bf16), static_cast<const __half*>(LB_f16),
                                   M, N, K, r, static_cast<__half*>(Y_f16), acc_debug, workspace,
-                                  static_cast<cudaStream_t>(stream), overlap_prev, ldt, cat);
+                                  static_cast<cudaStream_t>(stream), overlap_prev, ldt, cat, glu);
     }
     return launch_linear_tc(Xq, a_scale, static_cast<const uint8_t*>(Wk), w_scale,
                             static_cast<const __nv_bfloat16*>(T_bf16),
                             static_cast<const __half*>(LB_f16), M, N, K, r,
                             static_cast<__half*>(Y_f16), acc_debug, workspace, workspace_bytes,
-                            static_cast<cudaStream_t>(stream), overlap_prev, ldt, cat);
+                            static_cast<cudaStream_t>(stream), overlap_prev, ldt, cat, glu);
+}
+
+// act(g) = g / (1 + exp(-g (c0 + c1 g^2))), see glu_math.cuh; false for an activation that is not known.
+bool glu_form(int activation, GluForm* f) {
+    constexpr double kC0 = 1.5957691216057308;         // sqrt(8 / pi)
+    if (activation == ASER_ACT_SILU) { f->c0 = 1.f; f->c1 = 0.f; return true; }
+    if (activation == ASER_ACT_GELU_TANH) { f->c0 = (float)kC0; f->c1 = (float)(0.044715 * kC0); return true; }
+    return false;
+}
+
+// The parts of a feed-forward block's workspace: what the activation and linear kernels of either layer need, then the
+// intermediates, which the second layer takes over from the first (its activation step waits for the first layer's linear
+// kernel to complete before it writes anything).
+struct FfnLayout { size_t kernels, Xq, a_scale, T, H, total; };
+
+bool ffn_layout(int M, int K, int F, int N, int r, int r_down, FfnLayout* l) {
+    if (!shape_ok(M, 0, K, r) || !shape_ok(M, N, F, r_down) || F > 0x3fffffff) return false;
+    auto round_up = [](size_t v) { return (v + 255) / 256 * 256; };
+    const size_t first = aser_workspace_bytes(M, 2 * F, K, r), second = aser_workspace_bytes(M, N, F, r_down);
+    if (first == 0 || second == 0) return false;
+    const size_t m = (size_t)M;
+    l->kernels = round_up(first > second ? first : second);
+    l->Xq = l->kernels;
+    l->a_scale = l->Xq + round_up(m * (size_t)(K > F ? K : F));
+    l->T = l->a_scale + round_up(m * 4);
+    l->H = l->T + round_up(m * 2 * (size_t)(r > r_down ? r : r_down));
+    l->total = l->H + round_up(m * 2 * (size_t)F);
+    return true;
 }
 
 // Stacked ranks (several layers' down projections in one pass) go up to 512.
@@ -499,6 +527,70 @@ int aser_linear_w4a8_lr_ld(const int8_t* Xq, const float* a_scale, const void* W
                            void* workspace, size_t workspace_bytes, void* stream) {
     return linear_common(Xq, a_scale, Wk, w_scale, T_bf16, LB_f16, M, N, K, r, Y_f16, acc_debug,
                          workspace, workspace_bytes, stream, false, ldt);
+}
+
+int aser_linear_w4a8_lr_glu(const int8_t* Xq, const float* a_scale, const void* Wk, const float* w_scale,
+                            const void* T_bf16, const void* LB_f16, int M, int N, int K, int r, int activation,
+                            void* H_f16, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!shape_ok(M, N, K, r) || N % 16 != 0) return fail(ASER_ERR_SHAPE, "unsupported M, N, K or r");
+    GluForm glu;
+    if (!glu_form(activation, &glu)) return fail(ASER_ERR_SHAPE, "unknown activation");
+    return linear_common(Xq, a_scale, Wk, w_scale, T_bf16, LB_f16, M, N, K, r, H_f16, nullptr, workspace, workspace_bytes,
+                         stream, false, 0, CatSplit(), &glu);
+}
+
+size_t aser_forward_ffn_workspace_bytes(int M, int K, int F, int N, int r, int r_down) {
+    FfnLayout l;
+    return ffn_layout(M, K, F, N, r, r_down, &l) ? l.total : 0;
+}
+
+int aser_forward_ffn(const void* X_f16, const float* s, const void* LA_f16, const void* Wk_gu, const float* w_scale_gu,
+                     const void* LB_gu_f16, const float* s_down, const void* LA_down_f16, const void* Wk_down,
+                     const float* w_scale_down, const void* LB_down_f16, int M, int K, int F, int N, int r, int r_down,
+                     int activation, void* Y_f16, void* workspace, size_t workspace_bytes, void* stream) {
+    FfnLayout l;
+    if (!ffn_layout(M, K, F, N, r, r_down, &l)) return fail(ASER_ERR_SHAPE, "unsupported M, K, F, N, r or r_down");
+    GluForm glu;
+    if (!glu_form(activation, &glu)) return fail(ASER_ERR_SHAPE, "unknown activation");
+    if (M == 0 || N == 0) return ASER_OK;
+    // every argument of every launch is checked before the first one is enqueued
+    ASER_REQUIRE_PTR(X_f16);
+    ASER_OPTIONAL_PTR(s);
+    ASER_REQUIRE_PTR(Wk_gu);
+    ASER_REQUIRE_PTR(w_scale_gu);
+    ASER_OPTIONAL_PTR(s_down);
+    ASER_REQUIRE_PTR(Wk_down);
+    ASER_REQUIRE_PTR(w_scale_down);
+    ASER_REQUIRE_PTR(Y_f16);
+    if (r > 0) {
+        ASER_REQUIRE_PTR(LA_f16);
+        ASER_REQUIRE_PTR(LB_gu_f16);
+    }
+    if (r_down > 0) {
+        ASER_REQUIRE_PTR(LA_down_f16);
+        ASER_REQUIRE_PTR(LB_down_f16);
+    }
+    if (workspace == nullptr || misaligned16(workspace) || workspace_bytes < l.total)
+        return fail(ASER_ERR_WORKSPACE, "workspace missing, misaligned or too small");
+    int rc = check_device();
+    if (rc != ASER_OK) return rc;
+    if (!linear_decode_prefers(M, 2 * F, K) && (rc = linear_tc_check(M, 2 * F, K, r, l.kernels)) != ASER_OK) return rc;
+    if (!linear_decode_prefers(M, N, F) && (rc = linear_tc_check(M, N, F, r_down, l.kernels)) != ASER_OK) return rc;
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    int8_t* Xq = reinterpret_cast<int8_t*>(ws + l.Xq);
+    float* a_scale = reinterpret_cast<float*>(ws + l.a_scale);
+    void *T = ws + l.T, *H = ws + l.H;
+    rc = quant_with_workspace(X_f16, s, r > 0 ? LA_f16 : nullptr, M, M, K, r, 8, false, Xq, a_scale, r > 0 ? T : nullptr,
+                              workspace, l.kernels, stream);
+    if (rc != ASER_OK) return rc;
+    rc = linear_common(Xq, a_scale, Wk_gu, w_scale_gu, r > 0 ? T : nullptr, r > 0 ? LB_gu_f16 : nullptr, M, 2 * F, K, r, H,
+                       nullptr, workspace, l.kernels, stream, /*overlap_prev=*/true, 0, CatSplit(), &glu);
+    if (rc != ASER_OK) return rc;
+    rc = quant_with_workspace(H, s_down, r_down > 0 ? LA_down_f16 : nullptr, M, M, F, r_down, 8, false, Xq, a_scale,
+                              r_down > 0 ? T : nullptr, workspace, l.kernels, stream);
+    if (rc != ASER_OK) return rc;
+    return linear_common(Xq, a_scale, Wk_down, w_scale_down, r_down > 0 ? T : nullptr, r_down > 0 ? LB_down_f16 : nullptr, M, N, F,
+                         r_down, Y_f16, nullptr, workspace, l.kernels, stream, /*overlap_prev=*/true);
 }
 
 size_t aser_forward_shared_workspace_bytes(int n_layers, const int* N, const int* r, int M, int K) {

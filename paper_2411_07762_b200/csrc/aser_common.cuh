@@ -70,6 +70,12 @@ struct CatSplit {
 __host__ __device__ inline int cat_layer(const CatSplit& c, int row) {
     return (row >= c.b1 ? 1 : 0) + (row >= c.b2 ? 1 : 0) + (row >= c.b3 ? 1 : 0);
 }
+// A linear launch whose N channels are gate and up in turn writes H = act(gate) * up [M, N / 2] instead of Y (glu_math.cuh);
+// act(g) = g / (1 + exp(-g (c0 + c1 g^2))).
+struct GluForm {
+    float c0 = 0.f, c1 = 0.f;
+};
+// `glu`: the gated form (Y is then H; single layers without accumulator dump).
 // `ldt`: elements between rows of T (0 = r; larger when T is a column range of a wider matrix).
 // `overlap_prev`: the kernel launched before this one on `st` is this library's quant_act for
 // the same step.  The linear kernel may then start while that one still runs: it streams the
@@ -79,7 +85,7 @@ int launch_linear_tc(const int8_t* Xq, const float* a_scale, const uint8_t* Wk,
                      const float* w_scale, const __nv_bfloat16* T, const __half* LB,
                      int M, int N, int K, int r, __half* Y, int32_t* acc_debug,
                      void* workspace, size_t workspace_bytes, cudaStream_t st,
-                     bool overlap_prev = false, int ldt = 0, CatSplit cat = CatSplit());
+                     bool overlap_prev = false, int ldt = 0, CatSplit cat = CatSplit(), const GluForm* glu = nullptr);
 // Layers that read the same codes, each with operands of its own, served by one launch; layer l takes the columns
 // [t_col, t_col + r) of T.
 constexpr int kMaxGroup = 4;
@@ -98,28 +104,31 @@ bool linear_decode_prefers(int M, int N, int K);
 int launch_linear_decode(const int8_t* Xq, const float* a_scale, const uint8_t* Wk,
                          const float* w_scale, const __nv_bfloat16* T, const __half* LB,
                          int M, int N, int K, int r, __half* Y, int32_t* acc_debug,
-                         cudaStream_t st, bool overlap_prev = false, int ldt = 0, CatSplit cat = CatSplit());
+                         cudaStream_t st, bool overlap_prev = false, int ldt = 0, CatSplit cat = CatSplit(),
+                         const GluForm* glu = nullptr);
 int launch_linear_decode_group(const int8_t* Xq, const float* a_scale, const __nv_bfloat16* T, int M, int K,
                                const LinearGroup& group, int32_t* acc_debug, cudaStream_t st, bool overlap_prev, int ldt,
-                               CatSplit cat = CatSplit());
+                               CatSplit cat = CatSplit(), const GluForm* glu = nullptr);
 // Many-token kernel on pairs of CTAs (linear_pair.cu); uses the workspace's status word only.
 // linear_pair_prefers: the shapes for which it is faster than linear_tc (estimates of both, in cycles), where it can
 // run at all.  To be asked before every launch: it also sets the kernel up on its first yes.
 constexpr int kLinearPairMinTokens = 65;
-bool linear_pair_prefers(int M, int N, int K, const CatSplit& cat);
+bool linear_pair_prefers(int M, int N, int K, const CatSplit& cat, bool glu = false);
 int launch_linear_pair(const int8_t* Xq, const float* a_scale, const uint8_t* Wk, const float* w_scale,
                        const __nv_bfloat16* T, const __half* LB, int M, int N, int K, int r, __half* Y,
-                       int32_t* acc_debug, void* workspace, cudaStream_t st, bool overlap_prev, int ldt, CatSplit cat);
+                       int32_t* acc_debug, void* workspace, cudaStream_t st, bool overlap_prev, int ldt, CatSplit cat,
+                       const GluForm* glu = nullptr);
 // linear_pair_groups: whether one launch serves these layers (it also sets the kernel up on its first yes).
 bool linear_pair_groups(const LinearGroup& g, int M, int K);
 int launch_linear_pair_group(const int8_t* Xq, const float* a_scale, const __nv_bfloat16* T, int M, int K, const LinearGroup& g,
                              int32_t* acc_debug, void* workspace, cudaStream_t st, bool overlap_prev, int ldt,
-                             CatSplit cat = CatSplit());
+                             CatSplit cat = CatSplit(), const GluForm* glu = nullptr);
 // Tiles split along K over clusters (linear_split.cu), 17 to 512 tokens; uses the workspace's status word only.
 bool linear_split_prefers(int M, int N, int K);
 int launch_linear_split(const int8_t* Xq, const float* a_scale, const uint8_t* Wk, const float* w_scale,
                         const __nv_bfloat16* T, const __half* LB, int M, int N, int K, int r, __half* Y,
-                        int32_t* acc_debug, void* workspace, cudaStream_t st, bool overlap_prev, int ldt, CatSplit cat);
+                        int32_t* acc_debug, void* workspace, cudaStream_t st, bool overlap_prev, int ldt, CatSplit cat,
+                        const GluForm* glu = nullptr);
 // Estimated cycles of launch_linear_tc with 128-token tiles (M > 64): 530 per 128 x 128 x 128 unit of the
 // fullest CTA, and 8000 of fixed cost, or where tiles are shared between CTAs as much as 32 to 64 more units.
 long long linear_tc_estimate(int M, int N, int K, int num_sms);

@@ -28,6 +28,7 @@
 //   * the weight loads precede griddepcontrol.wait, so under a programmatic dependent launch
 //     they overlap the activation kernel; Xq, a_scale and T are read after it.
 #include "aser_common.cuh"
+#include "glu_math.cuh"
 
 namespace aser {
 
@@ -84,10 +85,11 @@ struct DecCfg {
     static constexpr int MinCtas = (R * B <= 2) ? 4 : 3;
 };
 
-template <int NT, int R, int B, bool GROUP>
+// GLU: the channels are gate and up in turn, a lane of an even channel stores the product with its neighbour's (no dump).
+template <int NT, int R, int B, bool GROUP, bool GLU>
 __global__ void __launch_bounds__(kDecThreads, DecCfg<NT, R, B>::MinCtas)
 linear_decode_kernel(const int8_t* Xq, const float* a_scale, const __nv_bfloat16* T, int M, int K, int ldt,
-                     int32_t* __restrict__ acc_debug, const CatSplit cat, const __grid_constant__ LinearGroup group) {
+                     int32_t* __restrict__ acc_debug, const CatSplit cat, const __grid_constant__ LinearGroup group, const GluForm glu) {
     using C = DecCfg<NT, R, B>;
     constexpr int BATCH = C::Batch;
     // partial sums of the eight warps: integer accumulators and fp32 accumulators of the low-rank term
@@ -269,7 +271,21 @@ linear_decode_kernel(const int8_t* Xq, const float* a_scale, const __nv_bfloat16
         const int idx = threadIdx.x + o * kDecThreads;
         const int row = idx % C::Rows, om = idx / C::Rows, col = om & 7;
         const int on = n0 + row;
-        if (om < M && on < N) {
+        if (GLU) {
+            // neighbouring lanes: the same token, channels 2 i and 2 i + 1
+            float y = 0.f;
+            if (om < M && on < N) {
+                const int reg = ((row >> 4) * NT + (om >> 3)) * 4 + ((row >> 3) & 1) * 2 + (col & 1);
+                const int ln = (row & 7) * 4 + (col >> 1);
+                float lr = 0.f;
+                for (int w = 0; w < lr_warps; ++w) lr += red_lr[w][reg][ln];
+                y = fmaf((float)sums[o], a_scale[om] * (__ldg(w_scale + on) * 0.0625f), lr);
+            }
+            const float own_y = __half2float(__float2half_rn(y));
+            const float up = __shfl_xor_sync(0xffffffffu, own_y, 1);
+            if (om < M && on < N && !(row & 1))
+                Y[(size_t)om * (N / 2) + on / 2] = __float2half_rn(gated_product(own_y, up, glu));
+        } else if (om < M && on < N) {
             const int reg = ((row >> 4) * NT + (om >> 3)) * 4 + ((row >> 3) & 1) * 2 + (col & 1);
             const int ln = (row & 7) * 4 + (col >> 1);
             float lr = 0.f;
@@ -282,9 +298,9 @@ linear_decode_kernel(const int8_t* Xq, const float* a_scale, const __nv_bfloat16
     }
 }
 
-template <int NT, int R, int B>
+template <int NT, int R, int B, bool GLU = false>
 int launch_cfg(const int8_t* Xq, const float* a_scale, const __nv_bfloat16* T, int M, int K, int32_t* acc_debug,
-               cudaStream_t st, bool overlap_prev, int ldt, const CatSplit& cat, const LinearGroup& group) {
+               cudaStream_t st, bool overlap_prev, int ldt, const CatSplit& cat, const LinearGroup& group, const GluForm& glu) {
     int tiles = 0;
     for (int l = 0; l < group.layers; ++l) tiles += (group.N[l] + DecCfg<NT, R, B>::Rows - 1) / DecCfg<NT, R, B>::Rows;
     cudaLaunchConfig_t cfg = {};
@@ -302,16 +318,16 @@ int launch_cfg(const int8_t* Xq, const float* a_scale, const __nv_bfloat16* T, i
     // holds (1 x 4096 x 14336 8.9 / 8.2, 16 x 8192 x 8192 11.2 / 10.9, 8 x 8192 x 8192 8.9 / 8.7).
     cudaError_t e;
     if (NT == 2 && R == 1 && group.layers == 1)
-        e = cudaLaunchKernelEx(&cfg, linear_decode_kernel<NT, R, B, NT != 2 || R != 1>, Xq, a_scale, T, M, K, ldt, acc_debug, cat, group);
+        e = cudaLaunchKernelEx(&cfg, linear_decode_kernel<NT, R, B, NT != 2 || R != 1, GLU>, Xq, a_scale, T, M, K, ldt, acc_debug, cat, group, glu);
     else
-        e = cudaLaunchKernelEx(&cfg, linear_decode_kernel<NT, R, B, true>, Xq, a_scale, T, M, K, ldt, acc_debug, cat, group);
+        e = cudaLaunchKernelEx(&cfg, linear_decode_kernel<NT, R, B, true, GLU>, Xq, a_scale, T, M, K, ldt, acc_debug, cat, group, glu);
     if (e != cudaSuccess) return record_cuda_error(e, "linear_decode_kernel");
     return check_launch("linear_decode_kernel");
 }
 
-template <int NT>
+template <int NT, bool GLU>
 int launch_nt(const int8_t* Xq, const float* a_scale, const __nv_bfloat16* T, int M, int K, int32_t* acc_debug,
-              cudaStream_t st, bool overlap_prev, int ldt, const CatSplit& cat, const LinearGroup& group) {
+              cudaStream_t st, bool overlap_prev, int ldt, const CatSplit& cat, const LinearGroup& group, const GluForm& glu) {
     // Rows per CTA: 32 where that still gives every SM about one and a half CTAs (activation
     // fragments reused twice), else 16 (few output channels: latency matters, every SM gets work).
     int num_sms = 0;
@@ -329,10 +345,10 @@ int launch_nt(const int8_t* Xq, const float* a_scale, const __nv_bfloat16* T, in
     int tiles = 0, rows = 0;
     for (int l = 0; l < group.layers; ++l) { tiles += (group.N[l] + 31) / 32; rows += group.N[l]; }
     if (NT == 1 && tiles > 3 * num_sms && tiles <= 4 * num_sms)
-        return launch_cfg<1, 2, 1>(Xq, a_scale, T, M, K, acc_debug, st, overlap_prev, ldt, cat, group);
+        return launch_cfg<1, 2, 1, GLU>(Xq, a_scale, T, M, K, acc_debug, st, overlap_prev, ldt, cat, group, glu);
     if (rows >= 32 * 3 * num_sms / 2)
-        return launch_cfg<NT, 2, 2>(Xq, a_scale, T, M, K, acc_debug, st, overlap_prev, ldt, cat, group);
-    return launch_cfg<NT, 1, 4>(Xq, a_scale, T, M, K, acc_debug, st, overlap_prev, ldt, cat, group);
+        return launch_cfg<NT, 2, 2, GLU>(Xq, a_scale, T, M, K, acc_debug, st, overlap_prev, ldt, cat, group, glu);
+    return launch_cfg<NT, 1, 4, GLU>(Xq, a_scale, T, M, K, acc_debug, st, overlap_prev, ldt, cat, group, glu);
 }
 
 }  // namespace
@@ -343,24 +359,29 @@ bool linear_decode_prefers(int M, int N, int K) {
 
 int launch_linear_decode_group(const int8_t* Xq, const float* a_scale, const __nv_bfloat16* T, int M, int K,
                                const LinearGroup& group, int32_t* acc_debug, cudaStream_t st, bool overlap_prev, int ldt,
-                               CatSplit cat) {
+                               CatSplit cat, const GluForm* glu) {
     if (M > kLinearDecodeMaxTokens) return record_error(ASER_ERR_SHAPE, "linear_decode: more than 16 tokens");
     if (group.layers > 1 && (acc_debug || cat.layers > 1))
         return record_error(ASER_ERR_SHAPE, "linear_decode: neither accumulators nor fused layers of a group");
-    if (M <= 8) return launch_nt<1>(Xq, a_scale, T, M, K, acc_debug, st, overlap_prev, ldt, cat, group);
-    return launch_nt<2>(Xq, a_scale, T, M, K, acc_debug, st, overlap_prev, ldt, cat, group);
+    if (glu) {
+        if (group.layers > 1 || acc_debug || cat.layers > 1) return record_error(ASER_ERR_SHAPE, "linear_decode: the gated form is of one layer");
+        if (M <= 8) return launch_nt<1, true>(Xq, a_scale, T, M, K, nullptr, st, overlap_prev, ldt, cat, group, *glu);
+        return launch_nt<2, true>(Xq, a_scale, T, M, K, nullptr, st, overlap_prev, ldt, cat, group, *glu);
+    }
+    if (M <= 8) return launch_nt<1, false>(Xq, a_scale, T, M, K, acc_debug, st, overlap_prev, ldt, cat, group, GluForm());
+    return launch_nt<2, false>(Xq, a_scale, T, M, K, acc_debug, st, overlap_prev, ldt, cat, group, GluForm());
 }
 
 int launch_linear_decode(const int8_t* Xq, const float* a_scale, const uint8_t* Wk,
                          const float* w_scale, const __nv_bfloat16* T, const __half* LB,
                          int M, int N, int K, int r, __half* Y, int32_t* acc_debug,
-                         cudaStream_t st, bool overlap_prev, int ldt, CatSplit cat) {
+                         cudaStream_t st, bool overlap_prev, int ldt, CatSplit cat, const GluForm* glu) {
     if (ldt <= 0) ldt = r * cat.layers;
     LinearGroup group = {};
     group.layers = 1;
     group.Wk[0] = Wk; group.w_scale[0] = w_scale; group.LB[0] = LB; group.Y[0] = Y;
     group.N[0] = N; group.r[0] = r;
-    return launch_linear_decode_group(Xq, a_scale, T, M, K, group, acc_debug, st, overlap_prev, ldt, cat);
+    return launch_linear_decode_group(Xq, a_scale, T, M, K, group, acc_debug, st, overlap_prev, ldt, cat, glu);
 }
 
 }  // namespace aser

@@ -41,6 +41,7 @@
 // with a low-rank term.  Sixteen epilogue warps (72 registers at launch) or both halves' sums read at once cost
 // more in spilled registers than they saved there (gate projection 116 -> 122 ... 139 us).
 #include "aser_common.cuh"
+#include "glu_math.cuh"
 #include "sm100_ptx.cuh"
 
 namespace aser {
@@ -95,6 +96,7 @@ struct Params {
     int full, cut, items;  // items [0, full): whole tiles; [full, full + 2 cut): the halves of further tiles; then the short ones
     int tt_outer;          // tile numbering: 1 = token tile outer
     CatSplit cat;
+    GluForm glu;
 };
 
 struct Maps { CUtensorMap lb[kMaxGroup], y[kMaxGroup]; };
@@ -174,7 +176,8 @@ __device__ __forceinline__ void let_copies_land() {
     while (clock64() - t0 < 2000000) {}
 }
 
-template <bool DEBUG_ACC, bool GROUP>
+// GLU: the channels are gate and up in turn, and what leaves is act(gate) * up.
+template <bool DEBUG_ACC, bool GROUP, bool GLU = false>
 __global__ void __launch_bounds__(kThreads, 1)
 linear_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_t,
                    const __grid_constant__ Maps maps, const __grid_constant__ Params p) {
@@ -562,6 +565,14 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 if (h >= w.halves || !ok) continue;
+                if (GLU) {              // rows of 64 products; a lane has one of the two tokens of a register
+                    uint16_t* out = reinterpret_cast<uint16_t*>(smem + kOffLr) + ((h * 2 + side) * kHw + (lane & 1)) * 64 + (q * 32 + lane) / 2;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) out[(c * 16 + 2 * j) * 64] = gated_exchange(y[h][c][j], lane, p.glu);
+                    continue;
+                }
                 uint16_t* stage = reinterpret_cast<uint16_t*>(smem + kOffLr) + ((h * 2 + side) * kHw) * (kYRow / 2) + q * 32 + lane;
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
@@ -578,7 +589,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                 if (n0 < N) {
                     for (int b = 0; b < 2 * w.halves; ++b) {
                         const int tok = w.tok0 + (b & 1) * w.step + (b >> 1) * kHw;
-                        if (tok < p.M) tma_store_2d_tile(&maps.y[w.layer], n0, tok, sbase + kOffLr + b * kHw * kYRow);
+                        if (tok < p.M) tma_store_2d_tile(&maps.y[w.layer], GLU ? n0 / 2 : n0, tok, sbase + kOffLr + b * kHw * (GLU ? 128 : kYRow));
                     }
                     bulk_store_commit();
                     bulk_store_wait_read();
@@ -639,14 +650,14 @@ Plan make_plan(int M, int NT, int pairs) {
 
 // Whether the kernel can run as it was built: the warpgroups' budgets add up to what the block is launched with and to
 // nothing else, so a compiler that gives a thread another number of registers leaves every shape to linear_tc.
-template <bool DEBUG_ACC, bool GROUP>
+template <bool DEBUG_ACC, bool GROUP, bool GLU = false>
 bool configure(int dev) {
     static int state[kMaxDevices] = {0};         // 1: ready, 2: not usable
     if (state[dev] == 0) {
         cudaFuncAttributes a;
-        cudaError_t e = cudaFuncGetAttributes(&a, linear_pair_kernel<DEBUG_ACC, GROUP>);
+        cudaError_t e = cudaFuncGetAttributes(&a, linear_pair_kernel<DEBUG_ACC, GROUP, GLU>);
         const bool fits = e == cudaSuccess && a.numRegs == kRegsLaunch;
-        if (fits) e = cudaFuncSetAttribute(linear_pair_kernel<DEBUG_ACC, GROUP>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+        if (fits) e = cudaFuncSetAttribute(linear_pair_kernel<DEBUG_ACC, GROUP, GLU>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
         if (e != cudaSuccess) (void)cudaGetLastError();
         state[dev] = fits && e == cudaSuccess ? 1 : 2;
     }
@@ -662,13 +673,14 @@ bool configure(int dev) {
 // which pairs do not do.  Looked at again on 920 points (18 layer shapes of 1152 to 28672 columns, 65 to 4096 tokens drawn,
 // ranks 0, 64 and 128; linear step in a graph): 1.153 times as fast as linear_tc alone in the geometric mean, four points slower
 // by more than 1.5 %, the worst 6 % (1027 x 8192 x 28672: a short column of three tokens costs a pass over its weights).
-bool linear_pair_prefers(int M, int N, int K, const CatSplit& cat) {
+bool linear_pair_prefers(int M, int N, int K, const CatSplit& cat, bool glu) {
     if (M < kLinearPairMinTokens) return false;
     if (cat.layers > 1 && ((cat.b1 | (cat.layers > 2 ? cat.b2 : 0) | (cat.layers > 3 ? cat.b3 : 0)) & 255)) return false;
     int num_sms = 0, dev = 0;
     if (device_sm_count(&num_sms) != ASER_OK || num_sms < 2 || current_device(&dev) != ASER_OK) return false;
     const long long stages = (K / kWkCols + kKS - 1) / kKS;
     if (make_plan(M, (N + 255) / 256, num_sms / 2).cost * stages + 12000 >= linear_tc_estimate(M, N, K, num_sms)) return false;
+    if (glu) return configure<false, false, true>(dev);
     return configure<false, false>(dev) && configure<true, false>(dev);
 }
 
@@ -685,7 +697,10 @@ bool linear_pair_groups(const LinearGroup& g, int M, int K) {
 }
 
 int launch_linear_pair_group(const int8_t* Xq, const float* a_scale, const __nv_bfloat16* T, int M, int K, const LinearGroup& g,
-                             int32_t* acc_debug, void* workspace, cudaStream_t st, bool overlap_prev, int ldt, CatSplit cat) {
+                             int32_t* acc_debug, void* workspace, cudaStream_t st, bool overlap_prev, int ldt, CatSplit cat,
+                             const GluForm* glu) {
+    if (glu && (g.layers > 1 || acc_debug || cat.layers > 1))
+        return record_error(ASER_ERR_SHAPE, "linear_pair: the gated form is of one layer");
     if (g.layers > 1 && (acc_debug || cat.layers > 1))
         return record_error(ASER_ERR_SHAPE, "linear_pair: neither accumulators nor fused layers of a group");
     int num_sms = 0;
@@ -715,7 +730,8 @@ int launch_linear_pair_group(const int8_t* Xq, const float* a_scale, const __nv_
     }
     for (int l = 0; l < kMaxGroup; ++l) {
         if (l >= g.layers) { maps.y[l] = maps.y[0]; maps.lb[l] = maps.lb[0]; continue; }
-        rc = encode_map_2d(&maps.y[l], CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, g.Y[l], M, g.N[l], kHw, 128, CU_TENSOR_MAP_SWIZZLE_NONE);
+        rc = encode_map_2d(&maps.y[l], CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, g.Y[l], M, glu ? g.N[l] / 2 : g.N[l], kHw, glu ? 64 : 128,
+                           CU_TENSOR_MAP_SWIZZLE_NONE);
         if (rc != ASER_OK) return rc;
         maps.lb[l] = mx;
         if (r > 0) rc = encode_map_2d(&maps.lb[l], CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, g.LB[l], g.N[l], r, 128, 64, CU_TENSOR_MAP_SWIZZLE_128B);
@@ -729,6 +745,7 @@ int launch_linear_pair_group(const int8_t* Xq, const float* a_scale, const __nv_
     // the smaller of the two operand sets stays in L2 while the other is streamed (as in linear_tc.cu)
     p.tt_outer = ((long long)M * K > rows * K / 2) ? 1 : 0;
     p.cat = cat;
+    if (glu) p.glu = *glu;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(2 * (plan.items < pairs ? plan.items : pairs), 1, 1);
     cfg.blockDim = dim3(kThreads, 1, 1);
@@ -741,7 +758,8 @@ int launch_linear_pair_group(const int8_t* Xq, const float* a_scale, const __nv_
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = overlap_prev ? 2 : 1;
-    const cudaError_t e = g.layers > 1 ? cudaLaunchKernelEx(&cfg, linear_pair_kernel<false, true>, mx, mt, maps, p)
+    const cudaError_t e = glu            ? cudaLaunchKernelEx(&cfg, linear_pair_kernel<false, false, true>, mx, mt, maps, p)
+                          : g.layers > 1 ? cudaLaunchKernelEx(&cfg, linear_pair_kernel<false, true>, mx, mt, maps, p)
                           : acc_debug  ? cudaLaunchKernelEx(&cfg, linear_pair_kernel<true, false>, mx, mt, maps, p)
                                        : cudaLaunchKernelEx(&cfg, linear_pair_kernel<false, false>, mx, mt, maps, p);
     if (e != cudaSuccess) return record_cuda_error(e, "linear_pair_kernel");
@@ -750,12 +768,13 @@ int launch_linear_pair_group(const int8_t* Xq, const float* a_scale, const __nv_
 
 int launch_linear_pair(const int8_t* Xq, const float* a_scale, const uint8_t* Wk, const float* w_scale,
                        const __nv_bfloat16* T, const __half* LB, int M, int N, int K, int r, __half* Y,
-                       int32_t* acc_debug, void* workspace, cudaStream_t st, bool overlap_prev, int ldt, CatSplit cat) {
+                       int32_t* acc_debug, void* workspace, cudaStream_t st, bool overlap_prev, int ldt, CatSplit cat,
+                       const GluForm* glu) {
     LinearGroup g = {};
     g.layers = 1;
     g.Wk[0] = Wk; g.w_scale[0] = w_scale; g.LB[0] = LB; g.Y[0] = Y;
     g.N[0] = N; g.r[0] = r;
-    return launch_linear_pair_group(Xq, a_scale, T, M, K, g, acc_debug, workspace, st, overlap_prev, ldt, cat);
+    return launch_linear_pair_group(Xq, a_scale, T, M, K, g, acc_debug, workspace, st, overlap_prev, ldt, cat, glu);
 }
 
 }  // namespace aser

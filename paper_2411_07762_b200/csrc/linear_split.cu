@@ -29,6 +29,7 @@
 // 8192, cold, L2 is 18 % busy, HBM 22, the SM 22; set-up takes 1.2 us, exchange and outputs 3, and between them a stage brings 44 KB
 // to every SM (activations are read once per 128 channels).
 #include "aser_common.cuh"
+#include "glu_math.cuh"
 #include "sm100_ptx.cuh"
 
 namespace aser {
@@ -57,6 +58,7 @@ struct Params {
     int tok, own;          // tokens of a tile, tokens that a CTA of the cluster finishes (multiples of 16)
     int TT;                // token tiles
     CatSplit cat;
+    GluForm glu;
 };
 
 // Shared memory behind a 1024-byte boundary: activation ring (later the staged sums and outputs), received sums, low-rank
@@ -131,6 +133,8 @@ __device__ __forceinline__ void send(uint32_t dst, uint32_t src, uint32_t bytes,
 }
 
 // Grid: S * NT * TT CTAs in clusters of S; cluster = nt * TT + tt.
+// GLU: the channels are gate and up in turn, and what leaves is act(gate) * up (no dump).
+template <bool GLU>
 __global__ void __launch_bounds__(kThreads, 1)
 linear_split_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_lb,
                     const __grid_constant__ CUtensorMap map_t, const __grid_constant__ CUtensorMap map_y,
@@ -406,6 +410,16 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
                 const int m0 = tok0 + own0 + c;
                 // outputs as [token][128 channels]: where this CTA's own sums would be staged (nobody sends those)
                 uint16_t* out = reinterpret_cast<uint16_t*>(smem + (size_t)own0 * 512) + c * 128 + row;
+                if (GLU) {          // rows of 64 products
+                    out = reinterpret_cast<uint16_t*>(smem + (size_t)own0 * 512) + (c + (lane & 1)) * 64 + row / 2;
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2) {
+                        const float y0 = fmaf((float)(int)v[e], scales[c + e] * ws16, chunks > 0 ? __uint_as_float(f[e]) : 0.f);
+                        const float y1 = fmaf((float)(int)v[e + 1], scales[c + e + 1] * ws16, chunks > 0 ? __uint_as_float(f[e + 1]) : 0.f);
+                        out[e * 64] = gated_exchange(pack_f16(y0, y1), lane, p.glu);
+                    }
+                    continue;
+                }
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const float y = fmaf((float)(int)v[e], scales[c + e] * ws16, chunks > 0 ? __uint_as_float(f[e]) : 0.f);
@@ -418,7 +432,7 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
         ok = named_bar_all(1, kUnpackWarps * 32, ok);
         if (threadIdx.x == 0 && ok) {
             for (int c = 0; c < owned; c += 16)
-                if (tok0 + own0 + c < p.M) tma_store_2d_tile(&map_y, n0, tok0 + own0 + c, sb + (uint32_t)(own0 * 512 + c * 256));
+                if (tok0 + own0 + c < p.M) tma_store_2d_tile(&map_y, GLU ? n0 / 2 : n0, tok0 + own0 + c, sb + (uint32_t)(own0 * 512 + c * (GLU ? 128 : 256)));
             bulk_store_commit();
             bulk_store_wait_read();      // (the stores themselves are complete when the kernel is)
         }
@@ -448,7 +462,8 @@ int configure() {
     const int rc = current_device(&dev);
     if (rc != ASER_OK) return rc;
     if (!done[dev]) {
-        const cudaError_t e = cudaFuncSetAttribute(linear_split_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+        cudaError_t e = cudaFuncSetAttribute(linear_split_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(linear_split_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
         if (e != cudaSuccess) return record_cuda_error(e, "linear_split smem attribute");
         done[dev] = 1;
     }
@@ -472,7 +487,7 @@ int active_clusters(int S) {
         cfg.attrs = attr;
         cfg.numAttrs = 1;
         int n = 0;
-        if (cudaOccupancyMaxActiveClusters(&n, linear_split_kernel, &cfg) != cudaSuccess) {
+        if (cudaOccupancyMaxActiveClusters(&n, linear_split_kernel<false>, &cfg) != cudaSuccess) {
             (void)cudaGetLastError();
             n = 0;
         }
@@ -508,13 +523,14 @@ bool linear_split_prefers(int M, int N, int K) {
 
 int launch_linear_split(const int8_t* Xq, const float* a_scale, const uint8_t* Wk, const float* w_scale,
                         const __nv_bfloat16* T, const __half* LB, int M, int N, int K, int r, __half* Y,
-                        int32_t* acc_debug, void* workspace, cudaStream_t st, bool overlap_prev, int ldt, CatSplit cat) {
+                        int32_t* acc_debug, void* workspace, cudaStream_t st, bool overlap_prev, int ldt, CatSplit cat,
+                        const GluForm* glu) {
     const Plan plan = make_plan(M, N, K);
     if (plan.S == 0) return record_error(ASER_ERR_SHAPE, "linear_split: too many tiles");
     int rc = configure();
     if (rc != ASER_OK) return rc;
     CUtensorMap mx, mlb, mt, my;
-    rc = encode_map_2d(&my, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, Y, M, N, 16, 128, CU_TENSOR_MAP_SWIZZLE_NONE);
+    rc = encode_map_2d(&my, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, Y, M, glu ? N / 2 : N, 16, glu ? 64 : 128, CU_TENSOR_MAP_SWIZZLE_NONE);
     if (rc != ASER_OK) return rc;
     rc = encode_map_blocks(&mx, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, Xq, M, K, plan.tok, 2);
     if (rc != ASER_OK) return rc;
@@ -534,6 +550,7 @@ int launch_linear_split(const int8_t* Xq, const float* a_scale, const uint8_t* W
     p.M = M; p.N = N; p.r = r; p.KB = K / kWkCols;
     p.tok = plan.tok; p.own = plan.own; p.TT = plan.TT;
     p.cat = cat;
+    if (glu) p.glu = *glu;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(plan.S * plan.NT * plan.TT, 1, 1);
     cfg.blockDim = dim3(kThreads, 1, 1);
@@ -546,7 +563,8 @@ int launch_linear_split(const int8_t* Xq, const float* a_scale, const uint8_t* W
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = overlap_prev ? 2 : 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, linear_split_kernel, mx, mlb, mt, my, p, plan.S);
+    const cudaError_t e = glu ? cudaLaunchKernelEx(&cfg, linear_split_kernel<true>, mx, mlb, mt, my, p, plan.S)
+                              : cudaLaunchKernelEx(&cfg, linear_split_kernel<false>, mx, mlb, mt, my, p, plan.S);
     if (e != cudaSuccess) return record_cuda_error(e, "linear_split_kernel");
     return check_launch("linear_split_kernel");
 }

@@ -24,6 +24,7 @@
 // rather than 608 for 64 and 128 tokens: with 608 the finishing of shared tiles spills more, 1500 x 512 x 8192 33.5 -> 37.8.)
 // Every wait is bounded: on expiry the CTA sets the status word and winds down.
 #include "aser_common.cuh"
+#include "glu_math.cuh"
 #include "sm100_ptx.cuh"
 
 namespace aser {
@@ -109,6 +110,7 @@ struct Params {
     int tail_first;        // work order: 1 = both shared tiles first, 0 = range order
     int tt_outer;          // tile numbering: 1 = token tile outer (consecutive tiles share the activations)
     CatSplit cat;          // layers stacked along N: which columns of T a weight tile multiplies
+    GluForm glu;
 };
 
 struct Work {
@@ -280,7 +282,8 @@ __device__ __forceinline__ bool group_mbar_wait(uint32_t bar, uint32_t parity, c
 // ---------------------------------------------------------------------------
 // MID: the mid-tile schedule for the low-rank chunks is compiled in (only useful, and only
 // instantiated, for 128-token tiles with r > 64; the other variants keep their loops free of it).
-template <int BT, bool MID>
+// GLU: the channels are gate and up in turn, and what is stored is act(gate) * up (no dump).
+template <int BT, bool MID, bool GLU>
 __global__ void __launch_bounds__(Cfg<BT>::Threads, 1)
 linear_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_lb,
                  const __grid_constant__ CUtensorMap map_t, const Params p) {
@@ -795,6 +798,18 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
 #pragma unroll
                         for (int j = 0; j < 16; ++j) as[j] = (c0 + j < valid) ? __ldg(p.a_scale + tok0 + c0 + j) : 0.f;
                     }
+                    if (GLU) {
+#pragma unroll
+                        for (int j = 0; j < 16; j += 2) {
+                            const float y0 = fmaf((float)(int)vi[j], as[j] * ws16, w.has_lr ? __uint_as_float(vf[j]) : 0.f);
+                            const float y1 = fmaf((float)(int)vi[j + 1], as[j + 1] * ws16, w.has_lr ? __uint_as_float(vf[j + 1]) : 0.f);
+                            const unsigned short h = gated_exchange(pack_f16(y0, y1), lane, p.glu);
+                            const int tok = c0 + j + (lane & 1);
+                            if (tok < valid && n_ok)
+                                __stcs(reinterpret_cast<unsigned short*>(p.Y + (size_t)(tok0 + tok) * (p.N / 2) + n / 2), h);
+                        }
+                        continue;
+                    }
                     const uint32_t row0 = (uint32_t)(tok0 + c0) * (uint32_t)p.N + (uint32_t)n;
 #pragma unroll
                     for (int j = 0; j < 16; ++j) {
@@ -903,6 +918,22 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
                         }
                         const uint32_t row0 = (uint32_t)(tok0 + c0) * (uint32_t)p.N + (uint32_t)n;
                         const uint32_t* lrw = reinterpret_cast<const uint32_t*>(lr4);
+                        if (GLU) {
+#pragma unroll
+                            for (int j = 0; j < 16; j += 2) {
+                                float y[2];
+#pragma unroll
+                                for (int e = 0; e < 2; ++e) {
+                                    const float as = c0 + j + e < valid ? __ldg(p.a_scale + tok0 + c0 + j + e) : 0.f;
+                                    y[e] = fmaf((float)sum[j + e], as * ws16, p.r > 0 ? __uint_as_float(lrw[j + e]) : 0.f);
+                                }
+                                const unsigned short h = gated_exchange(pack_f16(y[0], y[1]), lane, p.glu);
+                                const int tok = c0 + j + (lane & 1);
+                                if (tok < valid && n_ok)
+                                    __stcs(reinterpret_cast<unsigned short*>(p.Y + (size_t)(tok0 + tok) * (p.N / 2) + n / 2), h);
+                            }
+                            continue;
+                        }
 #pragma unroll
                         for (int j = 0; j < 16; ++j) {
                             if (c0 + j < valid && n_ok) {
@@ -1018,7 +1049,7 @@ int pick_grid(const Layout& L, int num_sms) {
     return grid;
 }
 
-template <int BT, bool MID>
+template <int BT, bool MID, bool GLU>
 int launch_bt(const CUtensorMap& mx, const CUtensorMap& mlb, const CUtensorMap& mt, const Params& p,
               int grid, cudaStream_t st, bool overlap_prev) {
     using C = Cfg<BT>;
@@ -1027,7 +1058,7 @@ int launch_bt(const CUtensorMap& mx, const CUtensorMap& mlb, const CUtensorMap& 
     const int drc = current_device(&dev);
     if (drc != ASER_OK) return drc;
     if (!configured[dev]) {
-        cudaError_t e = cudaFuncSetAttribute(linear_tc_kernel<BT, MID>,
+        cudaError_t e = cudaFuncSetAttribute(linear_tc_kernel<BT, MID, GLU>,
                                              cudaFuncAttributeMaxDynamicSharedMemorySize, C::SmemBytes);
         if (e != cudaSuccess) return record_cuda_error(e, "linear_tc smem attribute");
         configured[dev] = true;
@@ -1042,7 +1073,7 @@ int launch_bt(const CUtensorMap& mx, const CUtensorMap& mlb, const CUtensorMap& 
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = overlap_prev ? 1 : 0;
-    cudaError_t e = cudaLaunchKernelEx(&cfg, linear_tc_kernel<BT, MID>, mx, mlb, mt, p);
+    cudaError_t e = cudaLaunchKernelEx(&cfg, linear_tc_kernel<BT, MID, GLU>, mx, mlb, mt, p);
     if (e != cudaSuccess) return record_cuda_error(e, "linear_tc_kernel");
     return check_launch("linear_tc_kernel");
 }
@@ -1079,7 +1110,8 @@ int launch_linear_tc(const int8_t* Xq, const float* a_scale, const uint8_t* Wk,
                      const float* w_scale, const __nv_bfloat16* T, const __half* LB,
                      int M, int N, int K, int r, __half* Y, int32_t* acc_debug,
                      void* workspace, size_t workspace_bytes, cudaStream_t st, bool overlap_prev, int ldt,
-                     CatSplit cat) {
+                     CatSplit cat, const GluForm* glu) {
+    if (glu && (acc_debug || cat.layers > 1)) return record_error(ASER_ERR_SHAPE, "linear_tc: the gated form is of one layer");
     Layout L = make_layout(M, N, K, r);
     const int pre = linear_tc_check(M, N, K, r, workspace_bytes);
     if (pre != ASER_OK) return pre;
@@ -1115,6 +1147,7 @@ int launch_linear_tc(const int8_t* Xq, const float* a_scale, const uint8_t* Wk,
     p.part_lr = reinterpret_cast<float*>(ws + L.off_part_lr);
     p.M = M; p.N = N; p.K = K; p.r = r;
     p.cat = cat;
+    if (glu) p.glu = *glu;
     p.KB = L.KB; p.TT = L.TT; p.NT = L.NT; p.units = (int)L.units;
     // Both shared tiles first where a tile is long enough (K >= 8192) to hide two cross-CTA
     // reductions behind the next tiles' MMAs; with shorter tiles the epilogue warps fall behind
@@ -1129,12 +1162,18 @@ int launch_linear_tc(const int8_t* Xq, const float* a_scale, const uint8_t* Wk,
     p.tt_outer = ((long long)M * K > (long long)N * K / 2) ? 1 : 0;
 
     switch (L.BT) {
-        case 16: return launch_bt<16, false>(mx, mlb, mt, p, grid, st, overlap_prev);
-        case 32: return launch_bt<32, false>(mx, mlb, mt, p, grid, st, overlap_prev);
-        case 64: return launch_bt<64, false>(mx, mlb, mt, p, grid, st, overlap_prev);
+        case 16: return glu ? launch_bt<16, false, true>(mx, mlb, mt, p, grid, st, overlap_prev)
+                            : launch_bt<16, false, false>(mx, mlb, mt, p, grid, st, overlap_prev);
+        case 32: return glu ? launch_bt<32, false, true>(mx, mlb, mt, p, grid, st, overlap_prev)
+                            : launch_bt<32, false, false>(mx, mlb, mt, p, grid, st, overlap_prev);
+        case 64: return glu ? launch_bt<64, false, true>(mx, mlb, mt, p, grid, st, overlap_prev)
+                            : launch_bt<64, false, false>(mx, mlb, mt, p, grid, st, overlap_prev);
         default:
-            if (r > 64) return launch_bt<128, true>(mx, mlb, mt, p, grid, st, overlap_prev);
-            return launch_bt<128, false>(mx, mlb, mt, p, grid, st, overlap_prev);
+            if (glu)
+                return r > 64 ? launch_bt<128, true, true>(mx, mlb, mt, p, grid, st, overlap_prev)
+                              : launch_bt<128, false, true>(mx, mlb, mt, p, grid, st, overlap_prev);
+            if (r > 64) return launch_bt<128, true, false>(mx, mlb, mt, p, grid, st, overlap_prev);
+            return launch_bt<128, false, false>(mx, mlb, mt, p, grid, st, overlap_prev);
     }
 }
 

@@ -1,0 +1,48 @@
+"""Refusals of the entry points for feed-forward blocks and adapters: bad arguments are rejected with an error code before
+anything is launched (no GPU needed)."""
+import ctypes as C
+
+import pytest
+
+OK, NULL, ALIGN, SHAPE, WORKSPACE = 0, -1, -2, -3, -4
+GOOD, ODD = C.c_void_p(0x1000), C.c_void_p(0x1004)
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2411_07762_b200 import build
+    build.build()
+    from paper_2411_07762_b200 import binding
+    return binding.lib
+
+
+def test_gated_linear_is_refused(lib):
+    def call(M=4, N=256, K=128, r=16, act=0, Xq=GOOD, T=GOOD, LB=GOOD, H=GOOD, ws=GOOD, nbytes=1 << 26):
+        return lib.aser_linear_w4a8_lr_glu(Xq, GOOD, GOOD, GOOD, T, LB, M, N, K, r, act, H, ws, nbytes, None)
+    assert call(M=0, Xq=None, ws=None) == OK
+    assert call(N=264) == SHAPE and call(K=100) == SHAPE and call(r=8) == SHAPE and call(r=272) == SHAPE and call(M=-1) == SHAPE
+    assert call(act=2) == SHAPE and call(act=-1) == SHAPE
+    assert call(Xq=None) == NULL and call(T=None) == NULL and call(LB=None) == NULL and call(H=None) == NULL
+    assert call(H=ODD) == ALIGN
+    assert call(ws=None) == WORKSPACE and call(nbytes=1000) == WORKSPACE and call(ws=ODD) == WORKSPACE
+
+
+def test_feed_forward_is_refused(lib):
+    def call(M=4, K=128, F=256, N=128, r=16, rd=16, act=0, X=GOOD, LA=GOOD, LAd=GOOD, sd=None, Y=GOOD, ws=GOOD, nbytes=1 << 26):
+        return lib.aser_forward_ffn(X, None, LA, GOOD, GOOD, GOOD, sd, LAd, GOOD, GOOD, GOOD, M, K, F, N, r, rd, act, Y, ws,
+                                    nbytes, None)
+    assert call(M=0, X=None, ws=None) == OK
+    assert call(F=200) == SHAPE and call(K=130) == SHAPE and call(N=4) == SHAPE and call(rd=24) == SHAPE and call(F=0) == SHAPE
+    assert call(act=7) == SHAPE and call(M=-2) == SHAPE and call(F=-128) == SHAPE
+    assert call(X=None) == NULL and call(LA=None) == NULL and call(LAd=None) == NULL and call(Y=None) == NULL
+    assert call(sd=ODD) == ALIGN and call(Y=ODD) == ALIGN
+    need = lib.aser_forward_ffn_workspace_bytes(4, 128, 256, 128, 16, 16)
+    assert need > 0 and call(nbytes=need - 1) == WORKSPACE and call(ws=None) == WORKSPACE
+    assert lib.aser_forward_ffn_workspace_bytes(4, 128, 200, 128, 16, 16) == 0
+    assert lib.aser_forward_ffn_workspace_bytes(4, 128, 256, 128, 16, 17) == 0
+
+
+@pytest.mark.parametrize("K,F,N,r,rd", [(4096, 14336, 4096, 64, 64), (512, 1024, 512, 256, 16), (128, 128, 8, 0, 256), (1024, 512, 64, 0, 0)])
+def test_a_workspace_serves_fewer_tokens(lib, K, F, N, r, rd):
+    need = [lib.aser_forward_ffn_workspace_bytes(m, K, F, N, r, rd) for m in range(1, 2100)]
+    assert all(a <= b for a, b in zip(need, need[1:]))
