@@ -293,6 +293,40 @@ int aser_forward_ffn(const void* X_f16, const float* s, const void* LA_f16, cons
                      int activation, void* Y_f16, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Low-rank adapters of many requests beside a shared projection (fine-tuned variants of one model served together): token m
+ * names an adapter a of a pool, or none, and
+ *     out[m, :] = fp16( Y[m, :] + scale[a] * B_a (A_a x[m]) )            (fp32 sums; A_a x scaled by a power of two and
+ *                                                                        rounded to fp16 between the two products)
+ * x is the activation itself, not the smoothed one.  A_f16 [n_slots, r, K], B_f16 [n_slots, N, r]; ranks [n_slots] int32 (NULL: all r):
+ * adapter a is of rank ranks[a], a multiple of 16 from 0 to r (other values are taken down to one); rows of A and columns of B
+ * behind it are not read.  scale [n_slots] fp32 (NULL: ones).  r % 16 == 0, r <= 256, 1 <= n_slots <= 4096.
+ *
+ * aser_adapters_plan -- lists a batch's tokens by adapter: slot [M] int32, the adapter of each token; any value outside
+ * 0 .. n_slots - 1 means none (the padding of a batch, too).  One plan serves every adapter call of a step, whatever its layer; it is
+ * made on the device, so a captured graph that starts with it follows the slots of each replay.  plan: aser_adapters_plan_bytes(M,
+ * n_slots) bytes (0 for bad sizes), contents irrelevant.
+ *
+ * aser_adapters_add -- the update above.  Y [M, N] and out [M, N] may be one matrix (in place: rows without an adapter are then
+ * not touched; else they are copied); other overlaps of out with Y, X or the adapters are not allowed.  ldx, ldy, ldo: elements between rows,
+ * multiples of 8 (0: K, N, N), so a projection of a fused group is a column range.  plan must be one of these M and
+ * n_slots, made by work that precedes the call on `stream` (a plan of other sizes makes the call write nothing).  One launch, no
+ * workspace.
+ *
+ * aser_forward_adapters -- aser_forward, then the adapters of its tokens added to Y in place, enqueued together.  All
+ * arguments are checked before anything is.
+ */
+size_t aser_adapters_plan_bytes(int M, int n_slots);
+int aser_adapters_plan(const int32_t* slot, int M, int n_slots, void* plan, size_t plan_bytes, void* stream);
+int aser_adapters_add(const void* X_f16, int ldx, const void* A_f16, const void* B_f16, const int32_t* ranks,
+                      const float* scale, const void* plan, size_t plan_bytes, int M, int N, int K, int r, int n_slots,
+                      const void* Y_f16, int ldy, void* out_f16, int ldo, void* stream);
+int aser_forward_adapters(const void* X_f16, const float* s, const void* LA_f16, const void* Wk, const float* w_scale,
+                          const void* LB_f16, int M, int N, int K, int r, int8_t* Xq, float* a_scale, void* T_bf16,
+                          void* Y_f16, void* workspace, size_t workspace_bytes, const void* A_f16, const void* B_f16,
+                          const int32_t* ranks, const float* scale, const void* plan, size_t plan_bytes, int r_adapter,
+                          int n_slots, void* stream);
+
+/*
  * aser_forward_shared -- the forward pass of n_layers layers that read the SAME activation X
  * and share the smoothing vector s (Algorithm 1 builds each layer's factors on its own; where
  * the layers' inputs and s coincide their activation work is identical): X is smoothed and

@@ -15,7 +15,7 @@ _BINDING_NAMES = (
     "workspace_bytes", "new_workspace", "check_status", "forward_host",
     "AserLinear", "EXPORTED_SYMBOLS", "pad_rank", "pair_up_projection", "quant_act_ws", "quant_workspace_bytes", "quant_act_ws_launches", "forward_act_launches",
     "linear_w4a8_lr_ld", "AserSharedInput", "AserSharedInputCat", "construct",
-    "AserGatedFFN", "interleave_gate_up", "linear_w4a8_lr_glu", "ACTIVATIONS",
+    "AserGatedFFN", "interleave_gate_up", "linear_w4a8_lr_glu", "ACTIVATIONS", "AserAdapters", "AdapterPlan",
 )
 
 

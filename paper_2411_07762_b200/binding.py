@@ -17,6 +17,7 @@ EXPORTED_SYMBOLS = (
     "aser_forward_shared_workspace_bytes", "aser_construct", "aser_construct_workspace_bytes", "aser_linear_w4a8_lr", "aser_linear_w4a8", "aser_linear_w4a8_lr_simt", "aser_linear_w4a8_lr_static",
     "aser_workspace_bytes", "aser_workspace_init", "aser_check_status", "aser_forward",
     "aser_forward_host", "aser_linear_w4a8_lr_glu", "aser_forward_ffn_workspace_bytes", "aser_forward_ffn",
+    "aser_adapters_plan_bytes", "aser_adapters_plan", "aser_adapters_add", "aser_forward_adapters",
     "aser_last_error", "aser_version",
 )
 
@@ -67,6 +68,12 @@ lib.aser_linear_w4a8_lr_glu.argtypes = [_P, _P, _P, _P, _P, _P, _I, _I, _I, _I, 
 lib.aser_forward_ffn_workspace_bytes.argtypes = [_I, _I, _I, _I, _I, _I]
 lib.aser_forward_ffn_workspace_bytes.restype = _Z
 lib.aser_forward_ffn.argtypes = [_P] * 11 + [_I] * 7 + [_P, _P, _Z, _P]
+lib.aser_adapters_plan_bytes.argtypes = [_I, _I]
+lib.aser_adapters_plan_bytes.restype = _Z
+lib.aser_adapters_plan.argtypes = [_P, _I, _I, _P, _Z, _P]
+lib.aser_adapters_add.argtypes = [_P, _I, _P, _P, _P, _P, _P, _Z, _I, _I, _I, _I, _I, _P, _I, _P, _I, _P]
+lib.aser_forward_adapters.argtypes = [_P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _P, _P, _P, _P, _P, _Z,
+                                      _P, _P, _P, _P, _P, _Z, _I, _I, _P]
 lib.aser_construct_workspace_bytes.argtypes = [_I, _I, _I, _I, _I]
 lib.aser_construct_workspace_bytes.restype = _Z
 lib.aser_construct.argtypes = [_P, _P, _P, _I, _I, _I, _I, C.c_double, _I, _P, _P, _P, _P, _P, _P, _P, _I, _P, _Z, _P]
@@ -408,9 +415,13 @@ class AserLinear:
                                       _ptr(acc_debug), _ptr(self.ws), self.ws.numel(), _stream()),
                  "aser_linear_w4a8")
 
-    def __call__(self, X: torch.Tensor, lowrank: bool = True) -> torch.Tensor:
-        """One forward pass through aser_forward (quantization and linear kernel overlapped)."""
+    def __call__(self, X: torch.Tensor, lowrank: bool = True, adapters: "AserAdapters | None" = None,
+                 plan: "AdapterPlan | None" = None) -> torch.Tensor:
+        """One forward pass through aser_forward (quantization and linear kernel overlapped); with `adapters` and the
+        `plan` of the batch through aser_forward_adapters."""
         M = X.shape[0]
+        if adapters is not None:
+            return adapters._forward(self, X, plan, lowrank)
         assert M <= self.max_tokens
         r = self.r if lowrank else 0       # the plain W4A8 control: the same entry point at rank 0
         s, Y, ws = self.s, self.Y, self.ws
@@ -537,6 +548,103 @@ class AserSharedInputCat(AserSharedInput):
                                          _ptr(self.T) if self.r_total else None, _ptr(self.Y_cat),
                                          _ptr(self.ws), self.ws.numel(), _stream()), "aser_forward_shared_cat")
         return self._views(M)
+
+
+def _rows(v: torch.Tensor, M: int, cols: int, name: str) -> int:
+    """Elements between the rows of an fp16 matrix [M, cols] whose rows are contiguous."""
+    if not v.is_cuda or v.dtype != torch.float16 or v.dim() != 2 or v.shape[0] != M or v.shape[1] != cols:
+        raise TypeError("%s: need a CUDA tensor of torch.float16, [%d, %d]" % (name, M, cols))
+    ld, step = v.stride()
+    if M <= 1 and (cols <= 1 or step == 1):
+        return cols                                     # (the stride of a dimension of one element says nothing)
+    if step != 1 or ld < cols:
+        raise TypeError("%s: rows need to be contiguous and apart" % name)
+    return ld
+
+
+class AdapterPlan:
+    """The tokens of a batch by adapter (aser_adapters_plan): made once, used by the adapters of every layer of a step.
+    `update` follows new slots in the same memory, also inside a captured graph."""
+
+    def __init__(self, slot: torch.Tensor, n_slots: int):
+        self.M, self.n_slots = slot.numel(), n_slots
+        nbytes = int(lib.aser_adapters_plan_bytes(self.M, n_slots))
+        if nbytes == 0:
+            raise ValueError("unsupported number of tokens or adapters")
+        self.nbytes = nbytes
+        self.data = torch.empty((nbytes,), dtype=torch.uint8, device=slot.device)
+        self.update(slot)
+
+    def update(self, slot: torch.Tensor) -> "AdapterPlan":
+        _dev(slot, torch.int32, "slot")
+        if slot.dim() != 1 or slot.numel() != self.M:
+            raise ValueError("slot needs one dimension of %d tokens" % self.M)
+        _chk(lib.aser_adapters_plan(_ptr(slot), self.M, self.n_slots, _ptr(self.data), self.nbytes, _stream()),
+             "aser_adapters_plan")
+        return self
+
+
+class AserAdapters:
+    """A pool of low-rank adapters of one projection: A fp16 [slots, r, K], B fp16 [slots, N, r], with a rank each (int32
+    [slots], multiples of 16; None: all r) and a factor each (fp32 [slots]; None: ones).  The pool's tensors are used in place,
+    so an adapter is exchanged by writing to them."""
+
+    def __init__(self, A: torch.Tensor, B: torch.Tensor, scale: torch.Tensor | None = None,
+                 ranks: torch.Tensor | None = None):
+        _dev(A, torch.float16, "A")
+        _dev(B, torch.float16, "B")
+        if A.dim() != 3 or B.dim() != 3 or A.shape[0] != B.shape[0] or A.shape[1] != B.shape[2]:
+            raise ValueError("need A [slots, r, K] and B [slots, N, r]")
+        self.n_slots, self.r, self.K = A.shape
+        self.N = B.shape[1]
+        for v, dtype, name in ((scale, torch.float32, "scale"), (ranks, torch.int32, "ranks")):
+            if v is not None and _dev(v, dtype, name).shape != (self.n_slots,):
+                raise ValueError("%s needs one element per adapter" % name)
+        self.A, self.B, self.scale, self.ranks = A, B, scale, ranks
+
+    def plan(self, slot: torch.Tensor) -> AdapterPlan:
+        """slot int32 [M]: the adapter of each token, anything outside 0 .. slots - 1 for none."""
+        return AdapterPlan(slot, self.n_slots)
+
+    def _check_plan(self, plan, M: int):
+        if plan is None or plan.M != M or plan.n_slots != self.n_slots:
+            raise ValueError("need a plan of %d tokens and %d adapters" % (M, self.n_slots))
+
+    def add(self, X: torch.Tensor, Y: torch.Tensor, plan: AdapterPlan, out: torch.Tensor | None = None) -> torch.Tensor:
+        """out = Y + scale B (A x) by each token's adapter; X fp16 [M, K], Y and out fp16 [M, N], rows of which may be apart
+        (a column range of a fused projection).  Without `out` in place."""
+        if out is None:
+            out = Y
+        M = X.shape[0]
+        ldx, ldy, ldo = _rows(X, M, self.K, "X"), _rows(Y, M, self.N, "Y"), _rows(out, M, self.N, "out")
+        self._check_plan(plan, M)
+        scale, ranks = self.scale, self.ranks
+        rc = lib.aser_adapters_add(X.data_ptr(), ldx, self.A.data_ptr(), self.B.data_ptr(),
+                                   None if ranks is None else ranks.data_ptr(), None if scale is None else scale.data_ptr(),
+                                   plan.data.data_ptr(), plan.nbytes, M, self.N, self.K, self.r, self.n_slots, Y.data_ptr(),
+                                   ldy, out.data_ptr(), ldo, _stream())
+        if rc != 0:
+            raise AserError(rc, "aser_adapters_add")
+        return out
+
+    def _forward(self, layer: "AserLinear", X: torch.Tensor, plan: AdapterPlan, lowrank: bool) -> torch.Tensor:
+        M = X.shape[0]
+        if M > layer.max_tokens or (layer.K, layer.N) != (self.K, self.N):
+            raise ValueError("%d tokens of a [%d, %d] layer and adapters of [%d, %d]: they do not fit"
+                             % (M, layer.N, layer.K, self.N, self.K))
+        if _rows(X, M, self.K, "X") != self.K:
+            raise TypeError("X: rows need to be adjacent")
+        self._check_plan(plan, M)
+        r = layer.r if lowrank else 0
+        rc = lib.aser_forward_adapters(X.data_ptr(), _ptr(layer.s), layer.L_A.data_ptr() if r else None, layer.Wk.data_ptr(),
+                                       layer.w_scale.data_ptr(), layer.L_B.data_ptr() if r else None, M, self.N, self.K, r,
+                                       layer.Xq.data_ptr(), layer.a_scale.data_ptr(), layer.T.data_ptr() if r else None,
+                                       layer.Y.data_ptr(), layer.ws.data_ptr(), layer.ws.numel(), self.A.data_ptr(),
+                                       self.B.data_ptr(), _ptr(self.ranks), _ptr(self.scale), plan.data.data_ptr(), plan.nbytes,
+                                       self.r, self.n_slots, _stream())
+        if rc != 0:
+            raise AserError(rc, "aser_forward_adapters")
+        return layer.Y[:M]
 
 
 class AserGatedFFN:

@@ -3,6 +3,7 @@
 #include <stdio.h>
 #include <string.h>
 
+#include "adapters.cuh"
 #include "aser_common.cuh"
 
 namespace aser {
@@ -165,6 +166,31 @@ bool ffn_layout(int M, int K, int F, int N, int r, int r_down, FfnLayout* l) {
     l->H = l->T + round_up(m * 2 * (size_t)(r > r_down ? r : r_down));
     l->total = l->H + round_up(m * 2 * (size_t)F);
     return true;
+}
+
+// The part of an adapter call that does not depend on where its tokens come from.
+constexpr int kMaxSlots = 4096, kMaxAdapterTokens = 1 << 24;
+int adapters_check(const void* X_f16, int ldx, const void* A_f16, const void* B_f16, const int32_t* ranks, const float* scale,
+                   const void* plan, size_t plan_bytes, int M, int N, int K, int r, int n_slots, const void* Y_f16, int ldy,
+                   const void* out_f16, int ldo) {
+    if (!shape_ok(M, N, K, r) || M > kMaxAdapterTokens) return fail(ASER_ERR_SHAPE, "unsupported M, N, K or r");
+    if (n_slots < 1 || n_slots > kMaxSlots) return fail(ASER_ERR_SHAPE, "n_slots must be 1..4096");
+    if (ldx < K || ldy < N || ldo < N || (ldx | ldy | ldo) % 8 != 0)
+        return fail(ASER_ERR_SHAPE, "rows must be multiples of 8 elements apart and at least as far as they are long");
+    if (M == 0 || N == 0) return ASER_OK;
+    ASER_REQUIRE_PTR(plan);
+    ASER_REQUIRE_PTR(Y_f16);
+    ASER_REQUIRE_PTR(out_f16);
+    ASER_OPTIONAL_PTR(ranks);
+    ASER_OPTIONAL_PTR(scale);
+    if (Y_f16 == out_f16 && ldy != ldo) return fail(ASER_ERR_SHAPE, "in place, Y and out are one matrix: ldy and ldo differ");
+    if (r > 0) {
+        ASER_REQUIRE_PTR(X_f16);
+        ASER_REQUIRE_PTR(A_f16);
+        ASER_REQUIRE_PTR(B_f16);
+    }
+    if (plan_bytes < adapters_plan_bytes(M, n_slots)) return fail(ASER_ERR_WORKSPACE, "plan too small for M and n_slots");
+    return ASER_OK;
 }
 
 // Stacked ranks (several layers' down projections in one pass) go up to 512.
@@ -539,6 +565,38 @@ int aser_linear_w4a8_lr_glu(const int8_t* Xq, const float* a_scale, const void* 
                          stream, false, 0, CatSplit(), &glu);
 }
 
+size_t aser_adapters_plan_bytes(int M, int n_slots) {
+    if (M < 0 || M > kMaxAdapterTokens || n_slots < 1 || n_slots > kMaxSlots) return 0;
+    return adapters_plan_bytes(M, n_slots);
+}
+
+int aser_adapters_plan(const int32_t* slot, int M, int n_slots, void* plan, size_t plan_bytes, void* stream) {
+    const size_t need = aser_adapters_plan_bytes(M, n_slots);
+    if (need == 0) return fail(ASER_ERR_SHAPE, "unsupported M or n_slots");
+    if (M == 0) return ASER_OK;
+    ASER_REQUIRE_PTR(slot);
+    ASER_REQUIRE_PTR(plan);
+    if (plan_bytes < need) return fail(ASER_ERR_WORKSPACE, "plan too small for M and n_slots");
+    int rc = check_device();
+    if (rc != ASER_OK) return rc;
+    return launch_adapters_plan(slot, M, n_slots, plan, static_cast<cudaStream_t>(stream));
+}
+
+int aser_adapters_add(const void* X_f16, int ldx, const void* A_f16, const void* B_f16, const int32_t* ranks, const float* scale,
+                      const void* plan, size_t plan_bytes, int M, int N, int K, int r, int n_slots, const void* Y_f16, int ldy,
+                      void* out_f16, int ldo, void* stream) {
+    if (ldx == 0) ldx = K;
+    if (ldy == 0) ldy = N;
+    if (ldo == 0) ldo = N;
+    int rc = adapters_check(X_f16, ldx, A_f16, B_f16, ranks, scale, plan, plan_bytes, M, N, K, r, n_slots, Y_f16, ldy, out_f16, ldo);
+    if (rc != ASER_OK || M == 0 || N == 0) return rc;
+    rc = check_device();
+    if (rc != ASER_OK) return rc;
+    return launch_adapters(static_cast<const __half*>(X_f16), ldx, static_cast<const __half*>(A_f16), static_cast<const __half*>(B_f16),
+                           ranks, scale, plan, M, N, K, r, n_slots, static_cast<const __half*>(Y_f16), ldy,
+                           static_cast<__half*>(out_f16), ldo, static_cast<cudaStream_t>(stream));
+}
+
 size_t aser_forward_ffn_workspace_bytes(int M, int K, int F, int N, int r, int r_down) {
     FfnLayout l;
     return ffn_layout(M, K, F, N, r, r_down, &l) ? l.total : 0;
@@ -841,6 +899,20 @@ int aser_forward(const void* X_f16, const float* s, const void* LA_f16, const vo
     if (rc != ASER_OK) return rc;
     return forward_tokens(X_f16, s, LA_f16, Wk, w_scale, LB_f16, M, M, N, K, r, Xq, a_scale, T_bf16, Y_f16, workspace,
                           workspace_bytes, stream);
+}
+
+int aser_forward_adapters(const void* X_f16, const float* s, const void* LA_f16, const void* Wk, const float* w_scale,
+                          const void* LB_f16, int M, int N, int K, int r, int8_t* Xq, float* a_scale, void* T_bf16, void* Y_f16,
+                          void* workspace, size_t workspace_bytes, const void* A_f16, const void* B_f16, const int32_t* ranks,
+                          const float* scale, const void* plan, size_t plan_bytes, int r_adapter, int n_slots, void* stream) {
+    // the adapters' arguments are checked before the layer is enqueued (M == 0: nothing is)
+    int rc = adapters_check(X_f16, K, A_f16, B_f16, ranks, scale, plan, plan_bytes, M, N, K, r_adapter, n_slots, Y_f16, N, Y_f16, N);
+    if (rc != ASER_OK) return rc;
+    rc = aser_forward(X_f16, s, LA_f16, Wk, w_scale, LB_f16, M, N, K, r, Xq, a_scale, T_bf16, Y_f16, workspace, workspace_bytes, stream);
+    if (rc != ASER_OK || M == 0 || N == 0) return rc;
+    return launch_adapters(static_cast<const __half*>(X_f16), K, static_cast<const __half*>(A_f16), static_cast<const __half*>(B_f16),
+                           ranks, scale, plan, M, N, K, r_adapter, n_slots, static_cast<const __half*>(Y_f16), N,
+                           static_cast<__half*>(Y_f16), N, static_cast<cudaStream_t>(stream));
 }
 
 int aser_forward_host_parts(int M, int N, int K, int* first_token) {

@@ -46,3 +46,39 @@ def test_feed_forward_is_refused(lib):
 def test_a_workspace_serves_fewer_tokens(lib, K, F, N, r, rd):
     need = [lib.aser_forward_ffn_workspace_bytes(m, K, F, N, r, rd) for m in range(1, 2100)]
     assert all(a <= b for a, b in zip(need, need[1:]))
+
+
+def test_adapter_plan_is_refused(lib):
+    assert lib.aser_adapters_plan_bytes(-1, 4) == 0 and lib.aser_adapters_plan_bytes(8, 0) == 0
+    assert lib.aser_adapters_plan_bytes(8, 4097) == 0 and lib.aser_adapters_plan_bytes((1 << 24) + 1, 4) == 0
+    need = lib.aser_adapters_plan_bytes(8, 4)
+    assert need >= 4 * (4 + 8)
+    call = lambda slot=GOOD, M=8, S=4, plan=GOOD, nbytes=need: lib.aser_adapters_plan(slot, M, S, plan, nbytes, None)
+    assert call(M=0, slot=None, plan=None, nbytes=0) == OK
+    assert call(S=0) == SHAPE and call(M=-1) == SHAPE and call(S=5000) == SHAPE
+    assert call(slot=None) == NULL and call(plan=None) == NULL and call(plan=ODD) == ALIGN
+    assert call(nbytes=need - 1) == WORKSPACE
+
+
+def test_adapters_are_refused(lib):
+    def call(M=8, N=64, K=256, r=16, S=4, X=GOOD, A=GOOD, B=GOOD, ranks=None, plan=GOOD, nbytes=1 << 20, Y=GOOD, out=GOOD, ldx=0,
+             ldy=0, ldo=0):
+        return lib.aser_adapters_add(X, ldx, A, B, ranks, None, plan, nbytes, M, N, K, r, S, Y, ldy, out, ldo, None)
+    assert call(M=0, X=None, plan=None, nbytes=0) == OK and call(N=0, Y=None) == OK
+    assert call(K=200) == SHAPE and call(N=60) == SHAPE and call(r=24) == SHAPE and call(r=272) == SHAPE and call(M=-1) == SHAPE
+    assert call(M=(1 << 24) + 1) == SHAPE and call(S=0) == SHAPE and call(S=4097) == SHAPE
+    assert call(ldx=128) == SHAPE and call(ldx=260) == SHAPE and call(ldy=68, ldo=68) == SHAPE and call(ldo=56) == SHAPE
+    assert call(ldy=128) == SHAPE                   # in place, rows of one matrix
+    assert call(X=None) == NULL and call(A=None) == NULL and call(B=None) == NULL and call(plan=None) == NULL
+    assert call(Y=None) == NULL and call(out=None) == NULL and call(ranks=ODD) == ALIGN and call(out=ODD) == ALIGN
+    assert call(nbytes=lib.aser_adapters_plan_bytes(8, 4) - 1) == WORKSPACE
+
+
+def test_projection_with_adapters_is_refused(lib):
+    def call(M=8, N=64, K=256, r=16, ra=16, X=GOOD, LA=GOOD, Y=GOOD, ws=GOOD, A=GOOD, plan=GOOD, nbytes=1 << 20):
+        return lib.aser_forward_adapters(X, None, LA, GOOD, GOOD, GOOD, M, N, K, r, GOOD, GOOD, GOOD, Y, ws, 1 << 26, A, GOOD, None,
+                                         None, plan, nbytes, ra, 4, None)
+    assert call(M=0, X=None, ws=None) == OK
+    assert call(K=100) == SHAPE and call(ra=8) == SHAPE and call(r=8) == SHAPE and call(N=12) == SHAPE
+    assert call(X=None) == NULL and call(LA=None) == NULL and call(A=None) == NULL and call(plan=None) == NULL
+    assert call(ws=None) == WORKSPACE and call(nbytes=8) == WORKSPACE
