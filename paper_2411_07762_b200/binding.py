@@ -17,7 +17,7 @@ EXPORTED_SYMBOLS = (
     "aser_forward_shared_workspace_bytes", "aser_construct", "aser_construct_workspace_bytes", "aser_linear_w4a8_lr", "aser_linear_w4a8", "aser_linear_w4a8_lr_simt", "aser_linear_w4a8_lr_static",
     "aser_workspace_bytes", "aser_workspace_init", "aser_check_status", "aser_forward",
     "aser_forward_host", "aser_linear_w4a8_lr_glu", "aser_forward_ffn_workspace_bytes", "aser_forward_ffn",
-    "aser_adapters_plan_bytes", "aser_adapters_plan", "aser_adapters_add", "aser_forward_adapters",
+    "aser_adapters_plan_bytes", "aser_adapters_plan", "aser_adapters_add", "aser_adapters_workspace_bytes", "aser_forward_adapters",
     "aser_last_error", "aser_version",
 )
 
@@ -71,9 +71,11 @@ lib.aser_forward_ffn.argtypes = [_P] * 11 + [_I] * 7 + [_P, _P, _Z, _P]
 lib.aser_adapters_plan_bytes.argtypes = [_I, _I]
 lib.aser_adapters_plan_bytes.restype = _Z
 lib.aser_adapters_plan.argtypes = [_P, _I, _I, _P, _Z, _P]
-lib.aser_adapters_add.argtypes = [_P, _I, _P, _P, _P, _P, _P, _Z, _I, _I, _I, _I, _I, _P, _I, _P, _I, _P]
+lib.aser_adapters_workspace_bytes.argtypes = [_I, _I, _I]
+lib.aser_adapters_workspace_bytes.restype = _Z
+lib.aser_adapters_add.argtypes = [_P, _I, _P, _P, _P, _P, _P, _Z, _I, _I, _I, _I, _I, _P, _I, _P, _I, _P, _Z, _P]
 lib.aser_forward_adapters.argtypes = [_P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _P, _P, _P, _P, _P, _Z,
-                                      _P, _P, _P, _P, _P, _Z, _I, _I, _P]
+                                      _P, _P, _P, _P, _P, _Z, _I, _I, _P, _Z, _P]
 lib.aser_construct_workspace_bytes.argtypes = [_I, _I, _I, _I, _I]
 lib.aser_construct_workspace_bytes.restype = _Z
 lib.aser_construct.argtypes = [_P, _P, _P, _I, _I, _I, _I, C.c_double, _I, _P, _P, _P, _P, _P, _P, _P, _I, _P, _Z, _P]
@@ -610,6 +612,11 @@ class AserAdapters:
         if plan is None or plan.M != M or plan.n_slots != self.n_slots:
             raise ValueError("need a plan of %d tokens and %d adapters" % (M, self.n_slots))
 
+    def _workspace(self, M: int):
+        """What a call of many tokens keeps between its two launches: torch's memory of the current stream."""
+        nbytes = lib.aser_adapters_workspace_bytes(M, self.r, self.n_slots)
+        return None if nbytes == 0 else torch.empty((nbytes,), dtype=torch.uint8, device=self.A.device)
+
     def add(self, X: torch.Tensor, Y: torch.Tensor, plan: AdapterPlan, out: torch.Tensor | None = None) -> torch.Tensor:
         """out = Y + scale B (A x) by each token's adapter; X fp16 [M, K], Y and out fp16 [M, N], rows of which may be apart
         (a column range of a fused projection).  Without `out` in place."""
@@ -618,11 +625,12 @@ class AserAdapters:
         M = X.shape[0]
         ldx, ldy, ldo = _rows(X, M, self.K, "X"), _rows(Y, M, self.N, "Y"), _rows(out, M, self.N, "out")
         self._check_plan(plan, M)
-        scale, ranks = self.scale, self.ranks
+        scale, ranks, ws = self.scale, self.ranks, self._workspace(M)
         rc = lib.aser_adapters_add(X.data_ptr(), ldx, self.A.data_ptr(), self.B.data_ptr(),
                                    None if ranks is None else ranks.data_ptr(), None if scale is None else scale.data_ptr(),
                                    plan.data.data_ptr(), plan.nbytes, M, self.N, self.K, self.r, self.n_slots, Y.data_ptr(),
-                                   ldy, out.data_ptr(), ldo, _stream())
+                                   ldy, out.data_ptr(), ldo, None if ws is None else ws.data_ptr(),
+                                   0 if ws is None else ws.numel(), _stream())
         if rc != 0:
             raise AserError(rc, "aser_adapters_add")
         return out
@@ -636,12 +644,13 @@ class AserAdapters:
             raise TypeError("X: rows need to be adjacent")
         self._check_plan(plan, M)
         r = layer.r if lowrank else 0
+        ws = self._workspace(M)
         rc = lib.aser_forward_adapters(X.data_ptr(), _ptr(layer.s), layer.L_A.data_ptr() if r else None, layer.Wk.data_ptr(),
                                        layer.w_scale.data_ptr(), layer.L_B.data_ptr() if r else None, M, self.N, self.K, r,
                                        layer.Xq.data_ptr(), layer.a_scale.data_ptr(), layer.T.data_ptr() if r else None,
                                        layer.Y.data_ptr(), layer.ws.data_ptr(), layer.ws.numel(), self.A.data_ptr(),
                                        self.B.data_ptr(), _ptr(self.ranks), _ptr(self.scale), plan.data.data_ptr(), plan.nbytes,
-                                       self.r, self.n_slots, _stream())
+                                       self.r, self.n_slots, _ptr(ws), 0 if ws is None else ws.numel(), _stream())
         if rc != 0:
             raise AserError(rc, "aser_forward_adapters")
         return layer.Y[:M]

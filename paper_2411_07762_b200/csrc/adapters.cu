@@ -3,17 +3,18 @@
 //
 // Two products with a small intermediate, S = A_a x (r numbers per token) and B_a S.  The bytes are those of the adapters in
 // use (2 r (K + N) each), X, and Y twice; a token's 2 r (K + N) multiply-adds come to at most r of them per byte of X and Y, so
-// at the ranks of adapters the tensor cores' older instruction (mma.sync m16n8k16) keeps up with HBM and its operands can
-// go straight from global memory into registers.  What is left to arrange:
+// at the ranks of adapters mma.sync (m16n8k16) keeps up with HBM and takes tokens from anywhere in a batch.  Arranged are:
 //  * tokens of one adapter have to meet, wherever they stand in the batch: a plan (adapters_plan_kernel), made once per batch
-//    and used by all layers of a step, lists the tokens by adapter and cuts each adapter's into tiles;
-//  * one launch: a tile belongs to a cluster of CTAs, which split K for the first product and N for the second.  The partial
-//    sums of S meet in distributed shared memory (in a fixed order; nothing depends on the order of tokens in a tile);
-//  * an inner product does not care about the order of k, so a thread's k positions are the 8 columns of one 16-byte load, the
-//    same for both operands; likewise the 32 rows of B that a warp takes are dealt so that a thread's outputs are 8 neighbours.
-// S is summed and exchanged in fp32.  For the second product it is rounded to fp16 (2^-11 of each number, where the output
-// has 2^-11 of the whole sum) after a scaling by a power of two that brings the token's largest entry to [2^14, 2^15): exact,
-// and no size of activations or adapters overflows.
+//    and used by all layers of a step, lists the tokens by adapter and cuts each adapter's into tiles of 16 and of 128;
+//  * few tokens per adapter (this file): one launch, a cluster of eight CTAs per tile of 16, which split K for the first
+//    product and N for the second.  What bounds it is the chain of loads, so operands go from global memory straight into
+//    registers (the first rows of B to shared memory, ahead of the first product): an inner product does not care about the order of k, so a thread's k positions are the 8 columns of one
+//    16-byte load, the same for both operands; likewise the 32 rows of B that a warp takes are dealt so that a thread's outputs
+//    are 8 neighbours.  Up to 64 ranks each CTA sends its sums to the others, so that one barrier is all that S waits for;
+//  * many tokens per adapter: two launches (adapters_many.cu).
+// S is summed and exchanged in fp32, in a fixed order; nothing depends on the order of tokens in a tile.  For the second product it
+// is rounded to fp16 (2^-11 of each number, where the output has 2^-11 of the whole sum) after a scaling by a power of two that
+// brings the token's largest entry to [2^14, 2^15): exact, and no size of activations or adapters overflows.
 #include "adapters.cuh"
 #include "sm100_ptx.cuh"
 
@@ -21,271 +22,254 @@ namespace aser {
 
 namespace {
 
-constexpr int kAThreads = 256, kAWarps = kAThreads / 32;
+constexpr int kThreads = 256, kWarps = kThreads / 32, kCL = 8, kTok = kTileFew;
 constexpr int kChunk = 64;                  // ranks of S summed at a time
 constexpr int kRedStride = kChunk + 8;      // floats: rows 8 banks apart
+constexpr int kSumBytes = kCL * kTok * kChunk * 4;      // (more than 16 x 256 sums)
 constexpr int kPlanThreads = 1024;
 
 // Bytes between the fp16 rows of S: an odd multiple of 64, so that 16-byte reads of two rows do not meet in a bank.
 __host__ __device__ constexpr int s_stride(int r) { return (2 * r + 63) / 128 * 128 + 64; }
 
-struct AdapterParams {
-    const __half* X;
-    const __half* A;          // [slots, r, K]
-    const __half* B;          // [slots, N, r]
-    const int32_t* ranks;     // [slots] or NULL
-    const float* scale;       // [slots] or NULL
-    const int32_t* plan;
-    const __half* Y;
-    __half* out;
-    size_t ldx, ldy, ldo;
-    int M, N, K, r, n_slots;
-    int parts;                // clusters per tile, each with its own part of N
-};
-
-__device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
-__device__ __forceinline__ void st_cluster_u2(uint32_t addr, uint32_t a, uint32_t b) {
-    asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(a), "r"(b) : "memory");
-}
-__device__ __forceinline__ void st_cluster_f32(uint32_t addr, float v) {
-    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
+__device__ __forceinline__ void st_cluster_f32x4(uint32_t addr, const float4& v) {
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
 }
 
-// A tile of up to 16 MT TW tokens of one adapter: TW groups of warps along the tokens, KW = 8 / TW along K and along N.
-template <int MT, int TW>
-__global__ void __launch_bounds__(kAThreads, 2)
-adapters_kernel(const AdapterParams p) {
-    constexpr int TM = 16 * MT * TW, KW = kAWarps / TW;
+// acc += X A^T over the 32-column units u0, u0 + step, ... of K, BATCH of them in flight; NT tiles of 8 ranks, of which n_tiles are there.
+template <int BATCH, int NT>
+__device__ __forceinline__ void down_units(float (&acc)[8][4], const __half* (&xp)[2], const bool (&ok)[2], const __half* ap, size_t K,
+                                           int n_tiles, int u0, int units, int step) {
+    for (; u0 < units; u0 += BATCH * step) {
+        uint4 x[BATCH][2], l[BATCH][NT];
+#pragma unroll
+        for (int b = 0; b < BATCH; ++b) {
+            const int u = u0 + b * step;
+            const bool in = BATCH == 1 || u < units;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) x[b][i] = in && ok[i] ? *reinterpret_cast<const uint4*>(xp[i] + u * 32) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+                l[b][nt] = in && nt < n_tiles ? __ldg(reinterpret_cast<const uint4*>(ap + nt * 8 * K + u * 32)) : make_uint4(0, 0, 0, 0);
+        }
+#pragma unroll
+        for (int b = 0; b < BATCH; ++b)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                if (nt >= n_tiles) break;
+                mma16816(acc[nt], x[b][0].x, x[b][1].x, x[b][0].y, x[b][1].y, l[b][nt].x, l[b][nt].y);
+                mma16816(acc[nt], x[b][0].z, x[b][1].z, x[b][0].w, x[b][1].w, l[b][nt].z, l[b][nt].w);
+            }
+    }
+}
+
+__global__ void __launch_bounds__(kThreads, 2)
+adapters_few_kernel(const AdapterParams p) {
     grid_dep_wait();
     grid_dep_launch();
-    extern __shared__ __align__(16) uint8_t smem[];
-    const uint32_t CL = cluster_size(), rank = cluster_rank();
-    const int tile = (int)(blockIdx.x / (CL * p.parts)), part = (int)(blockIdx.x / CL % p.parts);
-    const PlanView plan = plan_view(p.plan, p.M, p.n_slots);
-    const int4 head = *reinterpret_cast<const int4*>(p.plan);
-    if (head.x != p.M || head.y != p.n_slots || tile >= (TM == 16 ? head.z : head.w)) return;
-    const int4 t4 = (TM == 16 ? plan.tiles_few : plan.tiles_many)[tile];
-    const int slot = t4.x, count = t4.z;
-    const int32_t* tokens = plan.tokens + t4.y;
+    extern __shared__ __align__(128) uint8_t smem[];
+    const int rank = (int)cluster_rank(), cluster = (int)(blockIdx.x / kCL), tile = cluster / p.parts, part = cluster - tile * p.parts;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int tw = warp % TW, kw = warp / TW;
-    int rk = 0;
-    if (slot >= 0) {
-        rk = p.ranks ? __ldg(p.ranks + slot) : p.r;
-        rk = (rk < 0 ? 0 : rk > p.r ? p.r : rk) & ~15;
-    }
-    const int n_units = (p.N + 31) / 32, n_step = p.parts * (int)CL * KW, n_first = (part * (int)CL + (int)rank) * KW + kw;
-    size_t tok[2 * MT];
-    bool ok[2 * MT];
+    const PlanView plan = plan_view(p.plan, p.M, p.n_slots);
+    const int32_t* record = plan.tiles_few + (size_t)tile * kFewWords;
+    const int4 head = *reinterpret_cast<const int4*>(p.plan), t4 = *reinterpret_cast<const int4*>(record);
+    const int tok0 = record[4 + g], tok1 = record[12 + g];
+    if (head.x != p.M || head.y != p.n_slots || tile >= head.z) return;      // (the whole cluster, here and below)
+    const int slot = t4.x, count = t4.z;
+    const int rk = slot < 0 ? 0 : adapter_rank(p, slot);
+    if (rk == 0 && p.Y == p.out) return;
+    const int n_units = (p.N + 31) / 32, n_step = p.parts * kCL * kWarps, n_first = (part * kCL + rank) * kWarps + warp;
+    const bool ok[2] = {g < count, 8 + g < count};
+    const size_t tok[2] = {ok[0] ? (size_t)tok0 : 0, ok[1] ? (size_t)tok1 : 0};
+    auto load_y = [&](int u, uint4 (&y)[2]) {
+        const int n = u * 32 + 8 * t;
 #pragma unroll
-    for (int i = 0; i < 2 * MT; ++i) {
-        const int row = tw * 16 * MT + 8 * i + g;
-        ok[i] = row < count;
-        tok[i] = ok[i] ? (size_t)tokens[row] : 0;
-    }
-    if (rk == 0) {              // nothing to add (the whole cluster takes this way)
-        if (p.Y != p.out)
-            for (int u = n_first; u < n_units; u += n_step)
+        for (int i = 0; i < 2; ++i)
+            y[i] = ok[i] && n < p.N ? *reinterpret_cast<const uint4*>(p.Y + tok[i] * p.ldy + n) : make_uint4(0, 0, 0, 0);
+    };
+    uint4 y[2];
+    if (n_first < n_units) load_y(n_first, y);
+    if (rk == 0) {              // nothing to add
+        for (int u = n_first; u < n_units; u += n_step) {
+            if (u != n_first) load_y(u, y);
 #pragma unroll
-                for (int i = 0; i < 2 * MT; ++i) {
-                    const int n = u * 32 + 8 * t;
-                    if (ok[i] && n < p.N)
-                        *reinterpret_cast<uint4*>(p.out + tok[i] * p.ldo + n) = *reinterpret_cast<const uint4*>(p.Y + tok[i] * p.ldy + n);
-                }
+            for (int i = 0; i < 2; ++i)
+                if (ok[i] && u * 32 + 8 * t < p.N) *reinterpret_cast<uint4*>(p.out + tok[i] * p.ldo + u * 32 + 8 * t) = y[i];
+        }
         return;
     }
-    float* red = reinterpret_cast<float*>(smem);                             // [KW][TM][kRedStride]
-    float* sums = red + KW * TM * kRedStride;                                // [TM][r]
-    uint8_t* s16 = reinterpret_cast<uint8_t*>(sums + TM * p.r);              // [TM][s_stride(r)]
-    float* row_scale = reinterpret_cast<float*>(s16 + TM * s_stride(p.r));   // [TM]
+    cluster_arrive();           // (waited for before anything is sent: every CTA of the cluster runs by then)
+    float* red = reinterpret_cast<float*>(smem);                             // [warp][16][kRedStride]
+    float* sums = red + kWarps * kTok * kRedStride;                          // up to 64 ranks: [CTA][16][64], received; else [16][r]
+    uint8_t* s16 = reinterpret_cast<uint8_t*>(sums) + kSumBytes;             // [16][s_stride(r)]
+    float* row_scale = reinterpret_cast<float*>(s16 + kTok * s_stride(p.r)); // [16]
+    uint8_t* b_rows = reinterpret_cast<uint8_t*>(row_scale + kTok) + warp * (32 * 128);
+    const __half* B = p.B + (size_t)slot * p.N * p.r;
+    {   // the first 64 ranks of the warp's first rows of B: there when S is
+        const int chunks = (rk < kChunk ? rk : kChunk) / 8, shift = chunks <= 2 ? 1 : chunks <= 4 ? 2 : 3, c = lane & ((1 << shift) - 1);
+        for (int row = lane >> shift; row < 32; row += 32 >> shift) {
+            const int n = n_first * 32 + row;
+            if (c < chunks && n < p.N) cp_async16(smem_u32(b_rows) + row * 128 + ((c ^ ((row & 1) << 2)) << 4), B + (size_t)n * p.r + c * 8);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
 
     // ---- S = A x: this CTA's part of K, the warps' parts of it ----
     const __half* A = p.A + (size_t)slot * p.r * p.K + 8 * t;
-    const __half* xp[2 * MT];
-#pragma unroll
-    for (int i = 0; i < 2 * MT; ++i) xp[i] = p.X + tok[i] * p.ldx + 8 * t;
+    const __half* xp[2] = {p.X + tok[0] * p.ldx + 8 * t, p.X + tok[1] * p.ldx + 8 * t};
+    const bool narrow = rk <= kChunk;
     for (int r0 = 0; r0 < rk; r0 += kChunk) {
-        float acc[MT][8][4];
+        float acc[8][4];
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int nt = 0; nt < 8; ++nt)
 #pragma unroll
-            for (int nt = 0; nt < 8; ++nt)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[mt][nt][e] = 0.f;
+            for (int e = 0; e < 4; ++e) acc[nt][e] = 0.f;
         const __half* ap = A + (size_t)(r0 + g) * p.K;
-        const int n_tiles = (rk - r0) / 8;
-        for (int u = (int)rank * KW + kw; u < p.K / 32; u += (int)CL * KW) {
-            uint4 x[2 * MT], l[8];
-#pragma unroll
-            for (int i = 0; i < 2 * MT; ++i) x[i] = ok[i] ? *reinterpret_cast<const uint4*>(xp[i] + u * 32) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-            for (int nt = 0; nt < 8; ++nt)
-                if (nt < n_tiles) l[nt] = __ldg(reinterpret_cast<const uint4*>(ap + (size_t)nt * 8 * p.K + u * 32));
-#pragma unroll
-            for (int nt = 0; nt < 8; ++nt) {
-                if (nt >= n_tiles) break;
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    mma16816(acc[mt][nt], x[2 * mt].x, x[2 * mt + 1].x, x[2 * mt].y, x[2 * mt + 1].y, l[nt].x, l[nt].y);
-                    mma16816(acc[mt][nt], x[2 * mt].z, x[2 * mt + 1].z, x[2 * mt].w, x[2 * mt + 1].w, l[nt].z, l[nt].w);
-                }
-            }
-        }
+        const int n_tiles = (rk - r0) / 8, u0 = rank * kWarps + warp;
+        if (n_tiles <= 4) down_units<2, 4>(acc, xp, ok, ap, p.K, n_tiles, u0, p.K / 32, kCL * kWarps);
+        else down_units<1, 8>(acc, xp, ok, ap, p.K, n_tiles, u0, p.K / 32, kCL * kWarps);
         if (r0 > 0) __syncthreads();            // the chunk before has been summed
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int nt = 0; nt < 8; ++nt)
 #pragma unroll
-            for (int nt = 0; nt < 8; ++nt)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    float* q = red + (size_t)(kw * TM + (tw * MT + mt) * 16 + 8 * h + g) * kRedStride + nt * 8 + 2 * t;
-                    if (nt < n_tiles) *reinterpret_cast<float2*>(q) = make_float2(acc[mt][nt][2 * h], acc[mt][nt][2 * h + 1]);
-                }
+            for (int h = 0; h < 2; ++h)
+                if (nt < n_tiles && ok[h])
+                    *reinterpret_cast<float2*>(red + (warp * kTok + 8 * h + g) * kRedStride + nt * 8 + 2 * t) = make_float2(acc[nt][2 * h], acc[nt][2 * h + 1]);
         __syncthreads();
+        if (narrow) cluster_wait();
         const int per_row = (n_tiles < 8 ? n_tiles : 8) * 2;        // groups of four sums
-        for (int i = threadIdx.x; i < count * per_row; i += kAThreads) {
+        for (int i = threadIdx.x; i < count * per_row; i += kThreads) {
             const int row = i / per_row, j = i % per_row * 4;
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-            for (int w = 0; w < KW; ++w) {
-                const float4 a = *reinterpret_cast<const float4*>(red + (size_t)(w * TM + row) * kRedStride + j);
+            for (int w = 0; w < kWarps; ++w) {
+                const float4 a = *reinterpret_cast<const float4*>(red + (w * kTok + row) * kRedStride + j);
                 v.x += a.x; v.y += a.y; v.z += a.z; v.w += a.w;
             }
-            *reinterpret_cast<float4*>(sums + row * p.r + r0 + j) = v;
+            if (!narrow) {
+                *reinterpret_cast<float4*>(sums + row * p.r + r0 + j) = v;
+                continue;
+            }
+            const uint32_t at = smem_u32(sums + (rank * kTok + row) * kChunk + j);
+#pragma unroll
+            for (int q = 0; q < kCL; ++q) st_cluster_f32x4(map_to_rank(at, q), v);
         }
     }
-
-    // the first rows of B are fetched while the cluster meets
-    const __half* B = p.B + (size_t)slot * p.N * p.r;
-    uint4 b[4][2];
-    auto fetch = [&](int u, int r0) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int n = u * 32 + (g >> 1) * 8 + 2 * j + (g & 1);
-            const __half* row = B + (size_t)n * p.r + r0;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                b[j][h] = make_uint4(0, 0, 0, 0);
-                if (n >= p.N) continue;
-                if (r0 + 32 * h + 32 <= rk) b[j][h] = __ldg(reinterpret_cast<const uint4*>(row + 32 * h + 8 * t));
-                else if (r0 + 32 * h < rk) {            // the last 16 ranks
-                    const uint2 v = __ldg(reinterpret_cast<const uint2*>(row + 32 * h + 4 * t));
-                    b[j][h].x = v.x; b[j][h].y = v.y;
-                }
-            }
-        }
-    };
-    if (n_first < n_units) fetch(n_first, 0);
-
-    // ---- every CTA sums some tokens over the cluster, rounds them, and sends them to all ----
+    if (!narrow) cluster_wait();
     cluster_arrive();
     cluster_wait();
-    {
-        const int per = (TM + (int)CL - 1) / (int)CL;
-        for (int i = warp; i < per; i += kAWarps) {
-            const int row = (int)rank * per + i;
-            if (row >= count) continue;
+
+    // ---- every CTA has the sums of all eight, adds and rounds them ----
+    const float alpha = p.scale ? __ldg(p.scale + slot) : 1.f;
+    if (narrow) {                           // two rows side by side
+        const int row = warp * 2 + (lane >> 4), j = (lane & 15) * 4;
+        const bool mine = row < count && j < rk;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (mine)
+#pragma unroll
+            for (int q = 0; q < kCL; ++q) {
+                const float4 a = *reinterpret_cast<const float4*>(sums + (q * kTok + row) * kChunk + j);
+                v.x += a.x; v.y += a.y; v.z += a.z; v.w += a.w;
+            }
+        float top = max4_abs(v);
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const RowFactor f = row_factor(top);
+        if (mine) *reinterpret_cast<uint2*>(s16 + row * s_stride(p.r) + 2 * j) = scaled_f16(v, f.up);
+        if (mine && j == 0) row_scale[row] = f.down * alpha;
+    } else {
+        for (int row = warp; row < count; row += kWarps) {
             float4 v[2];
             float top = 0.f;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int j = h * 128 + lane * 4;
                 v[h] = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (j >= rk) continue;
-                const uint32_t at = smem_u32(sums + row * p.r + j);
-                for (uint32_t q = 0; q < CL; ++q) {
-                    const float4 a = ld_cluster_f32x4(map_to_rank(at, q));
-                    v[h].x += a.x; v[h].y += a.y; v[h].z += a.z; v[h].w += a.w;
-                }
-                top = fmaxf(top, fmaxf(fmaxf(fabsf(v[h].x), fabsf(v[h].y)), fmaxf(fabsf(v[h].z), fabsf(v[h].w))));
-            }
-            top = warp_max(top);
-            // 2^(14 - e) for top in [2^e, 2^(e+1)); an infinite or tiny top keeps a factor that is a normal number
-            int e = (int)(__float_as_uint(top) >> 23) - 127;
-            e = e < -100 ? -100 : e > 127 ? 127 : e;
-            const float up = __uint_as_float((uint32_t)(127 + 14 - e) << 23), down = __uint_as_float((uint32_t)(127 - 14 + e) << 23);
+                if (j < rk) {
+                    const uint32_t at = smem_u32(sums + row * p.r + j);
+                    float4 a[kCL];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int j = h * 128 + lane * 4;
-                if (j >= rk) continue;
-                const __half2 lo = __floats2half2_rn(v[h].x * up, v[h].y * up), hi = __floats2half2_rn(v[h].z * up, v[h].w * up);
-                const uint32_t at = smem_u32(s16 + row * s_stride(p.r) + 2 * j);
-                for (uint32_t q = 0; q < CL; ++q)
-                    st_cluster_u2(map_to_rank(at, q), *reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+                    for (int q = 0; q < kCL; ++q) a[q] = ld_cluster_f32x4(map_to_rank(at, q));
+#pragma unroll
+                    for (int q = 0; q < kCL; ++q) { v[h].x += a[q].x; v[h].y += a[q].y; v[h].z += a[q].z; v[h].w += a[q].w; }
+                }
+                top = fmaxf(top, max4_abs(v[h]));
             }
-            if (lane < (int)CL)
-                st_cluster_f32(map_to_rank(smem_u32(row_scale + row), lane), down * (p.scale ? __ldg(p.scale + slot) : 1.f));
+            const RowFactor f = row_factor(warp_max(top));
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (h * 128 + lane * 4 < rk) *reinterpret_cast<uint2*>(s16 + row * s_stride(p.r) + 2 * (h * 128 + lane * 4)) = scaled_f16(v[h], f.up);
+            if (lane == 0) row_scale[row] = f.down * alpha;
         }
     }
-    cluster_arrive();
-    cluster_wait();
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncthreads();
+    if (!narrow) cluster_arrive();          // (waited for at the end: nobody leaves while a peer may still read its sums)
 
     // ---- B S: this CTA's part of N ----
-    float factor[2 * MT];
+    float factor[2];
 #pragma unroll
-    for (int i = 0; i < 2 * MT; ++i) factor[i] = ok[i] ? row_scale[tw * 16 * MT + 8 * i + g] : 0.f;
-    const uint8_t* s_row = s16 + (size_t)(tw * 16 * MT + g) * s_stride(p.r);
+    for (int i = 0; i < 2; ++i) factor[i] = ok[i] ? row_scale[8 * i + g] : 0.f;
+    const uint8_t* s_row = s16 + g * s_stride(p.r);
     for (int u = n_first; u < n_units; u += n_step) {
         const int n = u * 32 + 8 * t;
-        uint4 y[2 * MT];
+        float acc[4][4];
 #pragma unroll
-        for (int i = 0; i < 2 * MT; ++i)
-            y[i] = ok[i] && n < p.N ? *reinterpret_cast<const uint4*>(p.Y + tok[i] * p.ldy + n) : make_uint4(0, 0, 0, 0);
-        float acc[MT][4][4];
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[mt][j][e] = 0.f;
+            for (int e = 0; e < 4; ++e) acc[j][e] = 0.f;
         for (int r0 = 0; r0 < rk; r0 += kChunk) {
-            if (u != n_first || r0 > 0) fetch(u, r0);
+            // rows (g / 2) 8 + 2 j + g % 2 of the unit, 8 ranks of each 32 a thread (4 of the last 16)
+            uint4 b[4][2];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int at = (g >> 1) * 8 + 2 * j + (g & 1), row_n = u * 32 + at;
+                const __half* row = B + (size_t)row_n * p.r + r0;
+                const uint8_t* kept = b_rows + at * 128;
+                const int swap = (at & 1) << 6;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int left = rk - r0 - 32 * h;
+                    b[j][h] = make_uint4(0, 0, 0, 0);
+                    if (left <= 0 || row_n >= p.N) continue;
+                    if (u == n_first && r0 == 0) {
+                        if (left >= 32) b[j][h] = *reinterpret_cast<const uint4*>(kept + ((64 * h + 16 * t) ^ swap));
+                        else { const uint2 v = *reinterpret_cast<const uint2*>(kept + ((64 * h + 8 * t) ^ swap)); b[j][h].x = v.x; b[j][h].y = v.y; }
+                    } else if (left >= 32) b[j][h] = __ldg(reinterpret_cast<const uint4*>(row + 32 * h + 8 * t));
+                    else { const uint2 v = __ldg(reinterpret_cast<const uint2*>(row + 32 * h + 4 * t)); b[j][h].x = v.x; b[j][h].y = v.y; }
+                }
+            }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int k0 = r0 + 32 * h;
                 if (k0 >= rk) continue;
                 const bool whole = k0 + 32 <= rk;
+                const uint8_t* q = s_row + 2 * k0;
+                uint4 a, c;
+                if (whole) {
+                    a = *reinterpret_cast<const uint4*>(q + 16 * t);
+                    c = *reinterpret_cast<const uint4*>(q + 8 * s_stride(p.r) + 16 * t);
+                } else {
+                    const uint2 a2 = *reinterpret_cast<const uint2*>(q + 8 * t), c2 = *reinterpret_cast<const uint2*>(q + 8 * s_stride(p.r) + 8 * t);
+                    a = make_uint4(a2.x, a2.y, 0, 0);
+                    c = make_uint4(c2.x, c2.y, 0, 0);
+                }
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    const uint8_t* q = s_row + (size_t)mt * 16 * s_stride(p.r) + 2 * k0;
-                    uint4 a, c;
-                    if (whole) {
-                        a = *reinterpret_cast<const uint4*>(q + 16 * t);
-                        c = *reinterpret_cast<const uint4*>(q + 8 * s_stride(p.r) + 16 * t);
-                    } else {
-                        const uint2 a2 = *reinterpret_cast<const uint2*>(q + 8 * t), c2 = *reinterpret_cast<const uint2*>(q + 8 * s_stride(p.r) + 8 * t);
-                        a = make_uint4(a2.x, a2.y, 0, 0);
-                        c = make_uint4(c2.x, c2.y, 0, 0);
-                    }
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        mma16816(acc[mt][j], a.x, c.x, a.y, c.y, b[j][h].x, b[j][h].y);
-                        if (whole) mma16816(acc[mt][j], a.z, c.z, a.w, c.w, b[j][h].z, b[j][h].w);
-                    }
+                for (int j = 0; j < 4; ++j) {
+                    mma16816(acc[j], a.x, c.x, a.y, c.y, b[j][h].x, b[j][h].y);
+                    if (whole) mma16816(acc[j], a.z, c.z, a.w, c.w, b[j][h].z, b[j][h].w);
                 }
             }
         }
-        if (n >= p.N) continue;
+        const uint4 mine[2] = {y[0], y[1]};
+        if (u + n_step < n_units) load_y(u + n_step, y);
 #pragma unroll
-        for (int i = 0; i < 2 * MT; ++i) {
-            if (!ok[i]) continue;
-            const uint32_t yw[4] = {y[i].x, y[i].y, y[i].z, y[i].w};
-            uint32_t o[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&yw[j]));
-                const __half2 v = __floats2half2_rn(fmaf(acc[i >> 1][j][2 * (i & 1)], factor[i], f.x),
-                                                    fmaf(acc[i >> 1][j][2 * (i & 1) + 1], factor[i], f.y));
-                o[j] = *reinterpret_cast<const uint32_t*>(&v);
-            }
-            *reinterpret_cast<uint4*>(p.out + tok[i] * p.ldo + n) = make_uint4(o[0], o[1], o[2], o[3]);
-        }
+        for (int i = 0; i < 2; ++i)
+            if (ok[i] && n < p.N) *reinterpret_cast<uint4*>(p.out + tok[i] * p.ldo + n) = add_scaled(mine[i], acc, i, factor[i]);
     }
+    if (!narrow) cluster_wait();
 }
 
 // Tokens by adapter (in their order within an adapter), then the tokens without one; every group cut into tiles.  One CTA.
@@ -322,11 +306,14 @@ adapters_plan_kernel(const int32_t* __restrict__ slot, int M, int n_slots, int32
     __syncthreads();
     at.x -= mine.x; at.y -= mine.y; at.z -= mine.z;
     for (int w = 0; w < warp; ++w) { at.x += warp_sum[w].x; at.y += warp_sum[w].y; at.z += warp_sum[w].z; }
-    if (tid == kPlanThreads - 1)
-        *reinterpret_cast<int4*>(out) = make_int4(M, n_slots, at.y + mine.y, at.z + mine.z);
+    __shared__ int few;
+    if (tid == kPlanThreads - 1) {
+        few = at.y + mine.y;
+        *reinterpret_cast<int4*>(out) = make_int4(M, n_slots, few, at.z + mine.z);
+    }
     for (int i = g0; i < g1; ++i) {
         const int n = cursor[i], s = i < n_slots ? i : -1;
-        for (int k = 0; k < n; k += kTileFew) plan.tiles_few[at.y++] = make_int4(s, at.x + k, min(kTileFew, n - k), 0);
+        for (int k = 0; k < n; k += kTileFew) *reinterpret_cast<int4*>(plan.tiles_few + (size_t)kFewWords * at.y++) = make_int4(s, at.x + k, min(kTileFew, n - k), 0);
         for (int k = 0; k < n; k += kTileMany) plan.tiles_many[at.z++] = make_int4(s, at.x + k, min(kTileMany, n - k), 0);
         cursor[i] = at.x;
         at.x += n;
@@ -350,47 +337,51 @@ adapters_plan_kernel(const int32_t* __restrict__ slot, int M, int n_slots, int32
             __syncthreads();
         }
     }
+    // the tiles of 16 carry their tokens' numbers
+    for (int i = tid; i < few * kTileFew; i += kPlanThreads) {
+        int32_t* record = plan.tiles_few + (size_t)kFewWords * (i / kTileFew);
+        const int e = i % kTileFew;
+        record[4 + e] = e < record[2] ? plan.tokens[record[1] + e] : 0;
+    }
 }
 
-template <int MT, int TW>
-size_t smem_bytes(int r) {
-    constexpr int TM = 16 * MT * TW, KW = kAWarps / TW;
-    return (size_t)KW * TM * kRedStride * 4 + (size_t)TM * r * 4 + (size_t)TM * s_stride(r) + TM * 4;
-}
+int few_smem(int r) { return kWarps * kTok * kRedStride * 4 + kSumBytes + kTok * s_stride(r) + kTok * 4 + kWarps * 32 * 128; }
 
-template <int MT, int TW>
-int launch_tiles(AdapterParams p, int tiles, int CL, cudaStream_t st) {
+int launch_few(AdapterParams p, cudaStream_t st) {
     static bool configured[kMaxDevices] = {false};
-    int dev = 0;
-    const int rc = current_device(&dev);
+    int dev = 0, num_sms = 0;
+    int rc = current_device(&dev);
+    if (rc == ASER_OK) rc = device_sm_count(&num_sms);
     if (rc != ASER_OK) return rc;
     if (!configured[dev]) {
-        const cudaError_t e = cudaFuncSetAttribute(adapters_kernel<MT, TW>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                   (int)smem_bytes<MT, TW>(256));
+        const cudaError_t e = cudaFuncSetAttribute(adapters_few_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, few_smem(256));
         if (e != cudaSuccess) return record_cuda_error(e, "adapters smem attribute");
         configured[dev] = true;
     }
+    // several clusters to a tile where few tiles leave room, each with S of its own, until a warp has 32 channels
+    const int tiles = plan_tiles(p.M, p.n_slots, kTok), want = (p.N + 32 * kCL * kWarps - 1) / (32 * kCL * kWarps), room = 2 * num_sms / (tiles * kCL);
+    p.parts = room < 1 ? 1 : room > want ? want : room;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(tiles * p.parts * CL, 1, 1);
-    cfg.blockDim = dim3(kAThreads, 1, 1);
-    cfg.dynamicSmemBytes = smem_bytes<MT, TW>(p.r);
+    cfg.gridDim = dim3(tiles * p.parts * kCL, 1, 1);
+    cfg.blockDim = dim3(kThreads, 1, 1);
+    cfg.dynamicSmemBytes = few_smem(p.r);
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = CL; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    attr[1].val.clusterDim.x = kCL; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, adapters_kernel<MT, TW>, p);
-    if (e != cudaSuccess) return record_cuda_error(e, "adapters_kernel");
-    return check_launch("adapters_kernel");
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, adapters_few_kernel, p);
+    if (e != cudaSuccess) return record_cuda_error(e, "adapters_few_kernel");
+    return check_launch("adapters_few_kernel");
 }
 
 }  // namespace
 
 size_t adapters_plan_bytes(int M, int n_slots) {
-    const PlanView v = plan_view(static_cast<int32_t*>(nullptr), M, n_slots);
+    const PlanView v = plan_view(nullptr, M, n_slots);
     return (size_t)v.words * 4;
 }
 
@@ -399,25 +390,21 @@ int launch_adapters_plan(const int32_t* slot, int M, int n_slots, void* plan, cu
     return check_launch("adapters_plan_kernel");
 }
 
-int launch_adapters(const __half* X, size_t ldx, const __half* A, const __half* B, const int32_t* ranks, const float* scale,
-                    const void* plan, int M, int N, int K, int r, int n_slots, const __half* Y, size_t ldy, __half* out,
-                    size_t ldo, cudaStream_t st) {
-    AdapterParams p = {};
-    p.X = X; p.A = A; p.B = B; p.ranks = ranks; p.scale = scale; p.plan = static_cast<const int32_t*>(plan);
-    p.Y = Y; p.out = out;
-    p.ldx = ldx; p.ldy = ldy; p.ldo = ldo;
-    p.M = M; p.N = N; p.K = K; p.r = r; p.n_slots = n_slots;
-    int num_sms = 0;
-    const int rc = device_sm_count(&num_sms);
-    if (rc != ASER_OK) return rc;
+bool adapters_many(int M, int n_slots) {
     const int used = n_slots < M ? n_slots : M;
-    const bool few = M <= 16 * used;
-    const int CL = 8;
-    const int bound = plan_tiles(M, n_slots, few ? kTileFew : kTileMany);
-    const int parts = 2 * num_sms / (bound * CL);
-    const int want = (N + K - 1) / K;
-    p.parts = parts < 1 ? 1 : parts > want ? want : parts;
-    return few ? launch_tiles<1, 1>(p, bound, CL, st) : launch_tiles<2, 2>(p, bound, CL, st);
+    return M > 24 * used;
+}
+
+size_t adapters_workspace_bytes(int M, int r, int n_slots) {
+    return adapters_many(M, n_slots) ? (size_t)M * 2 * r + (size_t)M * 4 : 0;
+}
+
+int launch_adapters(AdapterParams p, void* workspace, cudaStream_t st) {
+    if (!adapters_many(p.M, p.n_slots)) return launch_few(p, st);
+    p.S = static_cast<__half*>(workspace);
+    p.row_scale = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + (size_t)p.M * 2 * p.r);
+    const int rc = launch_adapters_down(p, st);
+    return rc != ASER_OK ? rc : launch_adapters_up(p, true, st);
 }
 
 }  // namespace aser

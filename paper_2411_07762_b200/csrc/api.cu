@@ -172,7 +172,7 @@ bool ffn_layout(int M, int K, int F, int N, int r, int r_down, FfnLayout* l) {
 constexpr int kMaxSlots = 4096, kMaxAdapterTokens = 1 << 24;
 int adapters_check(const void* X_f16, int ldx, const void* A_f16, const void* B_f16, const int32_t* ranks, const float* scale,
                    const void* plan, size_t plan_bytes, int M, int N, int K, int r, int n_slots, const void* Y_f16, int ldy,
-                   const void* out_f16, int ldo) {
+                   const void* out_f16, int ldo, const void* workspace, size_t workspace_bytes) {
     if (!shape_ok(M, N, K, r) || M > kMaxAdapterTokens) return fail(ASER_ERR_SHAPE, "unsupported M, N, K or r");
     if (n_slots < 1 || n_slots > kMaxSlots) return fail(ASER_ERR_SHAPE, "n_slots must be 1..4096");
     if (ldx < K || ldy < N || ldo < N || (ldx | ldy | ldo) % 8 != 0)
@@ -190,7 +190,22 @@ int adapters_check(const void* X_f16, int ldx, const void* A_f16, const void* B_
         ASER_REQUIRE_PTR(B_f16);
     }
     if (plan_bytes < adapters_plan_bytes(M, n_slots)) return fail(ASER_ERR_WORKSPACE, "plan too small for M and n_slots");
+    const size_t need = adapters_workspace_bytes(M, r, n_slots);
+    if (need > 0 && (workspace == nullptr || misaligned16(workspace) || workspace_bytes < need))
+        return fail(ASER_ERR_WORKSPACE, "workspace missing, misaligned or too small");
     return ASER_OK;
+}
+
+AdapterParams adapter_params(const void* X_f16, int ldx, const void* A_f16, const void* B_f16, const int32_t* ranks,
+                             const float* scale, const void* plan, int M, int N, int K, int r, int n_slots, const void* Y_f16,
+                             int ldy, void* out_f16, int ldo) {
+    AdapterParams p = {};
+    p.X = static_cast<const __half*>(X_f16); p.A = static_cast<const __half*>(A_f16); p.B = static_cast<const __half*>(B_f16);
+    p.ranks = ranks; p.scale = scale; p.plan = static_cast<const int32_t*>(plan);
+    p.Y = static_cast<const __half*>(Y_f16); p.out = static_cast<__half*>(out_f16);
+    p.ldx = ldx; p.ldy = ldy; p.ldo = ldo;
+    p.M = M; p.N = N; p.K = K; p.r = r; p.n_slots = n_slots;
+    return p;
 }
 
 // Stacked ranks (several layers' down projections in one pass) go up to 512.
@@ -582,19 +597,24 @@ int aser_adapters_plan(const int32_t* slot, int M, int n_slots, void* plan, size
     return launch_adapters_plan(slot, M, n_slots, plan, static_cast<cudaStream_t>(stream));
 }
 
+size_t aser_adapters_workspace_bytes(int M, int r, int n_slots) {
+    if (M < 0 || M > kMaxAdapterTokens || !shape_ok(0, 0, 128, r) || n_slots < 1 || n_slots > kMaxSlots) return 0;
+    return adapters_workspace_bytes(M, r, n_slots);
+}
+
 int aser_adapters_add(const void* X_f16, int ldx, const void* A_f16, const void* B_f16, const int32_t* ranks, const float* scale,
                       const void* plan, size_t plan_bytes, int M, int N, int K, int r, int n_slots, const void* Y_f16, int ldy,
-                      void* out_f16, int ldo, void* stream) {
+                      void* out_f16, int ldo, void* workspace, size_t workspace_bytes, void* stream) {
     if (ldx == 0) ldx = K;
     if (ldy == 0) ldy = N;
     if (ldo == 0) ldo = N;
-    int rc = adapters_check(X_f16, ldx, A_f16, B_f16, ranks, scale, plan, plan_bytes, M, N, K, r, n_slots, Y_f16, ldy, out_f16, ldo);
+    int rc = adapters_check(X_f16, ldx, A_f16, B_f16, ranks, scale, plan, plan_bytes, M, N, K, r, n_slots, Y_f16, ldy, out_f16, ldo,
+                            workspace, workspace_bytes);
     if (rc != ASER_OK || M == 0 || N == 0) return rc;
     rc = check_device();
     if (rc != ASER_OK) return rc;
-    return launch_adapters(static_cast<const __half*>(X_f16), ldx, static_cast<const __half*>(A_f16), static_cast<const __half*>(B_f16),
-                           ranks, scale, plan, M, N, K, r, n_slots, static_cast<const __half*>(Y_f16), ldy,
-                           static_cast<__half*>(out_f16), ldo, static_cast<cudaStream_t>(stream));
+    return launch_adapters(adapter_params(X_f16, ldx, A_f16, B_f16, ranks, scale, plan, M, N, K, r, n_slots, Y_f16, ldy, out_f16, ldo),
+                           workspace, static_cast<cudaStream_t>(stream));
 }
 
 size_t aser_forward_ffn_workspace_bytes(int M, int K, int F, int N, int r, int r_down) {
@@ -904,15 +924,16 @@ int aser_forward(const void* X_f16, const float* s, const void* LA_f16, const vo
 int aser_forward_adapters(const void* X_f16, const float* s, const void* LA_f16, const void* Wk, const float* w_scale,
                           const void* LB_f16, int M, int N, int K, int r, int8_t* Xq, float* a_scale, void* T_bf16, void* Y_f16,
                           void* workspace, size_t workspace_bytes, const void* A_f16, const void* B_f16, const int32_t* ranks,
-                          const float* scale, const void* plan, size_t plan_bytes, int r_adapter, int n_slots, void* stream) {
+                          const float* scale, const void* plan, size_t plan_bytes, int r_adapter, int n_slots, void* adapter_workspace,
+                          size_t adapter_workspace_bytes, void* stream) {
     // the adapters' arguments are checked before the layer is enqueued (M == 0: nothing is)
-    int rc = adapters_check(X_f16, K, A_f16, B_f16, ranks, scale, plan, plan_bytes, M, N, K, r_adapter, n_slots, Y_f16, N, Y_f16, N);
+    int rc = adapters_check(X_f16, K, A_f16, B_f16, ranks, scale, plan, plan_bytes, M, N, K, r_adapter, n_slots, Y_f16, N, Y_f16, N,
+                            adapter_workspace, adapter_workspace_bytes);
     if (rc != ASER_OK) return rc;
     rc = aser_forward(X_f16, s, LA_f16, Wk, w_scale, LB_f16, M, N, K, r, Xq, a_scale, T_bf16, Y_f16, workspace, workspace_bytes, stream);
     if (rc != ASER_OK || M == 0 || N == 0) return rc;
-    return launch_adapters(static_cast<const __half*>(X_f16), K, static_cast<const __half*>(A_f16), static_cast<const __half*>(B_f16),
-                           ranks, scale, plan, M, N, K, r_adapter, n_slots, static_cast<const __half*>(Y_f16), N,
-                           static_cast<__half*>(Y_f16), N, static_cast<cudaStream_t>(stream));
+    return launch_adapters(adapter_params(X_f16, K, A_f16, B_f16, ranks, scale, plan, M, N, K, r_adapter, n_slots, Y_f16, N, Y_f16, N),
+                           adapter_workspace, static_cast<cudaStream_t>(stream));
 }
 
 int aser_forward_host_parts(int M, int N, int K, int* first_token) {

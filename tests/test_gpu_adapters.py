@@ -26,8 +26,8 @@ def normal(g, *shape, scale=1.0):
 
 def expected(X, Y, A, B, ranks, scale, slot):
     """The update in 64 bits, and how far the kernel may be from it, element by element:
-      * S = A x in fp32: the products of two fp16 numbers are exact; K / 512 + 32 additions on a sum's longest way (an
-        instruction adds 16 products, 32 warps and more share K, then their sums are added), each off by at most 2^-22 of the
+      * S = A x in fp32: the products of two fp16 numbers are exact; K / 128 + 32 additions on a sum's longest way (an
+        instruction adds 16 products, 8 warps and more share K, then their sums are added), each off by at most 2^-22 of the
         sum of magnitudes (a truncated addition in the tensor cores);
       * S to fp16: 2^-11 of each entry, or 2^-25 2^(e - 14) <= 2^-38 of the token's largest below the normal range;
       * B S in fp32: r / 16 + 8 additions, as above; the factor and the final addition 2^-22 of the update and Y;
@@ -45,7 +45,7 @@ def expected(X, Y, A, B, ranks, scale, slot):
         x, aa, bb = X[rows].double(), A[a, :r].double(), B[a, :, :r].double()
         s = x @ aa.T
         l1 = x.abs() @ aa.abs().T
-        ds = (K / 512 + 32) * 2.0 ** -22 * l1 + 2.0 ** -11 * s.abs() + 2.0 ** -38 * s.abs().amax(1, keepdim=True)
+        ds = (K / 128 + 32) * 2.0 ** -22 * l1 + 2.0 ** -11 * s.abs() + 2.0 ** -38 * s.abs().amax(1, keepdim=True)
         f = abs(float(scale[a]))
         ref[rows] += float(scale[a]) * (s @ bb.T)
         bound[rows] = f * (ds @ bb.abs().T + (r / 16 + 8 + 1) * 2.0 ** -22 * (s.abs() @ bb.abs().T)) * (1 + 2.0 ** -9) \
@@ -182,13 +182,12 @@ def test_ranks_that_are_no_ranks(aser):
 def read_plan(plan):
     w = plan.data.view(torch.int32).cpu()
     M, S = plan.M, plan.n_slots
-    few, many = (M // t + min(S + 1, M) for t in (16, 64))
-    head, at = w[:4].tolist(), 4
-    tiles = []
-    for bound, n in ((few, head[2]), (many, head[3])):
+    head, at, tiles = w[:4].tolist(), 4, []
+    for size, words, n in ((16, 20, head[2]), (128, 4, head[3])):
+        bound = M // size + min(S + 1, M)
         assert n <= bound
-        tiles.append(w[at:at + 4 * n].reshape(-1, 4).tolist())
-        at += 4 * bound
+        tiles.append(w[at:at + words * n].reshape(-1, words).tolist())
+        at += words * bound
     return head, tiles, w[at:at + M].tolist()
 
 
@@ -200,10 +199,11 @@ def test_plan(aser, M, slots):
     s = [a if 0 <= a < slots else -1 for a in slot.tolist()]
     want = sorted(range(M), key=lambda m: (s[m] if s[m] >= 0 else slots, m))
     assert head[:2] == [M, slots] and tokens == want
-    for size, ts in zip((16, 64), tiles):
+    for size, ts in zip((16, 128), tiles):
         at = 0
-        for a, first, count, _ in ts:
+        for a, first, count, _, *own in ts:
             assert first == at and 1 <= count <= size and all(s[m] == a for m in tokens[first:first + count])
+            assert not own or own[:count] == tokens[first:first + count]
             at += count
         assert at == M
 

@@ -62,8 +62,9 @@ def test_adapter_plan_is_refused(lib):
 
 def test_adapters_are_refused(lib):
     def call(M=8, N=64, K=256, r=16, S=4, X=GOOD, A=GOOD, B=GOOD, ranks=None, plan=GOOD, nbytes=1 << 20, Y=GOOD, out=GOOD, ldx=0,
-             ldy=0, ldo=0):
-        return lib.aser_adapters_add(X, ldx, A, B, ranks, None, plan, nbytes, M, N, K, r, S, Y, ldy, out, ldo, None)
+             ldy=0, ldo=0, ws=GOOD, wbytes=1 << 20):
+        return lib.aser_adapters_add(X, ldx, A, B, ranks, None, plan, nbytes, M, N, K, r, S, Y, ldy, out, ldo, ws, wbytes,
+                                     None)
     assert call(M=0, X=None, plan=None, nbytes=0) == OK and call(N=0, Y=None) == OK
     assert call(K=200) == SHAPE and call(N=60) == SHAPE and call(r=24) == SHAPE and call(r=272) == SHAPE and call(M=-1) == SHAPE
     assert call(M=(1 << 24) + 1) == SHAPE and call(S=0) == SHAPE and call(S=4097) == SHAPE
@@ -72,12 +73,16 @@ def test_adapters_are_refused(lib):
     assert call(X=None) == NULL and call(A=None) == NULL and call(B=None) == NULL and call(plan=None) == NULL
     assert call(Y=None) == NULL and call(out=None) == NULL and call(ranks=ODD) == ALIGN and call(out=ODD) == ALIGN
     assert call(nbytes=lib.aser_adapters_plan_bytes(8, 4) - 1) == WORKSPACE
+    need = lib.aser_adapters_workspace_bytes(500, 16, 4)
+    assert need == 500 * (2 * 16 + 4) and lib.aser_adapters_workspace_bytes(96, 16, 4) == 0
+    assert lib.aser_adapters_workspace_bytes(500, 24, 4) == 0 and lib.aser_adapters_workspace_bytes(-1, 16, 4) == 0
+    assert call(M=500, ws=None) == WORKSPACE and call(M=500, wbytes=need - 1) == WORKSPACE and call(M=500, ws=ODD) == WORKSPACE
 
 
 def test_projection_with_adapters_is_refused(lib):
     def call(M=8, N=64, K=256, r=16, ra=16, X=GOOD, LA=GOOD, Y=GOOD, ws=GOOD, A=GOOD, plan=GOOD, nbytes=1 << 20):
         return lib.aser_forward_adapters(X, None, LA, GOOD, GOOD, GOOD, M, N, K, r, GOOD, GOOD, GOOD, Y, ws, 1 << 26, A, GOOD, None,
-                                         None, plan, nbytes, ra, 4, None)
+                                         None, plan, nbytes, ra, 4, None, 0, None)
     assert call(M=0, X=None, ws=None) == OK
     assert call(K=100) == SHAPE and call(ra=8) == SHAPE and call(r=8) == SHAPE and call(N=12) == SHAPE
     assert call(X=None) == NULL and call(LA=None) == NULL and call(A=None) == NULL and call(plan=None) == NULL
