@@ -299,7 +299,8 @@ int aser_forward_ffn(const void* X_f16, const float* s, const void* LA_f16, cons
  *                                                                        rounded to fp16 between the two products)
  * x is the activation itself, not the smoothed one.  A_f16 [n_slots, r, K], B_f16 [n_slots, N, r]; ranks [n_slots] int32 (NULL: all r):
  * adapter a is of rank ranks[a], a multiple of 16 from 0 to r (other values are taken down to one); rows of A and columns of B
- * behind it are not read.  scale [n_slots] fp32 (NULL: ones).  r % 16 == 0, r <= 256, 1 <= n_slots <= 4096.
+ * behind it are not used.  scale [n_slots] fp32 (NULL: ones).  r % 16 == 0, r <= 256, 1 <= n_slots <= 4096,
+ * n_slots * N < 2^31.
  *
  * aser_adapters_plan -- lists a batch's tokens by adapter: slot [M] int32, the adapter of each token; any value outside
  * 0 .. n_slots - 1 means none (the padding of a batch, too).  One plan serves every adapter call of a step, whatever its layer; it is

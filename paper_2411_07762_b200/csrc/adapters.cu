@@ -31,9 +31,6 @@ constexpr int kPlanThreads = 1024;
 // Bytes between the fp16 rows of S: an odd multiple of 64, so that 16-byte reads of two rows do not meet in a bank.
 __host__ __device__ constexpr int s_stride(int r) { return (2 * r + 63) / 128 * 128 + 64; }
 
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
 __device__ __forceinline__ void st_cluster_f32x4(uint32_t addr, const float4& v) {
     asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
 }
@@ -113,7 +110,7 @@ adapters_few_kernel(const AdapterParams p) {
             const int n = n_first * 32 + row;
             if (c < chunks && n < p.N) cp_async16(smem_u32(b_rows) + row * 128 + ((c ^ ((row & 1) << 2)) << 4), B + (size_t)n * p.r + c * 8);
         }
-        asm volatile("cp.async.commit_group;" ::: "memory");
+        cp_async_commit();
     }
 
     // ---- S = A x: this CTA's part of K, the warps' parts of it ----
@@ -204,7 +201,7 @@ adapters_few_kernel(const AdapterParams p) {
             if (lane == 0) row_scale[row] = f.down * alpha;
         }
     }
-    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    cp_async_wait<0>();
     __syncthreads();
     if (!narrow) cluster_arrive();          // (waited for at the end: nobody leaves while a peer may still read its sums)
 
@@ -306,15 +303,16 @@ adapters_plan_kernel(const int32_t* __restrict__ slot, int M, int n_slots, int32
     __syncthreads();
     at.x -= mine.x; at.y -= mine.y; at.z -= mine.z;
     for (int w = 0; w < warp; ++w) { at.x += warp_sum[w].x; at.y += warp_sum[w].y; at.z += warp_sum[w].z; }
-    __shared__ int few;
+    __shared__ int few, many;
     if (tid == kPlanThreads - 1) {
         few = at.y + mine.y;
-        *reinterpret_cast<int4*>(out) = make_int4(M, n_slots, few, at.z + mine.z);
+        many = at.z + mine.z;
+        *reinterpret_cast<int4*>(out) = make_int4(M, n_slots, few, many);
     }
     for (int i = g0; i < g1; ++i) {
         const int n = cursor[i], s = i < n_slots ? i : -1;
         for (int k = 0; k < n; k += kTileFew) *reinterpret_cast<int4*>(plan.tiles_few + (size_t)kFewWords * at.y++) = make_int4(s, at.x + k, min(kTileFew, n - k), 0);
-        for (int k = 0; k < n; k += kTileMany) plan.tiles_many[at.z++] = make_int4(s, at.x + k, min(kTileMany, n - k), 0);
+        for (int k = 0; k < n; k += kTileMany) plan.tiles_many[at.z++] = make_int4(s, at.x + k, min(kTileMany, n - k), -1);
         cursor[i] = at.x;
         at.x += n;
     }
@@ -342,6 +340,11 @@ adapters_plan_kernel(const int32_t* __restrict__ slot, int M, int n_slots, int32
         int32_t* record = plan.tiles_few + (size_t)kFewWords * (i / kTileFew);
         const int e = i % kTileFew;
         record[4 + e] = e < record[2] ? plan.tokens[record[1] + e] : 0;
+    }
+    for (int i = tid; i < many; i += kPlanThreads) {         // (a group's tokens ascend)
+        const int4 r = plan.tiles_many[i];
+        const int a = plan.tokens[r.y], b = plan.tokens[r.y + r.z - 1];
+        if (b - a == r.z - 1) plan.tiles_many[i].w = a;
     }
 }
 
@@ -404,7 +407,7 @@ int launch_adapters(AdapterParams p, void* workspace, cudaStream_t st) {
     p.S = static_cast<__half*>(workspace);
     p.row_scale = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + (size_t)p.M * 2 * p.r);
     const int rc = launch_adapters_down(p, st);
-    return rc != ASER_OK ? rc : launch_adapters_up(p, true, st);
+    return rc != ASER_OK ? rc : launch_adapters_up(p, st);
 }
 
 }  // namespace aser

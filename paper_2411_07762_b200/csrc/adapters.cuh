@@ -1,7 +1,7 @@
 // The plan of a batch's adapters (adapters.cu): tokens by adapter, cut into tiles of one adapter each.
 //   words 0 .. 3   M, n_slots, tiles of kTileFew tokens, tiles of kTileMany tokens
 //   tiles of 16    {adapter or -1, first place in the list of tokens, tokens, 0, their numbers [16]}: one round of loads
-//   tiles of 128   the first four of these
+//   tiles of 128   {adapter or -1, first place, tokens, the first token's number if they follow one another, else -1}
 //   tokens         [M] token numbers by adapter, those without one last
 #pragma once
 #include "aser_common.cuh"
@@ -57,7 +57,7 @@ size_t adapters_workspace_bytes(int M, int r, int n_slots);
 // (p.S and p.row_scale are set from `workspace`.)
 int launch_adapters(AdapterParams p, void* workspace, cudaStream_t st);
 int launch_adapters_down(const AdapterParams& p, cudaStream_t st);
-int launch_adapters_up(const AdapterParams& p, bool y_ready, cudaStream_t st);
+int launch_adapters_up(const AdapterParams& p, cudaStream_t st);
 
 #ifdef __CUDACC__
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -66,6 +66,12 @@ __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 // The rank of an adapter: a multiple of 16 from 0 to r.
 __device__ __forceinline__ int adapter_rank(const AdapterParams& p, int slot) {
     const int rk = p.ranks ? __ldg(p.ranks + slot) : p.r;

@@ -1,16 +1,19 @@
-// Low-rank adapters of many requests (adapters.cu) where an adapter has many tokens, as in prompts: two launches.
+// Low-rank adapters of many requests (adapters.cu) where an adapter has many tokens, as in prompts: two launches, on the tensor
+// cores (tcgen05, kind::f16) with everything that is large brought by tensor copies.
 //
-//   S = A_a x      adapters_down_kernel: a cluster of CTAs per tile of 128 tokens of one adapter, split along K.  What bounds it is X
-//                  from HBM and A from L2 (again for every tile: the reason for 128 tokens).  Both go to shared memory 64 columns
-//                  at a time by asynchronous copies of 16 bytes, because a tile's rows lie anywhere in the batch; a ring of
-//                  stages keeps 72 KB a CTA in flight, two CTAs to an SM.  Partial sums meet in distributed shared memory, in a
-//                  fixed order, each CTA finishing 128 / CL tokens.
-//   out = Y + B S  adapters_up_kernel: a CTA per tile and 128 channels; bound by Y, read and written once.  Nothing carries over from
-//                  block to block, so enough CTAs are resident to keep the loads of Y in flight, and B and Y are asked for while
-//                  the first kernel still runs.
+//   S = A_a x      adapters_down_kernel: a cluster of CTAs per tile of 128 tokens of one adapter, split along K; D[token, rank] in
+//                  tensor memory for all ranks at once, so X is read once whatever the rank.  What bounds it is X from HBM and A from
+//                  L2 (again for every tile: the reason for 128 tokens).  Partial sums meet in distributed shared memory, in a
+//                  fixed order, each CTA finishing its share of the tokens.
+//   out = Y + B S  adapters_up_kernel: a CTA per tile and a range of channels, 64 at a time, D[token, channel]; bound by Y, read and
+//                  written once.  Y and B come through a ring; eight warps, alternately four to a block, add a block's sums to Y where
+//                  it lies in shared memory, a token to a thread, and write whole 128-byte lines from there.
 //
-// One launch for both (the kernel for few tokens with larger tiles) spent most of its time in phases that wait for one
-// another: 4096 tokens of 6 adapters, rank 64, 4096 x 4096 65.7 us.
+// A tile's tokens lie anywhere in the batch.  Where they follow one another (a prompt), copies take 32 rows at a time, else four
+// rows by number (tile::gather4).  Before, threads fetched the rows 16 bytes at a time: 15 cycles an instruction and
+// SM, which bound both kernels (4096 tokens of 6 adapters, rank 64, 4096 x 4096: 47 us).
+//
+// Every wait is bounded; a warp that gives up leaves NaN in what it would have written.
 #include "adapters.cuh"
 #include "sm100_ptx.cuh"
 
@@ -18,320 +21,507 @@ namespace aser {
 
 namespace {
 
-constexpr int kThreads = 256, kTok = kTileMany, kCL = 8;
-constexpr int kCols = 64;                            // columns of a stage: 128 bytes a row, swizzled by row % 8
-constexpr int kXBytes = kTok * kCols * 2;
-constexpr int kUpCols = 128;                         // channels of a CTA of the second kernel
+constexpr int kTok = kTileMany, kMaxCL = 8, kBox = 32;
+constexpr int kCols = 64;                            // columns or channels of a stage: 128 bytes a row
+constexpr int kRowsBytes = kTok * kCols * 2;
+constexpr int kMaxStages = 6;
+constexpr long long kWaitClocks = 400000000ll;       // about 0.2 s of SM clocks per wait
 
-// Ranks side by side in a pass of the first kernel: 64, the two halves of the warps taking alternate steps of K, or 128, half each.
-template <int NR>
-struct DownCfg {
-    static constexpr int Ranks = 64 * NR;
-    static constexpr int Stage = kXBytes + Ranks * kCols * 2;
-    static constexpr int Stages = NR == 1 ? 4 : 3;
-    static constexpr int RowFloats = Ranks + 4;      // of the partial sums, which take the place of the stages
-    static constexpr int Smem = Stage * Stages;
-    static_assert(kTok * RowFloats * 4 <= Smem, "partial sums fit the ring");
-    static_assert(2 * Smem + 4096 <= 227 * 1024, "two CTAs to an SM");
+// False after the limit, or when another warp of this CTA gave up.
+__device__ __forceinline__ bool bounded_wait(uint32_t bar, uint32_t parity, volatile int* stop) {
+    long long t0 = 0;
+    for (uint32_t spins = 0; !mbar_try_wait(bar, parity); ++spins)
+        if ((spins & 255u) == 255u) {
+            if (*stop) return false;
+            const long long now = clock64();
+            if (t0 == 0) t0 = now;
+            else if (now - t0 > kWaitClocks) { *stop = 1; return false; }
+        }
+    return true;
+}
+// One lane polls.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* stop, int lane) {
+    int ok = 1;
+    if (lane == 0) ok = bounded_wait(bar, parity, stop) ? 1 : 0;
+    return __shfl_sync(0xffffffffu, ok, 0) != 0;
+}
+// Copies in flight land before a CTA that gave up lets go of its shared memory.
+__device__ __forceinline__ void let_copies_land() {
+    const long long t0 = clock64();
+    while (clock64() - t0 < 2000000) {}
+}
+
+// A tile's rows of a matrix, 64 columns from `col`, by one warp.
+struct TileRows {
+    int first_token;       // >= 0: the tokens follow one another from here
+    int count;
+    int4 four;             // else the numbers of tokens 4 lane .. 4 lane + 3 (the first one's in the place of those that are not there)
+    __device__ __forceinline__ int rows() const { return first_token >= 0 ? (count + kBox - 1) / kBox * kBox : (count + 3) / 4 * 4; }
+    __device__ __forceinline__ void load(uint32_t dst, const CUtensorMap* box, const CUtensorMap* one, int col, uint32_t bar, int lane) const {
+        if (first_token >= 0) {
+            if (lane * kBox < count) tma_load_2d(dst + lane * kBox * 128, box, col, first_token + lane * kBox, bar);
+        } else if (lane * 4 < count) {
+            tma_gather4(dst + lane * 512, one, col, four.x, four.y, four.z, four.w, bar);
+        }
+    }
 };
-
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+__device__ __forceinline__ TileRows tile_rows(const int4& t4, const int32_t* tokens, int lane) {
+    TileRows r;
+    r.first_token = t4.w;
+    r.count = t4.z;
+    r.four = make_int4(0, 0, 0, 0);
+    if (t4.w < 0) {
+        const int32_t* list = tokens + t4.y;
+        const int i = lane * 4, zero = list[0];
+        r.four = make_int4(i < t4.z ? list[i] : zero, i + 1 < t4.z ? list[i + 1] : zero, i + 2 < t4.z ? list[i + 2] : zero,
+                           i + 3 < t4.z ? list[i + 3] : zero);
+    }
+    return r;
 }
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-__device__ __forceinline__ void ldmatrix4(uint32_t (&v)[4], uint32_t addr) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
-                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(addr) : "memory");
+
+__device__ __forceinline__ void tmem_alloc(uint32_t* slot, uint32_t cols) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(slot)), "r"(cols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_free(uint32_t tmem, uint32_t cols) {
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(cols) : "memory");
 }
 
-template <int NR>
-__global__ void __launch_bounds__(kThreads, 2)
-adapters_down_kernel(const AdapterParams p) {
-    using C = DownCfg<NR>;
+// ---------------------------------------------------------------------------
+// S = A x
+// ---------------------------------------------------------------------------
+constexpr int kDownThreads = 256, kDownWarps = 8;
+
+struct DownMaps { CUtensorMap x, x_one, a; };
+
+__host__ __device__ constexpr int down_stage_bytes(int r) { return kRowsBytes + r * kCols * 2; }
+// The ring also holds the partial sums at the end, [128][rank + 4] floats; up to 200 KB of it.
+__host__ __device__ constexpr int down_stages(int r) { return r <= 128 ? 6 : 4; }
+constexpr int kDownTail = kMaxStages * 16 + 32;      // barriers, tensor memory's address, flag
+constexpr int down_smem(int r) { return down_stages(r) * down_stage_bytes(r) + kDownTail + 1024; }
+static_assert(down_smem(128) <= 227 * 1024 && down_smem(256) <= 227 * 1024, "shared memory budget");
+
+__global__ void __launch_bounds__(kDownThreads, 1)
+adapters_down_kernel(const __grid_constant__ DownMaps maps, const AdapterParams p, uint32_t tmem_cols) {
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    const int stage_bytes = down_stage_bytes(p.r), stages = down_stages(p.r);
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + stages * stage_bytes);       // [stage]: filled, free
+    uint64_t* done = bars + 2 * kMaxStages;                                          // all products are complete
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 1);
+    volatile int* stop = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (warp == 0) {
+        tmem_alloc(tmem_slot, tmem_cols);
+    } else if (warp == 1) {
+        if (lane < 2 * kMaxStages + 1) mbar_init(smem_u32(bars + lane), 1);
+        if (lane == 0) *stop = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_proxy_async_smem();
+    } else if (warp == 2 && lane == 0) {
+        prefetch_tensormap(&maps.x);
+        prefetch_tensormap(&maps.a);
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot, sb = smem_u32(smem), bar0 = smem_u32(bars);
+    auto filled = [&](int s) { return bar0 + 16u * s; };
+    auto free_ = [&](int s) { return bar0 + 16u * s + 8u; };
     grid_dep_wait();
     grid_dep_launch();
-    extern __shared__ __align__(128) uint8_t smem[];
-    const int rank = (int)cluster_rank(), tile = (int)(blockIdx.x / kCL);
+    const int CL = (int)cluster_size(), rank = (int)cluster_rank(), tile = (int)blockIdx.x / CL;
     const PlanView plan = plan_view(p.plan, p.M, p.n_slots);
     const int4 head = *reinterpret_cast<const int4*>(p.plan);
     const int4 t4 = plan.tiles_many[tile];
-    if (head.x != p.M || head.y != p.n_slots || tile >= head.w) return;
-    const int slot = t4.x, first = t4.y, count = t4.z;
+    const bool real = head.x == p.M && head.y == p.n_slots && tile < head.w;
+    const int slot = real ? t4.x : -1, first = t4.y, count = t4.z;
     const int rk = slot < 0 ? 0 : adapter_rank(p, slot);
-    if (rk == 0) return;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int tw = warp & 3, half = warp >> 2;
-    const uint32_t sb = smem_u32(smem);
-    // copies: this thread's 16 bytes of rows lr, lr + 32, ...
-    const int lr = threadIdx.x >> 3, lc = threadIdx.x & 7;
-    const uint32_t to = (uint32_t)(lr * 128 + ((lc ^ (lr & 7)) << 4));      // (rows 32 apart have the same swizzle)
-    const __half* xp[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        xp[i] = lr + 32 * i < count ? p.X + (size_t)plan.tokens[first + lr + 32 * i] * p.ldx + lc * 8 : nullptr;
-    const int steps = p.K / kCols, s0 = rank * steps / kCL, s1 = (rank + 1) * steps / kCL;
-    float4 sum[2][2];                     // [pass][row of this warp]: four sums a lane
-    float* part = reinterpret_cast<float*>(smem);
-#pragma unroll
-    for (int pass = 0; pass < 2; ++pass) {
-        const int r0 = pass * C::Ranks;
-        sum[pass][0] = sum[pass][1] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (r0 >= rk) continue;
-        const __half* ap = p.A + ((size_t)slot * p.r + r0 + lr) * p.K + lc * 8;
-        auto load = [&](int s) {
-            if (s < s1) {
-                const uint32_t at = sb + (uint32_t)((s - s0) % C::Stages * C::Stage) + to;
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (xp[i]) cp_async16(at + i * 4096, xp[i] + (size_t)s * kCols);
-#pragma unroll
-                for (int i = 0; i < 2 * NR; ++i)
-                    if (r0 + lr + 32 * i < rk) cp_async16(at + kXBytes + i * 4096, ap + (size_t)32 * i * p.K + (size_t)s * kCols);
+    if (rk > 0) {                     // (the whole cluster)
+        const int steps = p.K / kCols, s0 = rank * steps / CL, n = (rank + 1) * steps / CL - s0;
+        if (warp == 0) {              // copies
+            const TileRows rows = tile_rows(t4, plan.tokens, lane);
+            const uint32_t bytes = (uint32_t)(rows.rows() + rk) * 128u;
+            for (int i = 0, s = 0, turn = 0; i < n; ++i) {
+                if (turn > 0 && !warp_wait(free_(s), (uint32_t)(turn - 1) & 1u, stop, lane)) break;
+                if (lane == 0) mbar_arrive_expect_tx(filled(s), bytes);
+                __syncwarp();
+                const uint32_t at = sb + (uint32_t)(s * stage_bytes);
+                const int col = (s0 + i) * kCols;
+                rows.load(at, &maps.x, &maps.x_one, col, filled(s), lane);
+                if (lane * 16 < rk) tma_load_2d(at + kRowsBytes + lane * 2048, &maps.a, col, slot * p.r + lane * 16, filled(s));
+                if (++s == stages) { s = 0; ++turn; }
             }
-            cp_async_commit();
-        };
-        float acc[2][8][4];
+        } else if (warp == 1) {       // products (rows that are not there are whatever the ring holds: nobody reads their sums)
+            const uint32_t idesc = make_idesc(1, 0, 128, rk);
+            for (int i = 0, s = 0, turn = 0; i < n; ++i) {
+                if (!warp_wait(filled(s), (uint32_t)turn & 1u, stop, lane)) break;
+                tc_fence_after();
+                if (elect_one()) {
+                    const uint32_t at = sb + (uint32_t)(s * stage_bytes);
+                    const uint64_t xd = smem_desc_sw128(at), ad = smem_desc_sw128(at + kRowsBytes);
 #pragma unroll
-        for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-            for (int nt = 0; nt < 8; ++nt)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[mt][nt][e] = 0.f;
-#pragma unroll
-        for (int s = 0; s < C::Stages - 1; ++s) load(s0 + s);
-        // rows behind the tile's last token and ranks behind the adapter's are whatever the ring holds: nobody reads their sums
-        const int nts = NR == 2 ? (rk - r0 - 64 * half + 15) / 16 : (rk - r0 + 15) / 16;     // pairs of 8 ranks of this warp
-        for (int s = s0; s < s1; ++s) {
-            cp_async_wait<C::Stages - 2>();
-            __syncthreads();
-            load(s + C::Stages - 1);
-            const uint32_t xs = sb + (uint32_t)((s - s0) % C::Stages * C::Stage), as = xs + kXBytes;
-#pragma unroll
-            for (int kk0 = 0; kk0 < (NR == 2 ? 4 : 2); ++kk0) {
-                const int kk = NR == 2 ? kk0 : 2 * half + kk0;
-                uint32_t x[2][4];
-#pragma unroll
-                for (int mt = 0; mt < 2; ++mt) {
-                    const int row = tw * 32 + mt * 16 + (lane & 15);
-                    ldmatrix4(x[mt], xs + row * 128 + (((kk * 2 + (lane >> 4)) ^ (row & 7)) << 4));
+                    for (int kk = 0; kk < 4; ++kk) mma_f16_ss(tmem, xd + 2 * kk, ad + 2 * kk, idesc, (i | kk) != 0 ? 1u : 0u);
+                    tc_commit(free_(s));
+                    if (i == n - 1) tc_commit(smem_u32(done));
                 }
-#pragma unroll
-                for (int np = 0; np < 4; ++np) {
-                    if (np >= nts) break;
-                    uint32_t a[4];
-                    const int row = (NR == 2 ? half * 64 : 0) + np * 16 + (lane & 7) + ((lane >> 4) << 3);
-                    ldmatrix4(a, as + row * 128 + (((kk * 2 + ((lane >> 3) & 1)) ^ (row & 7)) << 4));
-#pragma unroll
-                    for (int mt = 0; mt < 2; ++mt) {
-                        mma16816(acc[mt][2 * np], x[mt][0], x[mt][1], x[mt][2], x[mt][3], a[0], a[1]);
-                        mma16816(acc[mt][2 * np + 1], x[mt][0], x[mt][1], x[mt][2], x[mt][3], a[2], a[3]);
-                    }
-                }
+                __syncwarp();
+                if (++s == stages) { s = 0; ++turn; }
             }
         }
-        cp_async_wait<0>();
+        bool ok = true;
+        if (n > 0) ok = warp_wait(smem_u32(done), 0u, stop, lane);
         __syncthreads();                  // the ring is free
-        // partial sums [128 tokens][ranks]; where both halves of the warps have some of the same, the second adds to the first's
-        for (int turn = 0; turn < (NR == 2 ? 1 : 2); ++turn) {
-            if (NR == 2 || half == turn) {
+        if (*stop) { ok = false; let_copies_land(); }
+        tc_fence_after();
+        // partial sums [128 tokens][rk + 4]
+        float* part = reinterpret_cast<float*>(smem);
+        const int stride = rk + 4;
+        for (int c = (warp >> 2) * 16; c < rk; c += 32) {
+            uint32_t v[16];
 #pragma unroll
-                for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-                    for (int nt = 0; nt < 8; ++nt)
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            if (nt >= 2 * nts) continue;
-                            float2* q = reinterpret_cast<float2*>(part + (tw * 32 + mt * 16 + 8 * h + g) * C::RowFloats +
-                                                                  (NR == 2 ? half * 64 : 0) + nt * 8 + 2 * t);
-                            float2 v = make_float2(acc[mt][nt][2 * h], acc[mt][nt][2 * h + 1]);
-                            if (turn) { const float2 o = *q; v.x += o.x; v.y += o.y; }
-                            *q = v;
-                        }
+            for (int e = 0; e < 16; ++e) v[e] = 0u;
+            if (n > 0) {
+                tmem_ld16(tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)c, v);
+                tmem_wait_ld(v);
             }
-            __syncthreads();
+            uint4* q = reinterpret_cast<uint4*>(part + ((warp & 3) * 32 + lane) * stride + c);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t nan = 0x7fffffffu;
+                q[e] = ok ? make_uint4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]) : make_uint4(nan, nan, nan, nan);
+            }
         }
+        tc_fence_before();
         cluster_arrive();
         cluster_wait();
+        const int per = kTok / CL;
+        const float alpha = p.scale ? __ldg(p.scale + slot) : 1.f;
+        auto gather = [&](int row, int j) {
+            const uint32_t at = smem_u32(part + row * stride + j);
+            float4 a[kMaxCL], v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int row = rank * (kTok / kCL) + warp * 2 + i, j = lane * 4;
-            if (row >= count || j >= C::Ranks || r0 + j >= rk) continue;
-            const uint32_t at = smem_u32(part + row * C::RowFloats + j);
-            float4 a[kCL];
+            for (int q = 0; q < kMaxCL; ++q) a[q] = q < CL ? ld_cluster_f32x4(map_to_rank(at, q)) : v;
 #pragma unroll
-            for (int q = 0; q < kCL; ++q) a[q] = ld_cluster_f32x4(map_to_rank(at, q));
+            for (int q = 0; q < kMaxCL; ++q) { v.x += a[q].x; v.y += a[q].y; v.z += a[q].z; v.w += a[q].w; }
+            return v;
+        };
+        if (rk <= 64) {                   // two tokens side by side
+            for (int i = warp * 2 + (lane >> 4); i < per; i += 2 * kDownWarps) {
+                const int row = rank * per + i, j = (lane & 15) * 4;
+                const bool mine = row < count && j < rk;
+                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (mine) v = gather(row, j);
+                float top = max4_abs(v);
 #pragma unroll
-            for (int q = 0; q < kCL; ++q) { sum[pass][i].x += a[q].x; sum[pass][i].y += a[q].y; sum[pass][i].z += a[q].z; sum[pass][i].w += a[q].w; }
+                for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                const RowFactor f = row_factor(top);
+                if (mine) *reinterpret_cast<uint2*>(p.S + (size_t)(first + row) * p.r + j) = scaled_f16(v, f.up);
+                if (mine && j == 0) p.row_scale[first + row] = f.down * alpha;
+            }
+        } else {
+            for (int i = warp; i < per && rank * per + i < count; i += kDownWarps) {
+                const int row = rank * per + i;
+                float4 v[2];
+                float top = 0.f;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    v[h] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (h * 128 + lane * 4 < rk) v[h] = gather(row, h * 128 + lane * 4);
+                    top = fmaxf(top, max4_abs(v[h]));
+                }
+                const RowFactor f = row_factor(warp_max(top));
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    if (h * 128 + lane * 4 < rk)
+                        *reinterpret_cast<uint2*>(p.S + (size_t)(first + row) * p.r + h * 128 + lane * 4) = scaled_f16(v[h], f.up);
+                if (lane == 0) p.row_scale[first + row] = f.down * alpha;
+            }
         }
-        cluster_arrive();                 // nobody overwrites or leaves what a peer still reads
+        cluster_arrive();                 // nobody leaves while a peer may still read its sums
         cluster_wait();
+        tc_fence_after();
     }
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int row = rank * (kTok / kCL) + warp * 2 + i;
-        if (row >= count) continue;
-        float top = 0.f;
-#pragma unroll
-        for (int pass = 0; pass < 2; ++pass) top = fmaxf(top, max4_abs(sum[pass][i]));
-        const RowFactor f = row_factor(warp_max(top));
-#pragma unroll
-        for (int pass = 0; pass < 2; ++pass) {
-            const int j = lane * 4;
-            if (j < C::Ranks && pass * C::Ranks + j < rk)
-                *reinterpret_cast<uint2*>(p.S + (size_t)(first + row) * p.r + pass * C::Ranks + j) = scaled_f16(sum[pass][i], f.up);
-        }
-        if (lane == 0) p.row_scale[first + row] = f.down * (p.scale ? __ldg(p.scale + slot) : 1.f);
-    }
+    if (warp == 0) tmem_free(tmem, tmem_cols);
 }
 
-// y_ready: what wrote Y is known to be complete when this kernel starts (the first kernel waited for it).
-__global__ void __launch_bounds__(kThreads, 2)
-adapters_up_kernel(const AdapterParams p, int n_blocks, bool y_ready) {
-    extern __shared__ __align__(128) uint8_t smem[];
-    if (!y_ready) grid_dep_wait();
-    const int tile = (int)blockIdx.x / n_blocks, n0 = ((int)blockIdx.x % n_blocks) * kUpCols;
+// ---------------------------------------------------------------------------
+// out = Y + B S
+// ---------------------------------------------------------------------------
+constexpr int kUpWarps = 10, kUpThreads = kUpWarps * 32;      // copies, products, twice four that finish blocks in turn
+
+struct UpMaps { CUtensorMap y, y_one, s, b; };
+
+__host__ __device__ constexpr int up_chunks(int r) { return (r + 63) / 64; }          // blocks of 64 ranks
+__host__ __device__ constexpr int up_stage_bytes(int r) { return kRowsBytes + up_chunks(r) * kCols * 128; }
+// Three stages; two where that lets two CTAs share an SM.
+__host__ __device__ constexpr int up_stages(int r) { return r <= 64 || r > 128 ? 3 : 2; }
+constexpr int kUpTail = 128;
+constexpr int up_smem(int r) { return up_chunks(r) * kTok * 128 + up_stages(r) * up_stage_bytes(r) + kUpTail + 1024; }
+static_assert(2 * (up_smem(128) + 1024) <= 228 * 1024 && 2 * (up_smem(64) + 1024) <= 228 * 1024, "two CTAs to an SM");
+static_assert(up_smem(256) <= 227 * 1024, "shared memory budget");
+constexpr uint32_t kUpTmem = 2 * kCols;
+
+// Blocks of 64 channels [c n / chunks, (c + 1) n / chunks) of a tile.  What wrote Y and the plan is known to be complete when this
+// kernel starts, because the first kernel waited for it; S is waited for.
+__global__ void __launch_bounds__(kUpThreads, 2)
+adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, int chunks) {
+    extern __shared__ uint8_t smem_raw[];
+    const int tile = (int)blockIdx.x / chunks, chunk = (int)blockIdx.x - tile * chunks;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const PlanView plan = plan_view(p.plan, p.M, p.n_slots);
     const int4 head = *reinterpret_cast<const int4*>(p.plan);
     const int4 t4 = plan.tiles_many[tile];
     if (head.x != p.M || head.y != p.n_slots || tile >= head.w) return;
     const int slot = t4.x, first = t4.y, count = t4.z;
+    const int32_t* tokens = plan.tokens + first;
     const int rk = slot < 0 ? 0 : adapter_rank(p, slot);
-    if (rk == 0 && p.Y == p.out) return;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int tw = warp & 3, nh = warp >> 2;
-    const int stride = 2 * p.r + 16;          // bytes of a row in shared memory: an odd multiple of 16
-    const uint32_t ss = smem_u32(smem), bs = ss + kTok * stride;
-    const int row_chunks = rk / 8;
-    for (int i = threadIdx.x; i < kUpCols * row_chunks; i += kThreads) {
-        const int row = i / row_chunks, c = i % row_chunks;
-        if (n0 + row < p.N) cp_async16(bs + row * stride + c * 16, p.B + ((size_t)slot * p.N + n0 + row) * p.r + c * 8);
+    const int blocks = (p.N + kCols - 1) / kCols;
+    const int b0 = (int)((long long)chunk * blocks / chunks), n = (int)((long long)(chunk + 1) * blocks / chunks) - b0;
+    if (rk == 0) {                        // nothing to add
+        if (p.Y != p.out)
+            for (int row = warp; row < count; row += kUpWarps) {
+                const size_t tok = (size_t)tokens[row];
+                for (int c = b0 * kCols + lane * 8; c < (b0 + n) * kCols && c < p.N; c += 256)
+                    *reinterpret_cast<uint4*>(p.out + tok * p.ldo + c) = *reinterpret_cast<const uint4*>(p.Y + tok * p.ldy + c);
+            }
+        return;
     }
-    size_t tok[4];
-    bool ok[4];
-    uint4 y[2][4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int row = tw * 32 + 8 * i + g;
-        ok[i] = row < count;
-        tok[i] = ok[i] ? (size_t)plan.tokens[first + row] : 0;
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    const int kch = up_chunks(rk), stage_bytes = up_stage_bytes(p.r), stages = up_stages(p.r);
+    const int s_bytes = up_chunks(p.r) * kTok * 128;
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + s_bytes + stages * stage_bytes);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 11);
+    volatile int* stop = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    const uint32_t sb = smem_u32(smem), bar0 = smem_u32(bars);
+    auto filled = [&](int s) { return bar0 + 8u * s; };                 // a stage's Y and B are there
+    auto free_ = [&](int s) { return bar0 + 24u + 8u * s; };            // ... and have been read (four warps)
+    auto full = [&](int h) { return bar0 + 48u + 8u * h; };             // a block's sums are complete
+    auto read = [&](int h) { return bar0 + 64u + 8u * h; };             // ... and have been read (four warps)
+    const uint32_t s_there = bar0 + 80u;
+    if (warp == 0) {
+        tmem_alloc(tmem_slot, kUpTmem);
+    } else if (warp == 1) {
+        if (lane < 11) mbar_init(bar0 + 8u * lane, (lane >= 3 && lane < 6) || lane == 8 || lane == 9 ? 4 : 1);
+        if (lane == 0) *stop = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_proxy_async_smem();
+    } else if (warp == 2 && lane == 0) {
+        prefetch_tensormap(&maps.y);
+        prefetch_tensormap(&maps.b);
+        prefetch_tensormap(&maps.s);
     }
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-        const int n = n0 + nh * 64 + u * 32 + 8 * t;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            y[u][i] = ok[i] && n < p.N ? *reinterpret_cast<const uint4*>(p.Y + tok[i] * p.ldy + n) : make_uint4(0, 0, 0, 0);
-    }
-    float factor[4] = {0.f, 0.f, 0.f, 0.f};
-    if (rk > 0) {
-        if (y_ready) grid_dep_wait();         // S is there
-        for (int i = threadIdx.x; i < count * row_chunks; i += kThreads) {
-            const int row = i / row_chunks, c = i % row_chunks;
-            cp_async16(ss + row * stride + c * 16, p.S + (size_t)(first + row) * p.r + c * 8);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    if (warp == 0) {                      // copies
+        const TileRows rows = tile_rows(t4, plan.tokens, lane);
+        const uint32_t bytes = (uint32_t)rows.rows() * 128u + (uint32_t)kch * kCols * 128u;
+        bool asked = false;
+        for (int i = 0, s = 0, turn = 0; i < n; ++i) {
+            if (i == stages && !asked) {
+                // S, once the ring is full: its own wait is the first kernel
+                grid_dep_wait();
+                asked = true;
+                if (lane == 0) {
+                    mbar_arrive_expect_tx(s_there, (uint32_t)kch * kTok * 128u);
+                    for (int c = 0; c < kch; ++c) tma_load_2d(sb + c * kTok * 128, &maps.s, c * 64, first, s_there);
+                }
+                __syncwarp();
+            }
+            if (turn > 0 && !warp_wait(free_(s), (uint32_t)(turn - 1) & 1u, stop, lane)) break;
+            if (lane == 0) mbar_arrive_expect_tx(filled(s), bytes);
+            __syncwarp();
+            const uint32_t at = sb + (uint32_t)(s_bytes + s * stage_bytes);
+            const int ch = (b0 + i) * kCols;
+            rows.load(at, &maps.y, &maps.y_one, ch, filled(s), lane);
+            if (lane < kch) tma_load_2d(at + kRowsBytes + lane * kCols * 128, &maps.b, lane * 64, slot * p.N + ch, filled(s));
+            if (++s == stages) { s = 0; ++turn; }
         }
-        cp_async_commit();
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (ok[i]) factor[i] = p.row_scale[first + tw * 32 + 8 * i + g];
-        cp_async_wait<0>();
-        __syncthreads();
-    }
-    grid_dep_launch();
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-        const int n = n0 + nh * 64 + u * 32 + 8 * t;
-        float acc[2][4][4];
-#pragma unroll
-        for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[mt][j][e] = 0.f;
-        // a tile of 8 channels takes rows (g / 2) 8 + 2 j + g % 2 of 32: a thread's outputs are then 8 neighbours
-        const uint32_t a_at = ss + (uint32_t)((tw * 32 + (lane & 15)) * stride + (lane >> 4) * 16);
-        const int br = nh * 64 + u * 32 + ((lane & 7) >> 1) * 8 + (lane & 1) + 2 * (lane >> 4);
-        const uint32_t b_at = bs + (uint32_t)(br * stride + ((lane >> 3) & 1) * 16);
-        for (int k = 0; k < rk; k += 16) {
-            uint32_t a[2][4], b[2][4];
-#pragma unroll
-            for (int mt = 0; mt < 2; ++mt) ldmatrix4(a[mt], a_at + mt * 16 * stride + 2 * k);
-#pragma unroll
-            for (int jp = 0; jp < 2; ++jp) ldmatrix4(b[jp], b_at + jp * 4 * stride + 2 * k);
-#pragma unroll
-            for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    mma16816(acc[mt][j], a[mt][0], a[mt][1], a[mt][2], a[mt][3], b[j >> 1][2 * (j & 1)], b[j >> 1][2 * (j & 1) + 1]);
+        if (!asked) {
+            grid_dep_wait();
+            if (lane == 0) {
+                mbar_arrive_expect_tx(s_there, (uint32_t)kch * kTok * 128u);
+                for (int c = 0; c < kch; ++c) tma_load_2d(sb + c * kTok * 128, &maps.s, c * 64, first, s_there);
+            }
         }
-        if (n >= p.N) continue;
+        grid_dep_launch();
+    } else if (warp == 1) {               // products
+        const uint32_t idesc = make_idesc(1, 0, 128, kCols);
+        bool ok = warp_wait(s_there, 0u, stop, lane);
+        for (int i = 0, s = 0, turn = 0; i < n && ok; ++i) {
+            const int h = i & 1;
+            ok = warp_wait(filled(s), (uint32_t)turn & 1u, stop, lane);
+            if (ok && i >= 2) ok = warp_wait(read(h), (uint32_t)((i >> 1) - 1) & 1u, stop, lane);
+            if (!ok) break;
+            tc_fence_after();
+            if (elect_one()) {
+                const uint32_t at = sb + (uint32_t)(s_bytes + s * stage_bytes) + kRowsBytes;
+                for (int k = 0; k < rk; k += 16) {
+                    const uint64_t sd = smem_desc_sw128(sb + (k >> 6) * kTok * 128) + 2 * ((k >> 4) & 3);
+                    const uint64_t bd = smem_desc_sw128(at + (k >> 6) * kCols * 128) + 2 * ((k >> 4) & 3);
+                    mma_f16_ss(tmem + h * kCols, sd, bd, idesc, k != 0 ? 1u : 0u);
+                }
+                tc_commit(full(h));
+            }
+            __syncwarp();
+            if (++s == stages) { s = 0; ++turn; }
+        }
+    } else {
+        const int q = warp & 3, h = (warp - 2) >> 2;      // a quarter of the tokens (of tensor memory's lanes), every other block
+        const int row = q * 32 + lane;
+        grid_dep_wait();                  // the factors come from the first kernel
+        const float factor = row < count ? p.row_scale[first + row] : 0.f;
+        // lines are written by eight lanes each: this lane's 16 bytes of rows q 32 + lane / 8, + 4, ...
+        const int wr = q * 32 + (lane >> 3), wc = lane & 7;
+        size_t out_row[8];
+        uint32_t there = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (ok[i])
-                *reinterpret_cast<uint4*>(p.out + tok[i] * p.ldo + n) =
-                    rk == 0 ? y[u][i] : add_scaled(y[u][i], acc[i >> 1], i & 1, factor[i]);
+        for (int e = 0; e < 8; ++e) {
+            out_row[e] = wr + 4 * e < count ? (size_t)tokens[wr + 4 * e] * p.ldo + wc * 8 : 0;
+            there |= wr + 4 * e < count ? 1u << e : 0u;
+        }
+        bool ok = true;
+        for (int i = h; i < n; i += 2) {
+            const int s = i % stages;
+            const uint32_t at = sb + (uint32_t)(s_bytes + s * stage_bytes);
+            if (ok) ok = warp_wait(filled(s), (uint32_t)(i / stages) & 1u, stop, lane);
+            if (ok) ok = warp_wait(full(h), (uint32_t)(i >> 1) & 1u, stop, lane);
+            if (ok) {
+                tc_fence_after();
+#pragma unroll
+                for (int c0 = 0; c0 < kCols; c0 += 32) {
+                    uint32_t v[2][16];
+                    tmem_ld16(tmem + h * kCols + ((uint32_t)(q * 32) << 16) + c0, v[0]);
+                    tmem_ld16(tmem + h * kCols + ((uint32_t)(q * 32) << 16) + c0 + 16, v[1]);
+                    tmem_wait_ld_all();
+                    tmem_use(v[0]);
+                    tmem_use(v[1]);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const uint32_t place = at + (uint32_t)(row * 128 + (((c0 / 8 + c) ^ (row & 7)) << 4));
+                        uint32_t y[4];
+                        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(y[0]), "=r"(y[1]), "=r"(y[2]), "=r"(y[3]) : "r"(place));
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&y[e]));
+                            const int j = (c & 1) * 8 + 2 * e;
+                            const __half2 o = __floats2half2_rn(fmaf(__uint_as_float(v[c >> 1][j]), factor, f.x),
+                                                                fmaf(__uint_as_float(v[c >> 1][j + 1]), factor, f.y));
+                            y[e] = *reinterpret_cast<const uint32_t*>(&o);
+                        }
+                        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(place), "r"(y[0]), "r"(y[1]), "r"(y[2]), "r"(y[3]) : "memory");
+                    }
+                }
+                tc_fence_before();
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(read(h));
+            const int ch = (b0 + i) * kCols;
+            const bool in = ch + wc * 8 < p.N;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                uint32_t o[4];
+                const int r = wr + 4 * e;
+                asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(o[0]), "=r"(o[1]), "=r"(o[2]), "=r"(o[3])
+                             : "r"(at + (uint32_t)(r * 128 + ((wc ^ (r & 7)) << 4))) : "memory");
+                if (!ok) o[0] = o[1] = o[2] = o[3] = 0x7fff7fffu;
+                if (in && (there >> e & 1)) *reinterpret_cast<uint4*>(p.out + out_row[e] + ch) = make_uint4(o[0], o[1], o[2], o[3]);
+            }
+            fence_proxy_async_smem();     // the next copy into this place comes after these reads and writes
+            __syncwarp();
+            if (lane == 0) mbar_arrive(free_(s));
+        }
     }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (*stop) let_copies_land();
+    if (warp == 0) tmem_free(tmem, kUpTmem);
 }
 
-template <int NR>
-int launch_down(const AdapterParams& p, int tiles, cudaStream_t st) {
-    static bool configured[kMaxDevices] = {false};
+// Tiles that a call probably has: half of the adapters leave a short one.
+int likely_tiles(const AdapterParams& p) { return p.M / kTok + ((p.n_slots < p.M ? p.n_slots : p.M) + 1) / 2; }
+
+template <typename Kernel>
+int opt_in(Kernel* kernel, int bytes, bool (&configured)[kMaxDevices], int* num_sms) {
     int dev = 0;
-    const int rc = current_device(&dev);
+    int rc = current_device(&dev);
+    if (rc == ASER_OK) rc = device_sm_count(num_sms);
+    if (rc != ASER_OK || configured[dev]) return rc;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != cudaSuccess) return record_cuda_error(e, "adapters smem attribute");
+    configured[dev] = true;
+    return ASER_OK;
+}
+
+constexpr int max_of(int a, int b) { return a > b ? a : b; }
+
+}  // namespace
+
+int launch_adapters_down(const AdapterParams& p, cudaStream_t st) {
+    static bool configured[kMaxDevices] = {false};
+    int num_sms = 0;
+    int rc = opt_in(adapters_down_kernel, max_of(down_smem(128), down_smem(256)), configured, &num_sms);
     if (rc != ASER_OK) return rc;
-    if (!configured[dev]) {
-        const cudaError_t e = cudaFuncSetAttribute(adapters_down_kernel<NR>, cudaFuncAttributeMaxDynamicSharedMemorySize, DownCfg<NR>::Smem);
-        if (e != cudaSuccess) return record_cuda_error(e, "adapters_down smem attribute");
-        configured[dev] = true;
-    }
+    DownMaps maps;
+    const CUtensorMapDataType f16 = CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    rc = encode_map_2d_ld(&maps.x, f16, 2, p.X, p.M, p.K, p.ldx, kBox, kCols, CU_TENSOR_MAP_SWIZZLE_128B);
+    if (rc == ASER_OK) rc = encode_map_2d_ld(&maps.x_one, f16, 2, p.X, p.M, p.K, p.ldx, 1, kCols, CU_TENSOR_MAP_SWIZZLE_128B);
+    if (rc == ASER_OK) rc = encode_map_2d(&maps.a, f16, 2, p.A, (uint64_t)p.n_slots * p.r, p.K, 16, kCols, CU_TENSOR_MAP_SWIZZLE_128B);
+    if (rc != ASER_OK) return rc;
+    // as large a share of the SMs as the tiles can be split over; a CTA has two steps of K at least
+    int CL = kMaxCL;
+    while (CL > 1 && (likely_tiles(p) * CL > num_sms + num_sms / 8 || p.K / kCols < 2 * CL)) CL /= 2;
+    uint32_t cols = 32;
+    while ((int)cols < p.r) cols *= 2;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(tiles * kCL, 1, 1);
-    cfg.blockDim = dim3(kThreads, 1, 1);
-    cfg.dynamicSmemBytes = DownCfg<NR>::Smem;
+    cfg.gridDim = dim3(plan_tiles(p.M, p.n_slots, kTok) * CL, 1, 1);
+    cfg.blockDim = dim3(kDownThreads, 1, 1);
+    cfg.dynamicSmemBytes = down_smem(p.r);
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = kCL; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    attr[1].val.clusterDim.x = CL; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, adapters_down_kernel<NR>, p);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, adapters_down_kernel, maps, p, cols);
     if (e != cudaSuccess) return record_cuda_error(e, "adapters_down_kernel");
     return check_launch("adapters_down_kernel");
 }
 
-}  // namespace
-
-int launch_adapters_down(const AdapterParams& p, cudaStream_t st) {
-    const int tiles = plan_tiles(p.M, p.n_slots, kTileMany);
-    return p.r <= 64 ? launch_down<1>(p, tiles, st) : launch_down<2>(p, tiles, st);
-}
-
-int launch_adapters_up(const AdapterParams& p, bool y_ready, cudaStream_t st) {
+int launch_adapters_up(const AdapterParams& p, cudaStream_t st) {
     static bool configured[kMaxDevices] = {false};
-    int dev = 0;
-    const int rc = current_device(&dev);
+    int num_sms = 0;
+    int rc = opt_in(adapters_up_kernel, up_smem(256), configured, &num_sms);
     if (rc != ASER_OK) return rc;
-    const int tiles = plan_tiles(p.M, p.n_slots, kTileMany), blocks = (p.N + kUpCols - 1) / kUpCols;
-    auto smem = [](int r) { return (kTok + kUpCols) * (2 * r + 16); };
-    if (!configured[dev]) {
-        const cudaError_t e = cudaFuncSetAttribute(adapters_up_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem(256));
-        if (e != cudaSuccess) return record_cuda_error(e, "adapters_up smem attribute");
-        configured[dev] = true;
-    }
+    UpMaps maps;
+    const CUtensorMapDataType f16 = CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    rc = encode_map_2d_ld(&maps.y, f16, 2, p.Y, p.M, p.N, p.ldy, kBox, kCols, CU_TENSOR_MAP_SWIZZLE_128B);
+    if (rc == ASER_OK) rc = encode_map_2d_ld(&maps.y_one, f16, 2, p.Y, p.M, p.N, p.ldy, 1, kCols, CU_TENSOR_MAP_SWIZZLE_128B);
+    if (rc == ASER_OK) rc = encode_map_2d(&maps.s, f16, 2, p.S, p.M, p.r, kTok, 64, CU_TENSOR_MAP_SWIZZLE_128B);
+    if (rc == ASER_OK) rc = encode_map_2d(&maps.b, f16, 2, p.B, (uint64_t)p.n_slots * p.N, p.r, kCols, 64, CU_TENSOR_MAP_SWIZZLE_128B);
+    if (rc != ASER_OK) return rc;
+    // as many CTAs as are resident at once, if every one has two blocks and more
+    const int resident = (p.r <= 128 ? 2 : 1) * num_sms, blocks = (p.N + kCols - 1) / kCols;
+    int chunks = resident / likely_tiles(p);
+    if (chunks > (blocks + 1) / 2) chunks = (blocks + 1) / 2;
+    if (chunks < 1) chunks = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(tiles * blocks, 1, 1);
-    cfg.blockDim = dim3(kThreads, 1, 1);
-    cfg.dynamicSmemBytes = smem(p.r);
+    cfg.gridDim = dim3(plan_tiles(p.M, p.n_slots, kTok) * chunks, 1, 1);
+    cfg.blockDim = dim3(kUpThreads, 1, 1);
+    cfg.dynamicSmemBytes = up_smem(p.r);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, adapters_up_kernel, p, blocks, y_ready);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, adapters_up_kernel, maps, p, chunks);
     if (e != cudaSuccess) return record_cuda_error(e, "adapters_up_kernel");
     return check_launch("adapters_up_kernel");
 }

@@ -175,6 +175,7 @@ int adapters_check(const void* X_f16, int ldx, const void* A_f16, const void* B_
                    const void* out_f16, int ldo, const void* workspace, size_t workspace_bytes) {
     if (!shape_ok(M, N, K, r) || M > kMaxAdapterTokens) return fail(ASER_ERR_SHAPE, "unsupported M, N, K or r");
     if (n_slots < 1 || n_slots > kMaxSlots) return fail(ASER_ERR_SHAPE, "n_slots must be 1..4096");
+    if ((long long)n_slots * N > 0x7fffffffll) return fail(ASER_ERR_SHAPE, "n_slots * N beyond the kernels' 31-bit row numbers");
     if (ldx < K || ldy < N || ldo < N || (ldx | ldy | ldo) % 8 != 0)
         return fail(ASER_ERR_SHAPE, "rows must be multiples of 8 elements apart and at least as far as they are long");
     if (M == 0 || N == 0) return ASER_OK;

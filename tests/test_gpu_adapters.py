@@ -201,9 +201,11 @@ def test_plan(aser, M, slots):
     assert head[:2] == [M, slots] and tokens == want
     for size, ts in zip((16, 128), tiles):
         at = 0
-        for a, first, count, _, *own in ts:
+        for a, first, count, run, *own in ts:
             assert first == at and 1 <= count <= size and all(s[m] == a for m in tokens[first:first + count])
             assert not own or own[:count] == tokens[first:first + count]
+            mine = tokens[first:first + count]
+            assert own or run == (mine[0] if mine == list(range(mine[0], mine[0] + count)) else -1)
             at += count
         assert at == M
 

@@ -68,6 +68,7 @@ def test_adapters_are_refused(lib):
     assert call(M=0, X=None, plan=None, nbytes=0) == OK and call(N=0, Y=None) == OK
     assert call(K=200) == SHAPE and call(N=60) == SHAPE and call(r=24) == SHAPE and call(r=272) == SHAPE and call(M=-1) == SHAPE
     assert call(M=(1 << 24) + 1) == SHAPE and call(S=0) == SHAPE and call(S=4097) == SHAPE
+    assert call(N=1 << 20, S=2048) == SHAPE
     assert call(ldx=128) == SHAPE and call(ldx=260) == SHAPE and call(ldy=68, ldo=68) == SHAPE and call(ldo=56) == SHAPE
     assert call(ldy=128) == SHAPE                   # in place, rows of one matrix
     assert call(X=None) == NULL and call(A=None) == NULL and call(B=None) == NULL and call(plan=None) == NULL
