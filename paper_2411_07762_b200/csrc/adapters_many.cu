@@ -24,7 +24,7 @@ namespace {
 constexpr int kTok = kTileMany, kMaxCL = 8, kBox = 32;
 constexpr int kCols = 64;                            // columns or channels of a stage: 128 bytes a row
 constexpr int kRowsBytes = kTok * kCols * 2;
-constexpr int kMaxStages = 6;
+constexpr int kMaxStages = 8;
 constexpr long long kWaitClocks = 400000000ll;       // about 0.2 s of SM clocks per wait
 
 // False after the limit, or when another warp of this CTA gave up.
@@ -95,13 +95,15 @@ constexpr int kDownThreads = 256, kDownWarps = 8;
 struct DownMaps { CUtensorMap x, x_one, a; };
 
 __host__ __device__ constexpr int down_stage_bytes(int r) { return kRowsBytes + r * kCols * 2; }
-// The ring also holds the partial sums at the end, [128][rank + 4] floats; up to 200 KB of it.
-__host__ __device__ constexpr int down_stages(int r) { return r <= 128 ? 6 : 4; }
+// The ring also holds the partial sums at the end, [128][rank + 4] floats.  Up to rank 128 two CTAs share an SM (one's set-up
+// and exchange beside the other's copies; and clusters of four do not fill the part at one CTA an SM).
+__host__ __device__ constexpr int down_stages(int r) { return r <= 64 ? 4 : r <= 128 ? 3 : 4; }
 constexpr int kDownTail = kMaxStages * 16 + 32;      // barriers, tensor memory's address, flag
 constexpr int down_smem(int r) { return down_stages(r) * down_stage_bytes(r) + kDownTail + 1024; }
-static_assert(down_smem(128) <= 227 * 1024 && down_smem(256) <= 227 * 1024, "shared memory budget");
+static_assert(2 * (down_smem(64) + 1024) <= 228 * 1024 && 2 * (down_smem(128) + 1024) <= 228 * 1024, "two CTAs to an SM");
+static_assert(down_smem(256) <= 227 * 1024, "shared memory budget");
 
-__global__ void __launch_bounds__(kDownThreads, 1)
+__global__ void __launch_bounds__(kDownThreads, 2)
 adapters_down_kernel(const __grid_constant__ DownMaps maps, const AdapterParams p, uint32_t tmem_cols) {
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -253,13 +255,12 @@ constexpr int kUpWarps = 10, kUpThreads = kUpWarps * 32;      // copies, product
 struct UpMaps { CUtensorMap y, y_one, s, b; };
 
 __host__ __device__ constexpr int up_chunks(int r) { return (r + 63) / 64; }          // blocks of 64 ranks
-__host__ __device__ constexpr int up_stage_bytes(int r) { return kRowsBytes + up_chunks(r) * kCols * 128; }
-// Three stages; two where that lets two CTAs share an SM.
-__host__ __device__ constexpr int up_stages(int r) { return r <= 64 || r > 128 ? 3 : 2; }
-constexpr int kUpTail = 128;
-constexpr int up_smem(int r) { return up_chunks(r) * kTok * 128 + up_stages(r) * up_stage_bytes(r) + kUpTail + 1024; }
-static_assert(2 * (up_smem(128) + 1024) <= 228 * 1024 && 2 * (up_smem(64) + 1024) <= 228 * 1024, "two CTAs to an SM");
-static_assert(up_smem(256) <= 227 * 1024, "shared memory budget");
+// Shared memory of a CTA: S, then as many stages as there is room for; they are as large as the tile's tokens and the adapter's
+// rank ask (128 tokens of rank 64: four, 64 tokens: six).  Up to rank 128 two CTAs share an SM.
+constexpr int kUpTail = 256;
+__host__ __device__ constexpr int up_smem(int r) { return (r <= 128 ? 112 : 224) * 1024; }
+static_assert(up_smem(128) - kUpTail - 1024 >= up_chunks(128) * kTok * 128 + 2 * (kRowsBytes + up_chunks(128) * kCols * 128), "two stages at least");
+static_assert(up_smem(256) - kUpTail - 1024 >= up_chunks(256) * kTok * 128 + 2 * (kRowsBytes + up_chunks(256) * kCols * 128), "two stages at least");
 constexpr uint32_t kUpTmem = 2 * kCols;
 
 // Blocks of 64 channels [c n / chunks, (c + 1) n / chunks) of a tile.  What wrote Y and the plan is known to be complete when this
@@ -288,21 +289,23 @@ adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, i
         return;
     }
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    const int kch = up_chunks(rk), stage_bytes = up_stage_bytes(p.r), stages = up_stages(p.r);
-    const int s_bytes = up_chunks(p.r) * kTok * 128;
-    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + s_bytes + stages * stage_bytes);
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 11);
+    // (the products read S as 128 rows: behind the tile's tokens whatever lies there, sums that nobody reads)
+    const int kch = up_chunks(rk), row_bytes = (count + kBox - 1) / kBox * kBox * 128, s_bytes = (kch - 1) * row_bytes + kTok * 128;
+    const int stage_bytes = row_bytes + kch * kCols * 128, room = up_smem(p.r) - kUpTail - 1024;
+    const int fit = (room - s_bytes) / stage_bytes, stages = fit < kMaxStages ? fit : kMaxStages;
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + room);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * kMaxStages + 5);
     volatile int* stop = reinterpret_cast<volatile int*>(tmem_slot + 1);
     const uint32_t sb = smem_u32(smem), bar0 = smem_u32(bars);
     auto filled = [&](int s) { return bar0 + 8u * s; };                 // a stage's Y and B are there
-    auto free_ = [&](int s) { return bar0 + 24u + 8u * s; };            // ... and have been read (four warps)
-    auto full = [&](int h) { return bar0 + 48u + 8u * h; };             // a block's sums are complete
-    auto read = [&](int h) { return bar0 + 64u + 8u * h; };             // ... and have been read (four warps)
-    const uint32_t s_there = bar0 + 80u;
+    auto free_ = [&](int s) { return bar0 + 8u * (kMaxStages + s); };   // ... and have been read (four warps)
+    auto read = [&](int h) { return bar0 + 8u * (2 * kMaxStages + h); };        // a block's sums have been read (four warps)
+    auto full = [&](int h) { return bar0 + 8u * (2 * kMaxStages + 2 + h); };    // ... are complete
+    const uint32_t s_there = bar0 + 8u * (2 * kMaxStages + 4);
     if (warp == 0) {
         tmem_alloc(tmem_slot, kUpTmem);
     } else if (warp == 1) {
-        if (lane < 11) mbar_init(bar0 + 8u * lane, (lane >= 3 && lane < 6) || lane == 8 || lane == 9 ? 4 : 1);
+        if (lane < 2 * kMaxStages + 5) mbar_init(bar0 + 8u * lane, lane >= kMaxStages && lane < 2 * kMaxStages + 2 ? 4 : 1);
         if (lane == 0) *stop = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_proxy_async_smem();
@@ -319,33 +322,26 @@ adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, i
         const TileRows rows = tile_rows(t4, plan.tokens, lane);
         const uint32_t bytes = (uint32_t)rows.rows() * 128u + (uint32_t)kch * kCols * 128u;
         bool asked = false;
+        auto ask_for_s = [&]() {          // once the ring is full: this waits for the first kernel
+            asked = true;
+            grid_dep_wait();
+            if (lane == 0) mbar_arrive_expect_tx(s_there, (uint32_t)(kch * row_bytes));
+            __syncwarp();
+            const int boxes = row_bytes / (kBox * 128);
+            if (lane < kch * boxes) tma_load_2d(sb + lane * kBox * 128, &maps.s, lane / boxes * 64, first + lane % boxes * kBox, s_there);
+        };
         for (int i = 0, s = 0, turn = 0; i < n; ++i) {
-            if (i == stages && !asked) {
-                // S, once the ring is full: its own wait is the first kernel
-                grid_dep_wait();
-                asked = true;
-                if (lane == 0) {
-                    mbar_arrive_expect_tx(s_there, (uint32_t)kch * kTok * 128u);
-                    for (int c = 0; c < kch; ++c) tma_load_2d(sb + c * kTok * 128, &maps.s, c * 64, first, s_there);
-                }
-                __syncwarp();
-            }
+            if (i == stages) ask_for_s();
             if (turn > 0 && !warp_wait(free_(s), (uint32_t)(turn - 1) & 1u, stop, lane)) break;
             if (lane == 0) mbar_arrive_expect_tx(filled(s), bytes);
             __syncwarp();
             const uint32_t at = sb + (uint32_t)(s_bytes + s * stage_bytes);
             const int ch = (b0 + i) * kCols;
             rows.load(at, &maps.y, &maps.y_one, ch, filled(s), lane);
-            if (lane < kch) tma_load_2d(at + kRowsBytes + lane * kCols * 128, &maps.b, lane * 64, slot * p.N + ch, filled(s));
+            if (lane < kch) tma_load_2d(at + row_bytes + lane * kCols * 128, &maps.b, lane * 64, slot * p.N + ch, filled(s));
             if (++s == stages) { s = 0; ++turn; }
         }
-        if (!asked) {
-            grid_dep_wait();
-            if (lane == 0) {
-                mbar_arrive_expect_tx(s_there, (uint32_t)kch * kTok * 128u);
-                for (int c = 0; c < kch; ++c) tma_load_2d(sb + c * kTok * 128, &maps.s, c * 64, first, s_there);
-            }
-        }
+        if (!asked) ask_for_s();
         grid_dep_launch();
     } else if (warp == 1) {               // products
         const uint32_t idesc = make_idesc(1, 0, 128, kCols);
@@ -357,9 +353,9 @@ adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, i
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
-                const uint32_t at = sb + (uint32_t)(s_bytes + s * stage_bytes) + kRowsBytes;
+                const uint32_t at = sb + (uint32_t)(s_bytes + s * stage_bytes) + row_bytes;
                 for (int k = 0; k < rk; k += 16) {
-                    const uint64_t sd = smem_desc_sw128(sb + (k >> 6) * kTok * 128) + 2 * ((k >> 4) & 3);
+                    const uint64_t sd = smem_desc_sw128(sb + (k >> 6) * row_bytes) + 2 * ((k >> 4) & 3);
                     const uint64_t bd = smem_desc_sw128(at + (k >> 6) * kCols * 128) + 2 * ((k >> 4) & 3);
                     mma_f16_ss(tmem + h * kCols, sd, bd, idesc, k != 0 ? 1u : 0u);
                 }
@@ -400,6 +396,7 @@ adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, i
                     tmem_use(v[1]);
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
+                        if (row >= count) break;
                         const uint32_t place = at + (uint32_t)(row * 128 + (((c0 / 8 + c) ^ (row & 7)) << 4));
                         uint32_t y[4];
                         asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(y[0]), "=r"(y[1]), "=r"(y[2]), "=r"(y[3]) : "r"(place));
@@ -422,12 +419,13 @@ adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, i
             const bool in = ch + wc * 8 < p.N;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
+                if (!in || !(there >> e & 1)) continue;
                 uint32_t o[4];
                 const int r = wr + 4 * e;
                 asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(o[0]), "=r"(o[1]), "=r"(o[2]), "=r"(o[3])
                              : "r"(at + (uint32_t)(r * 128 + ((wc ^ (r & 7)) << 4))) : "memory");
                 if (!ok) o[0] = o[1] = o[2] = o[3] = 0x7fff7fffu;
-                if (in && (there >> e & 1)) *reinterpret_cast<uint4*>(p.out + out_row[e] + ch) = make_uint4(o[0], o[1], o[2], o[3]);
+                *reinterpret_cast<uint4*>(p.out + out_row[e] + ch) = make_uint4(o[0], o[1], o[2], o[3]);
             }
             fence_proxy_async_smem();     // the next copy into this place comes after these reads and writes
             __syncwarp();
@@ -457,14 +455,12 @@ int opt_in(Kernel* kernel, int bytes, bool (&configured)[kMaxDevices], int* num_
     return ASER_OK;
 }
 
-constexpr int max_of(int a, int b) { return a > b ? a : b; }
-
 }  // namespace
 
 int launch_adapters_down(const AdapterParams& p, cudaStream_t st) {
     static bool configured[kMaxDevices] = {false};
     int num_sms = 0;
-    int rc = opt_in(adapters_down_kernel, max_of(down_smem(128), down_smem(256)), configured, &num_sms);
+    int rc = opt_in(adapters_down_kernel, down_smem(256), configured, &num_sms);
     if (rc != ASER_OK) return rc;
     DownMaps maps;
     const CUtensorMapDataType f16 = CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
@@ -503,7 +499,7 @@ int launch_adapters_up(const AdapterParams& p, cudaStream_t st) {
     const CUtensorMapDataType f16 = CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
     rc = encode_map_2d_ld(&maps.y, f16, 2, p.Y, p.M, p.N, p.ldy, kBox, kCols, CU_TENSOR_MAP_SWIZZLE_128B);
     if (rc == ASER_OK) rc = encode_map_2d_ld(&maps.y_one, f16, 2, p.Y, p.M, p.N, p.ldy, 1, kCols, CU_TENSOR_MAP_SWIZZLE_128B);
-    if (rc == ASER_OK) rc = encode_map_2d(&maps.s, f16, 2, p.S, p.M, p.r, kTok, 64, CU_TENSOR_MAP_SWIZZLE_128B);
+    if (rc == ASER_OK) rc = encode_map_2d(&maps.s, f16, 2, p.S, p.M, p.r, kBox, 64, CU_TENSOR_MAP_SWIZZLE_128B);
     if (rc == ASER_OK) rc = encode_map_2d(&maps.b, f16, 2, p.B, (uint64_t)p.n_slots * p.N, p.r, kCols, 64, CU_TENSOR_MAP_SWIZZLE_128B);
     if (rc != ASER_OK) return rc;
     // as many CTAs as are resident at once, if every one has two blocks and more
