@@ -67,6 +67,7 @@ adapters_few_kernel(const AdapterParams p) {
     grid_dep_wait();
     grid_dep_launch();
     extern __shared__ __align__(128) uint8_t smem[];
+    warm_ranks(p);
     const int rank = (int)cluster_rank(), cluster = (int)(blockIdx.x / kCL), tile = cluster / p.parts, part = cluster - tile * p.parts;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const PlanView plan = plan_view(p.plan, p.M, p.n_slots);
@@ -97,7 +98,8 @@ adapters_few_kernel(const AdapterParams p) {
         }
         return;
     }
-    cluster_arrive();           // (waited for before anything is sent: every CTA of the cluster runs by then)
+    // (waited for before anything is sent: every CTA of the cluster runs by then; relaxed, because a release waits for the loads)
+    cluster_arrive_relaxed();
     float* red = reinterpret_cast<float*>(smem);                             // [warp][16][kRedStride]
     float* sums = red + kWarps * kTok * kRedStride;                          // up to 64 ranks: [CTA][16][64], received; else [16][r]
     uint8_t* s16 = reinterpret_cast<uint8_t*>(sums) + kSumBytes;             // [16][s_stride(r)]

@@ -72,6 +72,15 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+// Which adapter a tile has is known one round trip later than where its rank stands: the whole list is asked for meanwhile (a
+// thread per 32 bytes), so that the look-up finds it near.
+__device__ __forceinline__ void warm_ranks(const AdapterParams& p) {
+    const int i = (int)threadIdx.x * 8;
+    int v;
+    if (p.ranks && i < p.n_slots) asm volatile("ld.global.nc.s32 %0, [%1];" : "=r"(v) : "l"(p.ranks + i));
+    float f;
+    if (p.scale && i < p.n_slots) asm volatile("ld.global.nc.f32 %0, [%1];" : "=f"(f) : "l"(p.scale + i));
+}
 // The rank of an adapter: a multiple of 16 from 0 to r.
 __device__ __forceinline__ int adapter_rank(const AdapterParams& p, int slot) {
     const int rk = p.ranks ? __ldg(p.ranks + slot) : p.r;

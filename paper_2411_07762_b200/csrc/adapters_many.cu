@@ -95,19 +95,25 @@ constexpr int kDownThreads = 256, kDownWarps = 8;
 struct DownMaps { CUtensorMap x, x_one, a; };
 
 __host__ __device__ constexpr int down_stage_bytes(int r) { return kRowsBytes + r * kCols * 2; }
-// The ring also holds the partial sums at the end, [128][rank + 4] floats.  Up to rank 128 two CTAs share an SM (one's set-up
-// and exchange beside the other's copies; and clusters of four do not fill the part at one CTA an SM).
-__host__ __device__ constexpr int down_stages(int r) { return r <= 64 ? 4 : r <= 128 ? 3 : 4; }
-constexpr int kDownTail = kMaxStages * 16 + 32;      // barriers, tensor memory's address, flag
-constexpr int down_smem(int r) { return down_stages(r) * down_stage_bytes(r) + kDownTail + 1024; }
-static_assert(2 * (down_smem(64) + 1024) <= 228 * 1024 && 2 * (down_smem(128) + 1024) <= 228 * 1024, "two CTAs to an SM");
-static_assert(down_smem(256) <= 227 * 1024, "shared memory budget");
+// The ring also holds the partial sums at the end, [128][rank + 4] floats.  Few CTAs have an SM each and the deeper ring; above
+// that two share one (one's set-up and exchange beside the other's copies), up to rank 128.
+constexpr int kDownTail = 2 * kMaxStages * 8 + 32;   // barriers, tensor memory's address, flag
+constexpr int down_stages(int r, bool alone) {
+    const int fit = ((alone || r > 128 ? 224 : 112) * 1024 - kDownTail - 1024) / down_stage_bytes(r);
+    return fit < kMaxStages ? fit : kMaxStages;
+}
+constexpr int down_smem(int r, bool alone) {         // (more than half of an SM's, where a CTA is to be alone)
+    const int bytes = down_stages(r, alone) * down_stage_bytes(r) + kDownTail + 1024;
+    return alone && bytes < 120 * 1024 ? 120 * 1024 : bytes;
+}
+static_assert(down_stages(128, false) >= 3 && down_stages(256, true) >= 4, "a ring");
+static_assert(2 * (down_smem(64, false) + 1024) <= 228 * 1024 && 2 * (down_smem(128, false) + 1024) <= 228 * 1024, "two CTAs to an SM");
 
 __global__ void __launch_bounds__(kDownThreads, 2)
-adapters_down_kernel(const __grid_constant__ DownMaps maps, const AdapterParams p, uint32_t tmem_cols) {
+adapters_down_kernel(const __grid_constant__ DownMaps maps, const AdapterParams p, int stages, uint32_t tmem_cols) {
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    const int stage_bytes = down_stage_bytes(p.r), stages = down_stages(p.r);
+    const int stage_bytes = down_stage_bytes(p.r);
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + stages * stage_bytes);       // [stage]: filled, free
     uint64_t* done = bars + 2 * kMaxStages;                                          // all products are complete
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 1);
@@ -132,6 +138,7 @@ adapters_down_kernel(const __grid_constant__ DownMaps maps, const AdapterParams 
     auto free_ = [&](int s) { return bar0 + 16u * s + 8u; };
     grid_dep_wait();
     grid_dep_launch();
+    warm_ranks(p);
     const int CL = (int)cluster_size(), rank = (int)cluster_rank(), tile = (int)blockIdx.x / CL;
     const PlanView plan = plan_view(p.plan, p.M, p.n_slots);
     const int4 head = *reinterpret_cast<const int4*>(p.plan);
@@ -270,6 +277,7 @@ adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, i
     extern __shared__ uint8_t smem_raw[];
     const int tile = (int)blockIdx.x / chunks, chunk = (int)blockIdx.x - tile * chunks;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    warm_ranks(p);
     const PlanView plan = plan_view(p.plan, p.M, p.n_slots);
     const int4 head = *reinterpret_cast<const int4*>(p.plan);
     const int4 t4 = plan.tiles_many[tile];
@@ -417,19 +425,22 @@ adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, i
             if (lane == 0) mbar_arrive(read(h));
             const int ch = (b0 + i) * kCols;
             const bool in = ch + wc * 8 < p.N;
+            uint4 o[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                if (!in || !(there >> e & 1)) continue;
-                uint32_t o[4];
+                if (!(there >> e & 1)) continue;
                 const int r = wr + 4 * e;
-                asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(o[0]), "=r"(o[1]), "=r"(o[2]), "=r"(o[3])
+                asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(o[e].x), "=r"(o[e].y), "=r"(o[e].z), "=r"(o[e].w)
                              : "r"(at + (uint32_t)(r * 128 + ((wc ^ (r & 7)) << 4))) : "memory");
-                if (!ok) o[0] = o[1] = o[2] = o[3] = 0x7fff7fffu;
-                *reinterpret_cast<uint4*>(p.out + out_row[e] + ch) = make_uint4(o[0], o[1], o[2], o[3]);
             }
             fence_proxy_async_smem();     // the next copy into this place comes after these reads and writes
             __syncwarp();
             if (lane == 0) mbar_arrive(free_(s));
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if (!ok) o[e] = make_uint4(0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu);
+                if (in && (there >> e & 1)) *reinterpret_cast<uint4*>(p.out + out_row[e] + ch) = o[e];
+            }
         }
     }
     __syncwarp();
@@ -460,7 +471,7 @@ int opt_in(Kernel* kernel, int bytes, bool (&configured)[kMaxDevices], int* num_
 int launch_adapters_down(const AdapterParams& p, cudaStream_t st) {
     static bool configured[kMaxDevices] = {false};
     int num_sms = 0;
-    int rc = opt_in(adapters_down_kernel, down_smem(256), configured, &num_sms);
+    int rc = opt_in(adapters_down_kernel, 224 * 1024, configured, &num_sms);
     if (rc != ASER_OK) return rc;
     DownMaps maps;
     const CUtensorMapDataType f16 = CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
@@ -470,13 +481,14 @@ int launch_adapters_down(const AdapterParams& p, cudaStream_t st) {
     if (rc != ASER_OK) return rc;
     // as large a share of the SMs as the tiles can be split over; a CTA has two steps of K at least
     int CL = kMaxCL;
-    while (CL > 1 && (likely_tiles(p) * CL > num_sms + num_sms / 8 || p.K / kCols < 2 * CL)) CL /= 2;
+    while (CL > 1 && (likely_tiles(p) * CL > 2 * num_sms + num_sms / 8 || p.K / kCols < 2 * CL)) CL /= 2;
+    const bool alone = likely_tiles(p) * CL <= num_sms + num_sms / 8;
     uint32_t cols = 32;
     while ((int)cols < p.r) cols *= 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(plan_tiles(p.M, p.n_slots, kTok) * CL, 1, 1);
     cfg.blockDim = dim3(kDownThreads, 1, 1);
-    cfg.dynamicSmemBytes = down_smem(p.r);
+    cfg.dynamicSmemBytes = down_smem(p.r, alone);
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -485,7 +497,7 @@ int launch_adapters_down(const AdapterParams& p, cudaStream_t st) {
     attr[1].val.clusterDim.x = CL; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, adapters_down_kernel, maps, p, cols);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, adapters_down_kernel, maps, p, down_stages(p.r, alone), cols);
     if (e != cudaSuccess) return record_cuda_error(e, "adapters_down_kernel");
     return check_launch("adapters_down_kernel");
 }

@@ -167,6 +167,7 @@ __device__ __forceinline__ uint32_t cluster_size() {
     return n;
 }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 // Loads from the shared memory of any CTA of the cluster (address from map_to_rank).
 __device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
