@@ -311,6 +311,8 @@ adapters_plan_kernel(const int32_t* __restrict__ slot, int M, int n_slots, int32
         many = at.z + mine.z;
         *reinterpret_cast<int4*>(out) = make_int4(M, n_slots, few, many);
     }
+    // (the last group is that of the tokens without an adapter)
+    if (g0 < groups && g1 == groups) *reinterpret_cast<int4*>(out + 4) = make_int4(at.z + mine.z - tiles_of(cursor[groups - 1], kTileMany), 0, 0, 0);
     for (int i = g0; i < g1; ++i) {
         const int n = cursor[i], s = i < n_slots ? i : -1;
         for (int k = 0; k < n; k += kTileFew) *reinterpret_cast<int4*>(plan.tiles_few + (size_t)kFewWords * at.y++) = make_int4(s, at.x + k, min(kTileFew, n - k), 0);

@@ -1,5 +1,5 @@
 // The plan of a batch's adapters (adapters.cu): tokens by adapter, cut into tiles of one adapter each.
-//   words 0 .. 3   M, n_slots, tiles of kTileFew tokens, tiles of kTileMany tokens
+//   words 0 .. 7   M, n_slots, tiles of kTileFew tokens, tiles of kTileMany tokens, those of the latter with an adapter, 0, 0, 0
 //   tiles of 16    {adapter or -1, first place in the list of tokens, tokens, 0, their numbers [16]}: one round of loads
 //   tiles of 128   {adapter or -1, first place, tokens, the first token's number if they follow one another, else -1}
 //   tokens         [M] token numbers by adapter, those without one last
@@ -26,10 +26,10 @@ __host__ __device__ inline PlanView plan_view(const int32_t* plan, int M, int n_
     int32_t* w = const_cast<int32_t*>(plan);
     const long long few = plan_tiles(M, n_slots, kTileFew), many = plan_tiles(M, n_slots, kTileMany);
     PlanView v;
-    v.tiles_few = w + 4;
-    v.tiles_many = reinterpret_cast<int4*>(w + 4 + kFewWords * few);
-    v.tokens = w + 4 + kFewWords * few + 4 * many;
-    v.words = 4 + kFewWords * few + 4 * many + M;
+    v.tiles_few = w + 8;
+    v.tiles_many = reinterpret_cast<int4*>(w + 8 + kFewWords * few);
+    v.tokens = w + 8 + kFewWords * few + 4 * many;
+    v.words = 8 + kFewWords * few + 4 * many + M;
     return v;
 }
 

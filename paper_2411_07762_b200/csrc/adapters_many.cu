@@ -79,6 +79,11 @@ __device__ __forceinline__ TileRows tile_rows(const int4& t4, const int32_t* tok
     return r;
 }
 
+__device__ __forceinline__ uint32_t pack_half2(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+
 __device__ __forceinline__ void tmem_alloc(uint32_t* slot, uint32_t cols) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(slot)), "r"(cols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -95,21 +100,17 @@ constexpr int kDownThreads = 256, kDownWarps = 8;
 struct DownMaps { CUtensorMap x, x_one, a; };
 
 __host__ __device__ constexpr int down_stage_bytes(int r) { return kRowsBytes + r * kCols * 2; }
-// The ring also holds the partial sums at the end, [128][rank + 4] floats.  Few CTAs have an SM each and the deeper ring; above
-// that two share one (one's set-up and exchange beside the other's copies), up to rank 128.
+// The ring also holds the partial sums at the end, [128][rank + 4] floats.  A CTA has an SM to itself: two of them side by side
+// left other SMs idle (4096 tokens of 6 adapters, 4096 columns: the copies of 144 CTAs took 9.5 instead of 6.6 us).
 constexpr int kDownTail = 2 * kMaxStages * 8 + 32;   // barriers, tensor memory's address, flag
-constexpr int down_stages(int r, bool alone) {
-    const int fit = ((alone || r > 128 ? 224 : 112) * 1024 - kDownTail - 1024) / down_stage_bytes(r);
+constexpr int kDownSmem = 224 * 1024;
+constexpr int down_stages(int r) {
+    const int fit = (kDownSmem - kDownTail - 1024) / down_stage_bytes(r);
     return fit < kMaxStages ? fit : kMaxStages;
 }
-constexpr int down_smem(int r, bool alone) {         // (more than half of an SM's, where a CTA is to be alone)
-    const int bytes = down_stages(r, alone) * down_stage_bytes(r) + kDownTail + 1024;
-    return alone && bytes < 120 * 1024 ? 120 * 1024 : bytes;
-}
-static_assert(down_stages(128, false) >= 3 && down_stages(256, true) >= 4, "a ring");
-static_assert(2 * (down_smem(64, false) + 1024) <= 228 * 1024 && 2 * (down_smem(128, false) + 1024) <= 228 * 1024, "two CTAs to an SM");
+static_assert(down_stages(256) >= 4, "a ring");
 
-__global__ void __launch_bounds__(kDownThreads, 2)
+__global__ void __launch_bounds__(kDownThreads, 1)
 adapters_down_kernel(const __grid_constant__ DownMaps maps, const AdapterParams p, int stages, uint32_t tmem_cols) {
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -204,7 +205,7 @@ adapters_down_kernel(const __grid_constant__ DownMaps maps, const AdapterParams 
         tc_fence_before();
         cluster_arrive();
         cluster_wait();
-        const int per = kTok / CL;
+        const int per = (kTok + CL - 1) / CL;
         const float alpha = p.scale ? __ldg(p.scale + slot) : 1.f;
         auto gather = [&](int row, int j) {
             const uint32_t at = smem_u32(part + row * stride + j);
@@ -216,9 +217,9 @@ adapters_down_kernel(const __grid_constant__ DownMaps maps, const AdapterParams 
             return v;
         };
         if (rk <= 64) {                   // two tokens side by side
-            for (int i = warp * 2 + (lane >> 4); i < per; i += 2 * kDownWarps) {
-                const int row = rank * per + i, j = (lane & 15) * 4;
-                const bool mine = row < count && j < rk;
+            for (int i0 = warp * 2; i0 < per; i0 += 2 * kDownWarps) {
+                const int i = i0 + (lane >> 4), row = rank * per + i, j = (lane & 15) * 4;
+                const bool mine = i < per && row < count && j < rk;
                 float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
                 if (mine) v = gather(row, j);
                 float top = max4_abs(v);
@@ -268,24 +269,29 @@ constexpr int kUpTail = 256;
 __host__ __device__ constexpr int up_smem(int r) { return (r <= 128 ? 112 : 224) * 1024; }
 static_assert(up_smem(128) - kUpTail - 1024 >= up_chunks(128) * kTok * 128 + 2 * (kRowsBytes + up_chunks(128) * kCols * 128), "two stages at least");
 static_assert(up_smem(256) - kUpTail - 1024 >= up_chunks(256) * kTok * 128 + 2 * (kRowsBytes + up_chunks(256) * kCols * 128), "two stages at least");
-constexpr uint32_t kUpTmem = 2 * kCols;
+constexpr int kUpSums = 4;                            // blocks whose sums are in tensor memory at once
+constexpr uint32_t kUpTmem = kUpSums * kCols;
 
-// Blocks of 64 channels [c n / chunks, (c + 1) n / chunks) of a tile.  What wrote Y and the plan is known to be complete when this
+// Blocks of 64 channels [c n / chunks, (c + 1) n / chunks) of a tile; `resident` CTAs are dealt over the tiles that there are.  What wrote Y and the plan is known to be complete when this
 // kernel starts, because the first kernel waited for it; S is waited for.
 __global__ void __launch_bounds__(kUpThreads, 2)
-adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, int chunks) {
+adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, int resident) {
     extern __shared__ uint8_t smem_raw[];
-    const int tile = (int)blockIdx.x / chunks, chunk = (int)blockIdx.x - tile * chunks;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     warm_ranks(p);
     const PlanView plan = plan_view(p.plan, p.M, p.n_slots);
-    const int4 head = *reinterpret_cast<const int4*>(p.plan);
+    const int4 head = *reinterpret_cast<const int4*>(p.plan), more = *reinterpret_cast<const int4*>(p.plan + 4);
+    const int tiles = p.Y == p.out ? more.x : head.w;        // (in place, those without an adapter, the last ones, have nothing to do)
+    if (head.x != p.M || head.y != p.n_slots || tiles == 0) return;
+    const int blocks = (p.N + kCols - 1) / kCols;
+    int chunks = resident / tiles;                           // (two blocks and more for a CTA)
+    chunks = chunks < 1 ? 1 : chunks > (blocks + 1) / 2 ? (blocks + 1) / 2 : chunks;
+    const int tile = (int)blockIdx.x / chunks, chunk = (int)blockIdx.x - tile * chunks;
+    if (tile >= tiles) return;
     const int4 t4 = plan.tiles_many[tile];
-    if (head.x != p.M || head.y != p.n_slots || tile >= head.w) return;
     const int slot = t4.x, first = t4.y, count = t4.z;
     const int32_t* tokens = plan.tokens + first;
     const int rk = slot < 0 ? 0 : adapter_rank(p, slot);
-    const int blocks = (p.N + kCols - 1) / kCols;
     const int b0 = (int)((long long)chunk * blocks / chunks), n = (int)((long long)(chunk + 1) * blocks / chunks) - b0;
     if (rk == 0) {                        // nothing to add
         if (p.Y != p.out)
@@ -302,18 +308,20 @@ adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, i
     const int stage_bytes = row_bytes + kch * kCols * 128, room = up_smem(p.r) - kUpTail - 1024;
     const int fit = (room - s_bytes) / stage_bytes, stages = fit < kMaxStages ? fit : kMaxStages;
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + room);
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * kMaxStages + 5);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * kMaxStages + 2 * kUpSums + 1);
     volatile int* stop = reinterpret_cast<volatile int*>(tmem_slot + 1);
     const uint32_t sb = smem_u32(smem), bar0 = smem_u32(bars);
     auto filled = [&](int s) { return bar0 + 8u * s; };                 // a stage's Y and B are there
     auto free_ = [&](int s) { return bar0 + 8u * (kMaxStages + s); };   // ... and have been read (four warps)
     auto read = [&](int h) { return bar0 + 8u * (2 * kMaxStages + h); };        // a block's sums have been read (four warps)
-    auto full = [&](int h) { return bar0 + 8u * (2 * kMaxStages + 2 + h); };    // ... are complete
-    const uint32_t s_there = bar0 + 8u * (2 * kMaxStages + 4);
+    auto full = [&](int h) { return bar0 + 8u * (2 * kMaxStages + kUpSums + h); };    // ... are complete
+    constexpr int kBars = 2 * kMaxStages + 2 * kUpSums + 1;
+    static_assert(kBars <= 32 && kBars * 8 + 8 <= kUpTail, "barriers");
+    const uint32_t s_there = bar0 + 8u * (kBars - 1);
     if (warp == 0) {
         tmem_alloc(tmem_slot, kUpTmem);
     } else if (warp == 1) {
-        if (lane < 2 * kMaxStages + 5) mbar_init(bar0 + 8u * lane, lane >= kMaxStages && lane < 2 * kMaxStages + 2 ? 4 : 1);
+        if (lane < kBars) mbar_init(bar0 + 8u * lane, lane >= kMaxStages && lane < 2 * kMaxStages + kUpSums ? 4 : 1);
         if (lane == 0) *stop = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_proxy_async_smem();
@@ -355,9 +363,9 @@ adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, i
         const uint32_t idesc = make_idesc(1, 0, 128, kCols);
         bool ok = warp_wait(s_there, 0u, stop, lane);
         for (int i = 0, s = 0, turn = 0; i < n && ok; ++i) {
-            const int h = i & 1;
+            const int h = i % kUpSums;
             ok = warp_wait(filled(s), (uint32_t)turn & 1u, stop, lane);
-            if (ok && i >= 2) ok = warp_wait(read(h), (uint32_t)((i >> 1) - 1) & 1u, stop, lane);
+            if (ok && i >= kUpSums) ok = warp_wait(read(h), (uint32_t)(i / kUpSums - 1) & 1u, stop, lane);
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
@@ -373,50 +381,55 @@ adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, i
             if (++s == stages) { s = 0; ++turn; }
         }
     } else {
-        const int q = warp & 3, h = (warp - 2) >> 2;      // a quarter of the tokens (of tensor memory's lanes), every other block
+        const int q = warp & 3;           // a quarter of the tokens (of tensor memory's lanes), every other block
         const int row = q * 32 + lane;
         grid_dep_wait();                  // the factors come from the first kernel
         const float factor = row < count ? p.row_scale[first + row] : 0.f;
         // lines are written by eight lanes each: this lane's 16 bytes of rows q 32 + lane / 8, + 4, ...
         const int wr = q * 32 + (lane >> 3), wc = lane & 7;
-        size_t out_row[8];
+        int out_tok[8];
         uint32_t there = 0;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            out_row[e] = wr + 4 * e < count ? (size_t)tokens[wr + 4 * e] * p.ldo + wc * 8 : 0;
+            out_tok[e] = wr + 4 * e < count ? tokens[wr + 4 * e] : 0;
             there |= wr + 4 * e < count ? 1u << e : 0u;
         }
         bool ok = true;
-        for (int i = h; i < n; i += 2) {
-            const int s = i % stages;
+        for (int i = (warp - 2) >> 2; i < n; i += 2) {
+            const int s = i % stages, h = i % kUpSums;
             const uint32_t at = sb + (uint32_t)(s_bytes + s * stage_bytes);
             if (ok) ok = warp_wait(filled(s), (uint32_t)(i / stages) & 1u, stop, lane);
-            if (ok) ok = warp_wait(full(h), (uint32_t)(i >> 1) & 1u, stop, lane);
-            if (ok) {
+            if (ok) ok = warp_wait(full(h), (uint32_t)(i / kUpSums) & 1u, stop, lane);
+            if (ok && q * 32 < count) {
                 tc_fence_after();
 #pragma unroll
-                for (int c0 = 0; c0 < kCols; c0 += 32) {
+                for (int c0 = 0; c0 < 8; c0 += 4) {
                     uint32_t v[2][16];
-                    tmem_ld16(tmem + h * kCols + ((uint32_t)(q * 32) << 16) + c0, v[0]);
-                    tmem_ld16(tmem + h * kCols + ((uint32_t)(q * 32) << 16) + c0 + 16, v[1]);
+                    tmem_ld16(tmem + h * kCols + ((uint32_t)(q * 32) << 16) + c0 * 8, v[0]);
+                    tmem_ld16(tmem + h * kCols + ((uint32_t)(q * 32) << 16) + c0 * 8 + 16, v[1]);
+                    uint4 y[4];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        y[c] = make_uint4(0, 0, 0, 0);
+                        if (row < count)
+                            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(y[c].x), "=r"(y[c].y), "=r"(y[c].z), "=r"(y[c].w)
+                                         : "r"(at + (uint32_t)(row * 128 + (((c0 + c) ^ (row & 7)) << 4))) : "memory");
+                    }
                     tmem_wait_ld_all();
                     tmem_use(v[0]);
                     tmem_use(v[1]);
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         if (row >= count) break;
-                        const uint32_t place = at + (uint32_t)(row * 128 + (((c0 / 8 + c) ^ (row & 7)) << 4));
-                        uint32_t y[4];
-                        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(y[0]), "=r"(y[1]), "=r"(y[2]), "=r"(y[3]) : "r"(place));
+                        uint32_t yw[4] = {y[c].x, y[c].y, y[c].z, y[c].w};
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&y[e]));
+                            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&yw[e]));
                             const int j = (c & 1) * 8 + 2 * e;
-                            const __half2 o = __floats2half2_rn(fmaf(__uint_as_float(v[c >> 1][j]), factor, f.x),
-                                                                fmaf(__uint_as_float(v[c >> 1][j + 1]), factor, f.y));
-                            y[e] = *reinterpret_cast<const uint32_t*>(&o);
+                            yw[e] = pack_half2(fmaf(__uint_as_float(v[c >> 1][j]), factor, f.x), fmaf(__uint_as_float(v[c >> 1][j + 1]), factor, f.y));
                         }
-                        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(place), "r"(y[0]), "r"(y[1]), "r"(y[2]), "r"(y[3]) : "memory");
+                        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at + (uint32_t)(row * 128 + (((c0 + c) ^ (row & 7)) << 4))),
+                                     "r"(yw[0]), "r"(yw[1]), "r"(yw[2]), "r"(yw[3]) : "memory");
                     }
                 }
                 tc_fence_before();
@@ -428,18 +441,18 @@ adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, i
             uint4 o[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                if (!(there >> e & 1)) continue;
                 const int r = wr + 4 * e;
-                asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(o[e].x), "=r"(o[e].y), "=r"(o[e].z), "=r"(o[e].w)
-                             : "r"(at + (uint32_t)(r * 128 + ((wc ^ (r & 7)) << 4))) : "memory");
+                o[e] = make_uint4(0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu);
+                if (ok && (there >> e & 1))
+                    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(o[e].x), "=r"(o[e].y), "=r"(o[e].z), "=r"(o[e].w)
+                                 : "r"(at + (uint32_t)(r * 128 + ((wc ^ (r & 7)) << 4))) : "memory");
             }
             fence_proxy_async_smem();     // the next copy into this place comes after these reads and writes
             __syncwarp();
             if (lane == 0) mbar_arrive(free_(s));
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                if (!ok) o[e] = make_uint4(0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu);
-                if (in && (there >> e & 1)) *reinterpret_cast<uint4*>(p.out + out_row[e] + ch) = o[e];
+                if (in && (there >> e & 1)) *reinterpret_cast<uint4*>(p.out + (size_t)out_tok[e] * p.ldo + (ch + wc * 8)) = o[e];
             }
         }
     }
@@ -466,12 +479,37 @@ int opt_in(Kernel* kernel, int bytes, bool (&configured)[kMaxDevices], int* num_
     return ASER_OK;
 }
 
+// Clusters of CL CTAs of the first kernel that are resident at once.
+int active_clusters(int CL) {
+    static int cached[kMaxDevices][kMaxCL + 1];       // 0: not asked yet
+    int dev = 0;
+    if (current_device(&dev) != ASER_OK) return 0;
+    if (cached[dev][CL] == 0) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(CL, 1, 1);
+        cfg.blockDim = dim3(kDownThreads, 1, 1);
+        cfg.dynamicSmemBytes = kDownSmem;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = CL; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        int n = 0;
+        if (cudaOccupancyMaxActiveClusters(&n, adapters_down_kernel, &cfg) != cudaSuccess) {
+            (void)cudaGetLastError();
+            n = 0;
+        }
+        cached[dev][CL] = n > 0 ? n : -1;
+    }
+    return cached[dev][CL] > 0 ? cached[dev][CL] : 0;
+}
+
 }  // namespace
 
 int launch_adapters_down(const AdapterParams& p, cudaStream_t st) {
     static bool configured[kMaxDevices] = {false};
     int num_sms = 0;
-    int rc = opt_in(adapters_down_kernel, 224 * 1024, configured, &num_sms);
+    int rc = opt_in(adapters_down_kernel, kDownSmem, configured, &num_sms);
     if (rc != ASER_OK) return rc;
     DownMaps maps;
     const CUtensorMapDataType f16 = CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
@@ -479,16 +517,15 @@ int launch_adapters_down(const AdapterParams& p, cudaStream_t st) {
     if (rc == ASER_OK) rc = encode_map_2d_ld(&maps.x_one, f16, 2, p.X, p.M, p.K, p.ldx, 1, kCols, CU_TENSOR_MAP_SWIZZLE_128B);
     if (rc == ASER_OK) rc = encode_map_2d(&maps.a, f16, 2, p.A, (uint64_t)p.n_slots * p.r, p.K, 16, kCols, CU_TENSOR_MAP_SWIZZLE_128B);
     if (rc != ASER_OK) return rc;
-    // as large a share of the SMs as the tiles can be split over; a CTA has two steps of K at least
+    // as many CTAs to a tile as let the tiles that are likely run at once; a CTA has two steps of K at least
     int CL = kMaxCL;
-    while (CL > 1 && (likely_tiles(p) * CL > 2 * num_sms + num_sms / 8 || p.K / kCols < 2 * CL)) CL /= 2;
-    const bool alone = likely_tiles(p) * CL <= num_sms + num_sms / 8;
+    while (CL > 1 && (likely_tiles(p) > active_clusters(CL) || p.K / kCols < 2 * CL)) --CL;
     uint32_t cols = 32;
     while ((int)cols < p.r) cols *= 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(plan_tiles(p.M, p.n_slots, kTok) * CL, 1, 1);
     cfg.blockDim = dim3(kDownThreads, 1, 1);
-    cfg.dynamicSmemBytes = down_smem(p.r, alone);
+    cfg.dynamicSmemBytes = kDownSmem;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -497,7 +534,7 @@ int launch_adapters_down(const AdapterParams& p, cudaStream_t st) {
     attr[1].val.clusterDim.x = CL; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, adapters_down_kernel, maps, p, down_stages(p.r, alone), cols);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, adapters_down_kernel, maps, p, down_stages(p.r), cols);
     if (e != cudaSuccess) return record_cuda_error(e, "adapters_down_kernel");
     return check_launch("adapters_down_kernel");
 }
@@ -514,13 +551,9 @@ int launch_adapters_up(const AdapterParams& p, cudaStream_t st) {
     if (rc == ASER_OK) rc = encode_map_2d(&maps.s, f16, 2, p.S, p.M, p.r, kBox, 64, CU_TENSOR_MAP_SWIZZLE_128B);
     if (rc == ASER_OK) rc = encode_map_2d(&maps.b, f16, 2, p.B, (uint64_t)p.n_slots * p.N, p.r, kCols, 64, CU_TENSOR_MAP_SWIZZLE_128B);
     if (rc != ASER_OK) return rc;
-    // as many CTAs as are resident at once, if every one has two blocks and more
-    const int resident = (p.r <= 128 ? 2 : 1) * num_sms, blocks = (p.N + kCols - 1) / kCols;
-    int chunks = resident / likely_tiles(p);
-    if (chunks > (blocks + 1) / 2) chunks = (blocks + 1) / 2;
-    if (chunks < 1) chunks = 1;
+    const int resident = (p.r <= 128 ? 2 : 1) * num_sms, bound = plan_tiles(p.M, p.n_slots, kTok);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(plan_tiles(p.M, p.n_slots, kTok) * chunks, 1, 1);
+    cfg.gridDim = dim3(resident > bound ? resident : bound, 1, 1);
     cfg.blockDim = dim3(kUpThreads, 1, 1);
     cfg.dynamicSmemBytes = up_smem(p.r);
     cfg.stream = st;
@@ -529,7 +562,7 @@ int launch_adapters_up(const AdapterParams& p, cudaStream_t st) {
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, adapters_up_kernel, maps, p, chunks);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, adapters_up_kernel, maps, p, resident);
     if (e != cudaSuccess) return record_cuda_error(e, "adapters_up_kernel");
     return check_launch("adapters_up_kernel");
 }

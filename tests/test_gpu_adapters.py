@@ -182,7 +182,7 @@ def test_ranks_that_are_no_ranks(aser):
 def read_plan(plan):
     w = plan.data.view(torch.int32).cpu()
     M, S = plan.M, plan.n_slots
-    head, at, tiles = w[:4].tolist(), 4, []
+    head, at, tiles = w[:5].tolist(), 8, []
     for size, words, n in ((16, 20, head[2]), (128, 4, head[3])):
         bound = M // size + min(S + 1, M)
         assert n <= bound
@@ -199,6 +199,7 @@ def test_plan(aser, M, slots):
     s = [a if 0 <= a < slots else -1 for a in slot.tolist()]
     want = sorted(range(M), key=lambda m: (s[m] if s[m] >= 0 else slots, m))
     assert head[:2] == [M, slots] and tokens == want
+    assert head[4] == sum(a >= 0 for a, *_ in tiles[1])
     for size, ts in zip((16, 128), tiles):
         at = 0
         for a, first, count, run, *own in ts:
