@@ -260,7 +260,7 @@ adapters_down_kernel(const __grid_constant__ DownMaps maps, const AdapterParams 
 // ---------------------------------------------------------------------------
 constexpr int kUpWarps = 10, kUpThreads = kUpWarps * 32;      // copies, products, twice four that finish blocks in turn
 
-struct UpMaps { CUtensorMap y, y_one, s, b; };
+struct UpMaps { CUtensorMap y, y_one, s, b, out; };
 
 __host__ __device__ constexpr int up_chunks(int r) { return (r + 63) / 64; }          // blocks of 64 ranks
 // Shared memory of a CTA: S, then as many stages as there is room for; they are as large as the tile's tokens and the adapter's
@@ -394,6 +394,8 @@ adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, i
             out_tok[e] = wr + 4 * e < count ? tokens[wr + 4 * e] : 0;
             there |= wr + 4 * e < count ? 1u << e : 0u;
         }
+        const bool box = t4.w >= 0 && (q + 1) * 32 <= count;
+        int kept = -1;
         bool ok = true;
         for (int i = (warp - 2) >> 2; i < n; i += 2) {
             const int s = i % stages, h = i % kUpSums;
@@ -437,6 +439,24 @@ adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, i
             __syncwarp();
             if (lane == 0) mbar_arrive(read(h));
             const int ch = (b0 + i) * kCols;
+            if (box && ok) {              // 32 rows that follow one another: one tensor store, which clips at N
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    tma_store_2d_tile(&maps.out, ch, t4.w + q * 32, at + (uint32_t)(q * 32 * 128));
+                    bulk_store_commit();
+                    // its place is given back with this warp's next block, two on, which a ring of three stages reaches without it
+                    if (stages >= 30) {
+                        bulk_store_wait_read_but<1>();
+                        if (kept >= 0) mbar_arrive(free_(kept));
+                    } else {
+                        bulk_store_wait_read();
+                        mbar_arrive(free_(s));
+                    }
+                }
+                kept = s;
+                continue;
+            }
             const bool in = ch + wc * 8 < p.N;
             uint4 o[8];
 #pragma unroll
@@ -455,6 +475,7 @@ adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, i
                 if (in && (there >> e & 1)) *reinterpret_cast<uint4*>(p.out + (size_t)out_tok[e] * p.ldo + (ch + wc * 8)) = o[e];
             }
         }
+        if (box && lane == 0) bulk_store_wait_read();        // nobody leaves before its shared memory has been read
     }
     __syncwarp();
     tc_fence_before();
@@ -550,6 +571,8 @@ int launch_adapters_up(const AdapterParams& p, cudaStream_t st) {
     if (rc == ASER_OK) rc = encode_map_2d_ld(&maps.y_one, f16, 2, p.Y, p.M, p.N, p.ldy, 1, kCols, CU_TENSOR_MAP_SWIZZLE_128B);
     if (rc == ASER_OK) rc = encode_map_2d(&maps.s, f16, 2, p.S, p.M, p.r, kBox, 64, CU_TENSOR_MAP_SWIZZLE_128B);
     if (rc == ASER_OK) rc = encode_map_2d(&maps.b, f16, 2, p.B, (uint64_t)p.n_slots * p.N, p.r, kCols, 64, CU_TENSOR_MAP_SWIZZLE_128B);
+    if (rc != ASER_OK) return rc;
+    rc = encode_map_2d_ld(&maps.out, f16, 2, p.out, p.M, p.N, p.ldo, kBox, kCols, CU_TENSOR_MAP_SWIZZLE_128B);
     if (rc != ASER_OK) return rc;
     const int resident = (p.r <= 128 ? 2 : 1) * num_sms, bound = plan_tiles(p.M, p.n_slots, kTok);
     cudaLaunchConfig_t cfg = {};
