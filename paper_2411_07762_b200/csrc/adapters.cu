@@ -312,7 +312,7 @@ adapters_plan_kernel(const int32_t* __restrict__ slot, int M, int n_slots, int32
         *reinterpret_cast<int4*>(out) = make_int4(M, n_slots, few, many);
     }
     // (the last group is that of the tokens without an adapter)
-    if (g0 < groups && g1 == groups) *reinterpret_cast<int4*>(out + 4) = make_int4(at.z + mine.z - tiles_of(cursor[groups - 1], kTileMany), 0, 0, 0);
+    if (g0 < groups && g1 == groups) *reinterpret_cast<int4*>(out + 4) = make_int4(at.z + mine.z - tiles_of(cursor[groups - 1], kTileMany), M - cursor[groups - 1], 0, 0);
     for (int i = g0; i < g1; ++i) {
         const int n = cursor[i], s = i < n_slots ? i : -1;
         for (int k = 0; k < n; k += kTileFew) *reinterpret_cast<int4*>(plan.tiles_few + (size_t)kFewWords * at.y++) = make_int4(s, at.x + k, min(kTileFew, n - k), 0);
@@ -402,14 +402,16 @@ bool adapters_many(int M, int n_slots) {
     return M > 24 * used;
 }
 
+// Sums of S in up to kMaxParts parts: as many as make no more CTAs than kMaxDownCtas, of 128 tokens each.
 size_t adapters_workspace_bytes(int M, int r, int n_slots) {
-    return adapters_many(M, n_slots) ? (size_t)M * 2 * r + (size_t)M * 4 : 0;
+    if (!adapters_many(M, n_slots)) return 0;
+    const size_t split = (size_t)M * kMaxParts, most = (size_t)kMaxDownCtas * kTileMany, rows = split < most ? split : (size_t)M > most ? (size_t)M : most;
+    return rows * r * 4;
 }
 
 int launch_adapters(AdapterParams p, void* workspace, cudaStream_t st) {
     if (!adapters_many(p.M, p.n_slots)) return launch_few(p, st);
-    p.S = static_cast<__half*>(workspace);
-    p.row_scale = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + (size_t)p.M * 2 * p.r);
+    p.S = static_cast<float*>(workspace);
     const int rc = launch_adapters_down(p, st);
     return rc != ASER_OK ? rc : launch_adapters_up(p, st);
 }

@@ -1,5 +1,6 @@
 // The plan of a batch's adapters (adapters.cu): tokens by adapter, cut into tiles of one adapter each.
-//   words 0 .. 7   M, n_slots, tiles of kTileFew tokens, tiles of kTileMany tokens, those of the latter with an adapter, 0, 0, 0
+//   words 0 .. 7   M, n_slots, tiles of kTileFew tokens, tiles of kTileMany tokens, those of the latter with an
+//                  adapter, tokens with an adapter, 0, 0
 //   tiles of 16    {adapter or -1, first place in the list of tokens, tokens, 0, their numbers [16]}: one round of loads
 //   tiles of 128   {adapter or -1, first place, tokens, the first token's number if they follow one another, else -1}
 //   tokens         [M] token numbers by adapter, those without one last
@@ -9,6 +10,7 @@
 namespace aser {
 
 constexpr int kTileFew = 16, kTileMany = 128;
+constexpr int kMaxParts = 16, kMaxDownCtas = 160;      // many tokens: parts of K, CTAs that they are dealt to
 
 constexpr int kFewWords = 4 + kTileFew;
 
@@ -42,8 +44,7 @@ struct AdapterParams {
     const int32_t* plan;
     const __half* Y;
     __half* out;
-    __half* S;                // [M, r] by place in the plan's list, and [M] what its rows are to be multiplied by: between the
-    float* row_scale;         // two kernels for many tokens
+    float* S;                 // between the two kernels for many tokens: [parts of K][tokens with an adapter][r]
     size_t ldx, ldy, ldo;
     int M, N, K, r, n_slots;
     int parts;                // few tokens: clusters per tile, each with its own part of N
@@ -54,7 +55,7 @@ int launch_adapters_plan(const int32_t* slot, int M, int n_slots, void* plan, cu
 // Whether a call runs the two kernels for many tokens, and the workspace that it then needs.
 bool adapters_many(int M, int n_slots);
 size_t adapters_workspace_bytes(int M, int r, int n_slots);
-// (p.S and p.row_scale are set from `workspace`.)
+// (p.S is set to `workspace`.)
 int launch_adapters(AdapterParams p, void* workspace, cudaStream_t st);
 int launch_adapters_down(const AdapterParams& p, cudaStream_t st);
 int launch_adapters_up(const AdapterParams& p, cudaStream_t st);

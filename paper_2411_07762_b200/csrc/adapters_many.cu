@@ -21,7 +21,7 @@ namespace aser {
 
 namespace {
 
-constexpr int kTok = kTileMany, kMaxCL = 8, kBox = 32;
+constexpr int kTok = kTileMany, kBox = 32;
 constexpr int kCols = 64;                            // columns or channels of a stage: 128 bytes a row
 constexpr int kRowsBytes = kTok * kCols * 2;
 constexpr int kMaxStages = 8;
@@ -79,6 +79,7 @@ __device__ __forceinline__ TileRows tile_rows(const int4& t4, const int32_t* tok
     return r;
 }
 
+__device__ __forceinline__ void add4(float4& a, const float4& b) { a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w; }
 __device__ __forceinline__ uint32_t pack_half2(float a, float b) {
     const __half2 h = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&h);
@@ -100,8 +101,7 @@ constexpr int kDownThreads = 256, kDownWarps = 8;
 struct DownMaps { CUtensorMap x, x_one, a; };
 
 __host__ __device__ constexpr int down_stage_bytes(int r) { return kRowsBytes + r * kCols * 2; }
-// The ring also holds the partial sums at the end, [128][rank + 4] floats.  A CTA has an SM to itself: two of them side by side
-// left other SMs idle (4096 tokens of 6 adapters, 4096 columns: the copies of 144 CTAs took 9.5 instead of 6.6 us).
+// A CTA has an SM to itself: two of them side by side left other SMs idle.
 constexpr int kDownTail = 2 * kMaxStages * 8 + 32;   // barriers, tensor memory's address, flag
 constexpr int kDownSmem = 224 * 1024;
 constexpr int down_stages(int r) {
@@ -110,8 +110,15 @@ constexpr int down_stages(int r) {
 }
 static_assert(down_stages(256) >= 4, "a ring");
 
+// Parts of K that a tile's sums are made in, at least two steps each: as many as `ctas` serve at once.
+__device__ __forceinline__ int down_parts(int tiles, int ctas, int K) {
+    const int steps = K / kCols, by_ctas = ctas / tiles, by_steps = steps / 2;
+    const int parts = by_ctas < by_steps ? by_ctas : by_steps;
+    return parts < 1 ? 1 : parts > kMaxParts ? kMaxParts : parts;
+}
+
 __global__ void __launch_bounds__(kDownThreads, 1)
-adapters_down_kernel(const __grid_constant__ DownMaps maps, const AdapterParams p, int stages, uint32_t tmem_cols) {
+adapters_down_kernel(const __grid_constant__ DownMaps maps, const AdapterParams p, int stages, int ctas, uint32_t tmem_cols) {
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const int stage_bytes = down_stage_bytes(p.r);
@@ -140,15 +147,16 @@ adapters_down_kernel(const __grid_constant__ DownMaps maps, const AdapterParams 
     grid_dep_wait();
     grid_dep_launch();
     warm_ranks(p);
-    const int CL = (int)cluster_size(), rank = (int)cluster_rank(), tile = (int)blockIdx.x / CL;
     const PlanView plan = plan_view(p.plan, p.M, p.n_slots);
-    const int4 head = *reinterpret_cast<const int4*>(p.plan);
-    const int4 t4 = plan.tiles_many[tile];
-    const bool real = head.x == p.M && head.y == p.n_slots && tile < head.w;
-    const int slot = real ? t4.x : -1, first = t4.y, count = t4.z;
+    const int4 head = *reinterpret_cast<const int4*>(p.plan), more = *reinterpret_cast<const int4*>(p.plan + 4);
+    const int tiles = head.x == p.M && head.y == p.n_slots ? more.x : 0, parts = tiles > 0 ? down_parts(tiles, ctas, p.K) : 1;
+    const int tile = (int)blockIdx.x / parts, part = (int)blockIdx.x - tile * parts;
+    int4 t4 = make_int4(-1, 0, 0, 0);
+    if (tile < tiles) t4 = plan.tiles_many[tile];
+    const int slot = t4.x, first = t4.y, count = t4.z;
     const int rk = slot < 0 ? 0 : adapter_rank(p, slot);
-    if (rk > 0) {                     // (the whole cluster)
-        const int steps = p.K / kCols, s0 = rank * steps / CL, n = (rank + 1) * steps / CL - s0;
+    if (rk > 0) {
+        const int steps = p.K / kCols, s0 = part * steps / parts, n = (part + 1) * steps / parts - s0;
         if (warp == 0) {              // copies
             const TileRows rows = tile_rows(t4, plan.tokens, lane);
             const uint32_t bytes = (uint32_t)(rows.rows() + rk) * 128u;
@@ -179,77 +187,24 @@ adapters_down_kernel(const __grid_constant__ DownMaps maps, const AdapterParams 
                 if (++s == stages) { s = 0; ++turn; }
             }
         }
-        bool ok = true;
-        if (n > 0) ok = warp_wait(smem_u32(done), 0u, stop, lane);
-        __syncthreads();                  // the ring is free
-        if (*stop) { ok = false; let_copies_land(); }
+        const bool ok = warp_wait(smem_u32(done), 0u, stop, lane);
         tc_fence_after();
-        // partial sums [128 tokens][rk + 4]
-        float* part = reinterpret_cast<float*>(smem);
-        const int stride = rk + 4;
+        // the sums leave as they are: a token to a thread, 16 ranks at a time
+        const int row = (warp & 3) * 32 + lane;
+        float* to = p.S + ((size_t)part * more.y + first + row) * p.r;
         for (int c = (warp >> 2) * 16; c < rk; c += 32) {
             uint32_t v[16];
+            tmem_ld16(tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)c, v);
+            tmem_wait_ld(v);
+            if (row < count)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) v[e] = 0u;
-            if (n > 0) {
-                tmem_ld16(tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)c, v);
-                tmem_wait_ld(v);
-            }
-            uint4* q = reinterpret_cast<uint4*>(part + ((warp & 3) * 32 + lane) * stride + c);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const uint32_t nan = 0x7fffffffu;
-                q[e] = ok ? make_uint4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]) : make_uint4(nan, nan, nan, nan);
-            }
+                for (int e = 0; e < 16; e += 4)
+                    *reinterpret_cast<uint4*>(to + c + e) = ok ? make_uint4(v[e], v[e + 1], v[e + 2], v[e + 3])
+                                                               : make_uint4(0x7fffffffu, 0x7fffffffu, 0x7fffffffu, 0x7fffffffu);
         }
         tc_fence_before();
-        cluster_arrive();
-        cluster_wait();
-        const int per = (kTok + CL - 1) / CL;
-        const float alpha = p.scale ? __ldg(p.scale + slot) : 1.f;
-        auto gather = [&](int row, int j) {
-            const uint32_t at = smem_u32(part + row * stride + j);
-            float4 a[kMaxCL], v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int q = 0; q < kMaxCL; ++q) a[q] = q < CL ? ld_cluster_f32x4(map_to_rank(at, q)) : v;
-#pragma unroll
-            for (int q = 0; q < kMaxCL; ++q) { v.x += a[q].x; v.y += a[q].y; v.z += a[q].z; v.w += a[q].w; }
-            return v;
-        };
-        if (rk <= 64) {                   // two tokens side by side
-            for (int i0 = warp * 2; i0 < per; i0 += 2 * kDownWarps) {
-                const int i = i0 + (lane >> 4), row = rank * per + i, j = (lane & 15) * 4;
-                const bool mine = i < per && row < count && j < rk;
-                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (mine) v = gather(row, j);
-                float top = max4_abs(v);
-#pragma unroll
-                for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                const RowFactor f = row_factor(top);
-                if (mine) *reinterpret_cast<uint2*>(p.S + (size_t)(first + row) * p.r + j) = scaled_f16(v, f.up);
-                if (mine && j == 0) p.row_scale[first + row] = f.down * alpha;
-            }
-        } else {
-            for (int i = warp; i < per && rank * per + i < count; i += kDownWarps) {
-                const int row = rank * per + i;
-                float4 v[2];
-                float top = 0.f;
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    v[h] = make_float4(0.f, 0.f, 0.f, 0.f);
-                    if (h * 128 + lane * 4 < rk) v[h] = gather(row, h * 128 + lane * 4);
-                    top = fmaxf(top, max4_abs(v[h]));
-                }
-                const RowFactor f = row_factor(warp_max(top));
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    if (h * 128 + lane * 4 < rk)
-                        *reinterpret_cast<uint2*>(p.S + (size_t)(first + row) * p.r + h * 128 + lane * 4) = scaled_f16(v[h], f.up);
-                if (lane == 0) p.row_scale[first + row] = f.down * alpha;
-            }
-        }
-        cluster_arrive();                 // nobody leaves while a peer may still read its sums
-        cluster_wait();
+        __syncthreads();
+        if (*stop) let_copies_land();
         tc_fence_after();
     }
     if (warp == 0) tmem_free(tmem, tmem_cols);
@@ -260,12 +215,12 @@ adapters_down_kernel(const __grid_constant__ DownMaps maps, const AdapterParams 
 // ---------------------------------------------------------------------------
 constexpr int kUpWarps = 10, kUpThreads = kUpWarps * 32;      // copies, products, twice four that finish blocks in turn
 
-struct UpMaps { CUtensorMap y, y_one, s, b, out; };
+struct UpMaps { CUtensorMap y, y_one, b, out; };
 
 __host__ __device__ constexpr int up_chunks(int r) { return (r + 63) / 64; }          // blocks of 64 ranks
 // Shared memory of a CTA: S, then as many stages as there is room for; they are as large as the tile's tokens and the adapter's
 // rank ask (128 tokens of rank 64: four, 64 tokens: six).  Up to rank 128 two CTAs share an SM.
-constexpr int kUpTail = 256;
+constexpr int kUpTail = 256 + kTok * 4;
 __host__ __device__ constexpr int up_smem(int r) { return (r <= 128 ? 112 : 224) * 1024; }
 static_assert(up_smem(128) - kUpTail - 1024 >= up_chunks(128) * kTok * 128 + 2 * (kRowsBytes + up_chunks(128) * kCols * 128), "two stages at least");
 static_assert(up_smem(256) - kUpTail - 1024 >= up_chunks(256) * kTok * 128 + 2 * (kRowsBytes + up_chunks(256) * kCols * 128), "two stages at least");
@@ -275,7 +230,7 @@ constexpr uint32_t kUpTmem = kUpSums * kCols;
 // Blocks of 64 channels [c n / chunks, (c + 1) n / chunks) of a tile; `resident` CTAs are dealt over the tiles that there are.  What wrote Y and the plan is known to be complete when this
 // kernel starts, because the first kernel waited for it; S is waited for.
 __global__ void __launch_bounds__(kUpThreads, 2)
-adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, int resident) {
+adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, int resident, int ctas) {
     extern __shared__ uint8_t smem_raw[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     warm_ranks(p);
@@ -316,19 +271,19 @@ adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, i
     auto read = [&](int h) { return bar0 + 8u * (2 * kMaxStages + h); };        // a block's sums have been read (four warps)
     auto full = [&](int h) { return bar0 + 8u * (2 * kMaxStages + kUpSums + h); };    // ... are complete
     constexpr int kBars = 2 * kMaxStages + 2 * kUpSums + 1;
-    static_assert(kBars <= 32 && kBars * 8 + 8 <= kUpTail, "barriers");
-    const uint32_t s_there = bar0 + 8u * (kBars - 1);
+    static_assert(kBars <= 32 && kBars * 8 + 8 <= 256, "barriers");
+    const uint32_t s_there = bar0 + 8u * (kBars - 1);                           // S is there (eight warps)
+    float* row_factors = reinterpret_cast<float*>(smem + room + 256);
     if (warp == 0) {
         tmem_alloc(tmem_slot, kUpTmem);
     } else if (warp == 1) {
-        if (lane < kBars) mbar_init(bar0 + 8u * lane, lane >= kMaxStages && lane < 2 * kMaxStages + kUpSums ? 4 : 1);
+        if (lane < kBars) mbar_init(bar0 + 8u * lane, lane >= kMaxStages && lane < 2 * kMaxStages + kUpSums ? 4 : lane == kBars - 1 ? 8 : 1);
         if (lane == 0) *stop = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_proxy_async_smem();
     } else if (warp == 2 && lane == 0) {
         prefetch_tensormap(&maps.y);
         prefetch_tensormap(&maps.b);
-        prefetch_tensormap(&maps.s);
     }
     tc_fence_before();
     __syncthreads();
@@ -337,17 +292,7 @@ adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, i
     if (warp == 0) {                      // copies
         const TileRows rows = tile_rows(t4, plan.tokens, lane);
         const uint32_t bytes = (uint32_t)rows.rows() * 128u + (uint32_t)kch * kCols * 128u;
-        bool asked = false;
-        auto ask_for_s = [&]() {          // once the ring is full: this waits for the first kernel
-            asked = true;
-            grid_dep_wait();
-            if (lane == 0) mbar_arrive_expect_tx(s_there, (uint32_t)(kch * row_bytes));
-            __syncwarp();
-            const int boxes = row_bytes / (kBox * 128);
-            if (lane < kch * boxes) tma_load_2d(sb + lane * kBox * 128, &maps.s, lane / boxes * 64, first + lane % boxes * kBox, s_there);
-        };
         for (int i = 0, s = 0, turn = 0; i < n; ++i) {
-            if (i == stages) ask_for_s();
             if (turn > 0 && !warp_wait(free_(s), (uint32_t)(turn - 1) & 1u, stop, lane)) break;
             if (lane == 0) mbar_arrive_expect_tx(filled(s), bytes);
             __syncwarp();
@@ -357,8 +302,6 @@ adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, i
             if (lane < kch) tma_load_2d(at + row_bytes + lane * kCols * 128, &maps.b, lane * 64, slot * p.N + ch, filled(s));
             if (++s == stages) { s = 0; ++turn; }
         }
-        if (!asked) ask_for_s();
-        grid_dep_launch();
     } else if (warp == 1) {               // products
         const uint32_t idesc = make_idesc(1, 0, 128, kCols);
         bool ok = warp_wait(s_there, 0u, stop, lane);
@@ -383,8 +326,76 @@ adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, i
     } else {
         const int q = warp & 3;           // a quarter of the tokens (of tensor memory's lanes), every other block
         const int row = q * 32 + lane;
-        grid_dep_wait();                  // the factors come from the first kernel
-        const float factor = row < count ? p.row_scale[first + row] : 0.f;
+        // ---- S: the parts are added, scaled and rounded, 16 tokens to a warp, into the swizzled layout of an operand ----
+        grid_dep_wait();
+        grid_dep_launch();
+        {
+            const int parts = down_parts(more.x, ctas, p.K), r0 = (warp - 2) * 16;
+            const float alpha = p.scale ? __ldg(p.scale + slot) : 1.f;
+            const float* S = p.S + (size_t)first * p.r;
+            const size_t part_step = (size_t)more.y * p.r;
+            auto put = [&](int r, int j, const float4& v, float up) {
+                const uint2 o = scaled_f16(v, up);
+                *reinterpret_cast<uint2*>(smem + (j >> 6) * row_bytes + r * 128 + ((((j >> 3) & 7) ^ (r & 7)) << 4) + (j & 7) * 2) = o;
+            };
+            if (rk <= 64) {               // two tokens side by side, four pairs in flight
+                const int j = (lane & 15) * 4;
+#pragma unroll
+                for (int b = 0; b < 16; b += 8) {
+                    float4 v[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+                    for (int part = 0; part < parts; ++part)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int r = r0 + b + 2 * e + (lane >> 4);
+                            if (r < count && j < rk) add4(v[e], *reinterpret_cast<const float4*>(S + part * part_step + (size_t)r * p.r + j));
+                        }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int r = r0 + b + 2 * e + (lane >> 4);
+                        float top = max4_abs(v[e]);
+#pragma unroll
+                        for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                        const RowFactor f = row_factor(top);
+                        if (r < count && j < rk) put(r, j, v[e], f.up);
+                        if (j == 0) row_factors[r] = f.down * alpha;
+                    }
+                }
+            } else {
+#pragma unroll 1
+                for (int b = 0; b < 16; b += 2) {
+                    float4 v[2][2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) v[e][0] = v[e][1] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+                    for (int part = 0; part < parts; ++part)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e)
+#pragma unroll
+                            for (int c = 0; c < 2; ++c) {
+                                const int r = r0 + b + e, j = c * 128 + lane * 4;
+                                if (r < count && j < rk) add4(v[e][c], *reinterpret_cast<const float4*>(S + part * part_step + (size_t)r * p.r + j));
+                            }
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int r = r0 + b + e;
+                        const RowFactor f = row_factor(warp_max(fmaxf(max4_abs(v[e][0]), max4_abs(v[e][1]))));
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) {
+                            const int j = c * 128 + lane * 4;
+                            if (r < count && j < rk) put(r, j, v[e][c], f.up);
+                        }
+                        if (lane == 0) row_factors[r] = f.down * alpha;
+                    }
+                }
+            }
+            fence_proxy_async_smem();
+            named_bar_sync(1, 256);
+            if (lane == 0) mbar_arrive(s_there);
+        }
+        const float factor = row_factors[row];
         // lines are written by eight lanes each: this lane's 16 bytes of rows q 32 + lane / 8, + 4, ...
         const int wr = q * 32 + (lane >> 3), wc = lane & 7;
         int out_tok[8];
@@ -395,7 +406,6 @@ adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, i
             there |= wr + 4 * e < count ? 1u << e : 0u;
         }
         const bool box = t4.w >= 0 && (q + 1) * 32 <= count;
-        int kept = -1;
         bool ok = true;
         for (int i = (warp - 2) >> 2; i < n; i += 2) {
             const int s = i % stages, h = i % kUpSums;
@@ -445,16 +455,10 @@ adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, i
                 if (lane == 0) {
                     tma_store_2d_tile(&maps.out, ch, t4.w + q * 32, at + (uint32_t)(q * 32 * 128));
                     bulk_store_commit();
-                    // its place is given back with this warp's next block, two on, which a ring of three stages reaches without it
-                    if (stages >= 30) {
-                        bulk_store_wait_read_but<1>();
-                        if (kept >= 0) mbar_arrive(free_(kept));
-                    } else {
-                        bulk_store_wait_read();
-                        mbar_arrive(free_(s));
-                    }
+                    // (giving the place back only with this warp's next block cost more in copies not yet asked for)
+                    bulk_store_wait_read();
+                    mbar_arrive(free_(s));
                 }
-                kept = s;
                 continue;
             }
             const bool in = ch + wc * 8 < p.N;
@@ -475,7 +479,6 @@ adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, i
                 if (in && (there >> e & 1)) *reinterpret_cast<uint4*>(p.out + (size_t)out_tok[e] * p.ldo + (ch + wc * 8)) = o[e];
             }
         }
-        if (box && lane == 0) bulk_store_wait_read();        // nobody leaves before its shared memory has been read
     }
     __syncwarp();
     tc_fence_before();
@@ -485,8 +488,8 @@ adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, i
     if (warp == 0) tmem_free(tmem, kUpTmem);
 }
 
-// Tiles that a call probably has: half of the adapters leave a short one.
-int likely_tiles(const AdapterParams& p) { return p.M / kTok + ((p.n_slots < p.M ? p.n_slots : p.M) + 1) / 2; }
+// CTAs that the tiles of the first kernel are dealt to (the bound is the workspace's).
+int down_ctas(int num_sms) { return num_sms < kMaxDownCtas ? num_sms : kMaxDownCtas; }
 
 template <typename Kernel>
 int opt_in(Kernel* kernel, int bytes, bool (&configured)[kMaxDevices], int* num_sms) {
@@ -498,31 +501,6 @@ int opt_in(Kernel* kernel, int bytes, bool (&configured)[kMaxDevices], int* num_
     if (e != cudaSuccess) return record_cuda_error(e, "adapters smem attribute");
     configured[dev] = true;
     return ASER_OK;
-}
-
-// Clusters of CL CTAs of the first kernel that are resident at once.
-int active_clusters(int CL) {
-    static int cached[kMaxDevices][kMaxCL + 1];       // 0: not asked yet
-    int dev = 0;
-    if (current_device(&dev) != ASER_OK) return 0;
-    if (cached[dev][CL] == 0) {
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3(CL, 1, 1);
-        cfg.blockDim = dim3(kDownThreads, 1, 1);
-        cfg.dynamicSmemBytes = kDownSmem;
-        cudaLaunchAttribute attr[1];
-        attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim.x = CL; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-        cfg.attrs = attr;
-        cfg.numAttrs = 1;
-        int n = 0;
-        if (cudaOccupancyMaxActiveClusters(&n, adapters_down_kernel, &cfg) != cudaSuccess) {
-            (void)cudaGetLastError();
-            n = 0;
-        }
-        cached[dev][CL] = n > 0 ? n : -1;
-    }
-    return cached[dev][CL] > 0 ? cached[dev][CL] : 0;
 }
 
 }  // namespace
@@ -538,24 +516,20 @@ int launch_adapters_down(const AdapterParams& p, cudaStream_t st) {
     if (rc == ASER_OK) rc = encode_map_2d_ld(&maps.x_one, f16, 2, p.X, p.M, p.K, p.ldx, 1, kCols, CU_TENSOR_MAP_SWIZZLE_128B);
     if (rc == ASER_OK) rc = encode_map_2d(&maps.a, f16, 2, p.A, (uint64_t)p.n_slots * p.r, p.K, 16, kCols, CU_TENSOR_MAP_SWIZZLE_128B);
     if (rc != ASER_OK) return rc;
-    // as many CTAs to a tile as let the tiles that are likely run at once; a CTA has two steps of K at least
-    int CL = kMaxCL;
-    while (CL > 1 && (likely_tiles(p) > active_clusters(CL) || p.K / kCols < 2 * CL)) --CL;
     uint32_t cols = 32;
     while ((int)cols < p.r) cols *= 2;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(plan_tiles(p.M, p.n_slots, kTok) * CL, 1, 1);
+    const int ctas = down_ctas(num_sms), bound = plan_tiles(p.M, p.n_slots, kTok);
+    cfg.gridDim = dim3(ctas > bound ? ctas : bound, 1, 1);
     cfg.blockDim = dim3(kDownThreads, 1, 1);
     cfg.dynamicSmemBytes = kDownSmem;
     cfg.stream = st;
-    cudaLaunchAttribute attr[2];
+    cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = CL; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 2;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, adapters_down_kernel, maps, p, down_stages(p.r), cols);
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, adapters_down_kernel, maps, p, down_stages(p.r), ctas, cols);
     if (e != cudaSuccess) return record_cuda_error(e, "adapters_down_kernel");
     return check_launch("adapters_down_kernel");
 }
@@ -569,7 +543,6 @@ int launch_adapters_up(const AdapterParams& p, cudaStream_t st) {
     const CUtensorMapDataType f16 = CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
     rc = encode_map_2d_ld(&maps.y, f16, 2, p.Y, p.M, p.N, p.ldy, kBox, kCols, CU_TENSOR_MAP_SWIZZLE_128B);
     if (rc == ASER_OK) rc = encode_map_2d_ld(&maps.y_one, f16, 2, p.Y, p.M, p.N, p.ldy, 1, kCols, CU_TENSOR_MAP_SWIZZLE_128B);
-    if (rc == ASER_OK) rc = encode_map_2d(&maps.s, f16, 2, p.S, p.M, p.r, kBox, 64, CU_TENSOR_MAP_SWIZZLE_128B);
     if (rc == ASER_OK) rc = encode_map_2d(&maps.b, f16, 2, p.B, (uint64_t)p.n_slots * p.N, p.r, kCols, 64, CU_TENSOR_MAP_SWIZZLE_128B);
     if (rc != ASER_OK) return rc;
     rc = encode_map_2d_ld(&maps.out, f16, 2, p.out, p.M, p.N, p.ldo, kBox, kCols, CU_TENSOR_MAP_SWIZZLE_128B);
@@ -585,7 +558,7 @@ int launch_adapters_up(const AdapterParams& p, cudaStream_t st) {
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, adapters_up_kernel, maps, p, resident);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, adapters_up_kernel, maps, p, resident, down_ctas(num_sms));
     if (e != cudaSuccess) return record_cuda_error(e, "adapters_up_kernel");
     return check_launch("adapters_up_kernel");
 }

@@ -71,9 +71,6 @@ __device__ __forceinline__ void tma_store_2d_tile(const CUtensorMap* map, int x,
                  ::"l"(map), "r"(x), "r"(y), "r"(src) : "memory");
 }
 __device__ __forceinline__ void bulk_store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
-// All but the last N groups of this thread's bulk stores have read their source.
-template <int N>
-__device__ __forceinline__ void bulk_store_wait_read_but() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory"); }
 // This thread's bulk stores have read their source / have completed.
 __device__ __forceinline__ void bulk_store_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 __device__ __forceinline__ void bulk_store_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
