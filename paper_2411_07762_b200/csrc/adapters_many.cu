@@ -79,7 +79,6 @@ __device__ __forceinline__ TileRows tile_rows(const int4& t4, const int32_t* tok
     return r;
 }
 
-__device__ __forceinline__ void add4(float4& a, const float4& b) { a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w; }
 __device__ __forceinline__ uint32_t pack_half2(float a, float b) {
     const __half2 h = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&h);
@@ -211,16 +210,79 @@ adapters_down_kernel(const __grid_constant__ DownMaps maps, const AdapterParams 
 }
 
 // ---------------------------------------------------------------------------
+// S from its parts
+// ---------------------------------------------------------------------------
+// In a launch of its own, 16 tokens to a CTA and two to a warp: every CTA of the second product adding them up for itself took 5 to
+// 10 us, most of it the same loads again.
+constexpr int kSumThreads = 256, kSumTokens = 16;
+
+__global__ void __launch_bounds__(kSumThreads)
+adapters_sum_kernel(const AdapterParams p, int ctas) {
+    grid_dep_wait();
+    grid_dep_launch();
+    warm_ranks(p);
+    const int tile = (int)blockIdx.x / (kTok / kSumTokens), r0 = ((int)blockIdx.x % (kTok / kSumTokens)) * kSumTokens;
+    const PlanView plan = plan_view(p.plan, p.M, p.n_slots);
+    const int4 head = *reinterpret_cast<const int4*>(p.plan), more = *reinterpret_cast<const int4*>(p.plan + 4);
+    const int4 t4 = plan.tiles_many[tile];
+    if (head.x != p.M || head.y != p.n_slots || tile >= more.x || r0 >= t4.z) return;
+    const int slot = t4.x, first = t4.y, count = t4.z, rk = adapter_rank(p, slot);
+    if (rk == 0) return;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, parts = down_parts(more.x, ctas, p.K);
+    const float alpha = p.scale ? __ldg(p.scale + slot) : 1.f;
+    const size_t part_step = (size_t)more.y * p.r;
+    // eight parts in flight, added in their order
+    auto sum = [&](int row, int j, bool there) {
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        const float* from = p.S + (size_t)(first + row) * p.r + j;
+        for (int part = 0; part < parts; part += 8) {
+            float4 a[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                a[e] = there && part + e < parts ? *reinterpret_cast<const float4*>(from + (part + e) * part_step) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) { v.x += a[e].x; v.y += a[e].y; v.z += a[e].z; v.w += a[e].w; }
+        }
+        return v;
+    };
+    if (rk <= 64) {                   // two tokens side by side
+        const int row = r0 + warp * 2 + (lane >> 4), j = (lane & 15) * 4;
+        const bool there = row < count && j < rk;
+        const float4 v = sum(row, j, there);
+        float top = max4_abs(v);
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const RowFactor f = row_factor(top);
+        if (there) *reinterpret_cast<uint2*>(p.S16 + (size_t)(first + row) * p.r + j) = scaled_f16(v, f.up);
+        if (there && j == 0) p.row_scale[first + row] = f.down * alpha;
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int row = r0 + warp * 2 + i;
+        float4 v[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) v[h] = sum(row, h * 128 + lane * 4, row < count && h * 128 + lane * 4 < rk);
+        const RowFactor f = row_factor(warp_max(fmaxf(max4_abs(v[0]), max4_abs(v[1]))));
+        if (row >= count) continue;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if (h * 128 + lane * 4 < rk) *reinterpret_cast<uint2*>(p.S16 + (size_t)(first + row) * p.r + h * 128 + lane * 4) = scaled_f16(v[h], f.up);
+        if (lane == 0) p.row_scale[first + row] = f.down * alpha;
+    }
+}
+
+// ---------------------------------------------------------------------------
 // out = Y + B S
 // ---------------------------------------------------------------------------
 constexpr int kUpWarps = 10, kUpThreads = kUpWarps * 32;      // copies, products, twice four that finish blocks in turn
 
-struct UpMaps { CUtensorMap y, y_one, b, out; };
+struct UpMaps { CUtensorMap y, y_one, s, b, out; };
 
 __host__ __device__ constexpr int up_chunks(int r) { return (r + 63) / 64; }          // blocks of 64 ranks
 // Shared memory of a CTA: S, then as many stages as there is room for; they are as large as the tile's tokens and the adapter's
 // rank ask (128 tokens of rank 64: four, 64 tokens: six).  Up to rank 128 two CTAs share an SM.
-constexpr int kUpTail = 256 + kTok * 4;
+constexpr int kUpTail = 256;
 __host__ __device__ constexpr int up_smem(int r) { return (r <= 128 ? 112 : 224) * 1024; }
 static_assert(up_smem(128) - kUpTail - 1024 >= up_chunks(128) * kTok * 128 + 2 * (kRowsBytes + up_chunks(128) * kCols * 128), "two stages at least");
 static_assert(up_smem(256) - kUpTail - 1024 >= up_chunks(256) * kTok * 128 + 2 * (kRowsBytes + up_chunks(256) * kCols * 128), "two stages at least");
@@ -230,7 +292,7 @@ constexpr uint32_t kUpTmem = kUpSums * kCols;
 // Blocks of 64 channels [c n / chunks, (c + 1) n / chunks) of a tile; `resident` CTAs are dealt over the tiles that there are.  What wrote Y and the plan is known to be complete when this
 // kernel starts, because the first kernel waited for it; S is waited for.
 __global__ void __launch_bounds__(kUpThreads, 2)
-adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, int resident, int ctas) {
+adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, int resident) {
     extern __shared__ uint8_t smem_raw[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     warm_ranks(p);
@@ -271,19 +333,19 @@ adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, i
     auto read = [&](int h) { return bar0 + 8u * (2 * kMaxStages + h); };        // a block's sums have been read (four warps)
     auto full = [&](int h) { return bar0 + 8u * (2 * kMaxStages + kUpSums + h); };    // ... are complete
     constexpr int kBars = 2 * kMaxStages + 2 * kUpSums + 1;
-    static_assert(kBars <= 32 && kBars * 8 + 8 <= 256, "barriers");
-    const uint32_t s_there = bar0 + 8u * (kBars - 1);                           // S is there (eight warps)
-    float* row_factors = reinterpret_cast<float*>(smem + room + 256);
+    static_assert(kBars <= 32 && kBars * 8 + 8 <= kUpTail, "barriers");
+    const uint32_t s_there = bar0 + 8u * (kBars - 1);
     if (warp == 0) {
         tmem_alloc(tmem_slot, kUpTmem);
     } else if (warp == 1) {
-        if (lane < kBars) mbar_init(bar0 + 8u * lane, lane >= kMaxStages && lane < 2 * kMaxStages + kUpSums ? 4 : lane == kBars - 1 ? 8 : 1);
+        if (lane < kBars) mbar_init(bar0 + 8u * lane, lane >= kMaxStages && lane < 2 * kMaxStages + kUpSums ? 4 : 1);
         if (lane == 0) *stop = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_proxy_async_smem();
     } else if (warp == 2 && lane == 0) {
         prefetch_tensormap(&maps.y);
         prefetch_tensormap(&maps.b);
+        prefetch_tensormap(&maps.s);
     }
     tc_fence_before();
     __syncthreads();
@@ -292,7 +354,17 @@ adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, i
     if (warp == 0) {                      // copies
         const TileRows rows = tile_rows(t4, plan.tokens, lane);
         const uint32_t bytes = (uint32_t)rows.rows() * 128u + (uint32_t)kch * kCols * 128u;
+        bool asked = false;
+        auto ask_for_s = [&]() {          // once the ring is full: this waits for the first kernel
+            asked = true;
+            grid_dep_wait();
+            if (lane == 0) mbar_arrive_expect_tx(s_there, (uint32_t)(kch * row_bytes));
+            __syncwarp();
+            const int boxes = row_bytes / (kBox * 128);
+            if (lane < kch * boxes) tma_load_2d(sb + lane * kBox * 128, &maps.s, lane / boxes * 64, first + lane % boxes * kBox, s_there);
+        };
         for (int i = 0, s = 0, turn = 0; i < n; ++i) {
+            if (i == stages) ask_for_s();
             if (turn > 0 && !warp_wait(free_(s), (uint32_t)(turn - 1) & 1u, stop, lane)) break;
             if (lane == 0) mbar_arrive_expect_tx(filled(s), bytes);
             __syncwarp();
@@ -302,6 +374,8 @@ adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, i
             if (lane < kch) tma_load_2d(at + row_bytes + lane * kCols * 128, &maps.b, lane * 64, slot * p.N + ch, filled(s));
             if (++s == stages) { s = 0; ++turn; }
         }
+        if (!asked) ask_for_s();
+        grid_dep_launch();
     } else if (warp == 1) {               // products
         const uint32_t idesc = make_idesc(1, 0, 128, kCols);
         bool ok = warp_wait(s_there, 0u, stop, lane);
@@ -326,76 +400,8 @@ adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, i
     } else {
         const int q = warp & 3;           // a quarter of the tokens (of tensor memory's lanes), every other block
         const int row = q * 32 + lane;
-        // ---- S: the parts are added, scaled and rounded, 16 tokens to a warp, into the swizzled layout of an operand ----
-        grid_dep_wait();
-        grid_dep_launch();
-        {
-            const int parts = down_parts(more.x, ctas, p.K), r0 = (warp - 2) * 16;
-            const float alpha = p.scale ? __ldg(p.scale + slot) : 1.f;
-            const float* S = p.S + (size_t)first * p.r;
-            const size_t part_step = (size_t)more.y * p.r;
-            auto put = [&](int r, int j, const float4& v, float up) {
-                const uint2 o = scaled_f16(v, up);
-                *reinterpret_cast<uint2*>(smem + (j >> 6) * row_bytes + r * 128 + ((((j >> 3) & 7) ^ (r & 7)) << 4) + (j & 7) * 2) = o;
-            };
-            if (rk <= 64) {               // two tokens side by side, four pairs in flight
-                const int j = (lane & 15) * 4;
-#pragma unroll
-                for (int b = 0; b < 16; b += 8) {
-                    float4 v[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 2
-                    for (int part = 0; part < parts; ++part)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int r = r0 + b + 2 * e + (lane >> 4);
-                            if (r < count && j < rk) add4(v[e], *reinterpret_cast<const float4*>(S + part * part_step + (size_t)r * p.r + j));
-                        }
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int r = r0 + b + 2 * e + (lane >> 4);
-                        float top = max4_abs(v[e]);
-#pragma unroll
-                        for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                        const RowFactor f = row_factor(top);
-                        if (r < count && j < rk) put(r, j, v[e], f.up);
-                        if (j == 0) row_factors[r] = f.down * alpha;
-                    }
-                }
-            } else {
-#pragma unroll 1
-                for (int b = 0; b < 16; b += 2) {
-                    float4 v[2][2];
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) v[e][0] = v[e][1] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 2
-                    for (int part = 0; part < parts; ++part)
-#pragma unroll
-                        for (int e = 0; e < 2; ++e)
-#pragma unroll
-                            for (int c = 0; c < 2; ++c) {
-                                const int r = r0 + b + e, j = c * 128 + lane * 4;
-                                if (r < count && j < rk) add4(v[e][c], *reinterpret_cast<const float4*>(S + part * part_step + (size_t)r * p.r + j));
-                            }
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const int r = r0 + b + e;
-                        const RowFactor f = row_factor(warp_max(fmaxf(max4_abs(v[e][0]), max4_abs(v[e][1]))));
-#pragma unroll
-                        for (int c = 0; c < 2; ++c) {
-                            const int j = c * 128 + lane * 4;
-                            if (r < count && j < rk) put(r, j, v[e][c], f.up);
-                        }
-                        if (lane == 0) row_factors[r] = f.down * alpha;
-                    }
-                }
-            }
-            fence_proxy_async_smem();
-            named_bar_sync(1, 256);
-            if (lane == 0) mbar_arrive(s_there);
-        }
-        const float factor = row_factors[row];
+        grid_dep_wait();                  // the factors come from the first kernel
+        const float factor = row < count ? p.row_scale[first + row] : 0.f;
         // lines are written by eight lanes each: this lane's 16 bytes of rows q 32 + lane / 8, + 4, ...
         const int wr = q * 32 + (lane >> 3), wc = lane & 7;
         int out_tok[8];
@@ -529,8 +535,13 @@ int launch_adapters_down(const AdapterParams& p, cudaStream_t st) {
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, adapters_down_kernel, maps, p, down_stages(p.r), ctas, cols);
+    cudaError_t e = cudaLaunchKernelEx(&cfg, adapters_down_kernel, maps, p, down_stages(p.r), ctas, cols);
     if (e != cudaSuccess) return record_cuda_error(e, "adapters_down_kernel");
+    cfg.gridDim = dim3(bound * (kTok / kSumTokens), 1, 1);
+    cfg.blockDim = dim3(kSumThreads, 1, 1);
+    cfg.dynamicSmemBytes = 0;
+    e = cudaLaunchKernelEx(&cfg, adapters_sum_kernel, p, ctas);
+    if (e != cudaSuccess) return record_cuda_error(e, "adapters_sum_kernel");
     return check_launch("adapters_down_kernel");
 }
 
@@ -543,6 +554,7 @@ int launch_adapters_up(const AdapterParams& p, cudaStream_t st) {
     const CUtensorMapDataType f16 = CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
     rc = encode_map_2d_ld(&maps.y, f16, 2, p.Y, p.M, p.N, p.ldy, kBox, kCols, CU_TENSOR_MAP_SWIZZLE_128B);
     if (rc == ASER_OK) rc = encode_map_2d_ld(&maps.y_one, f16, 2, p.Y, p.M, p.N, p.ldy, 1, kCols, CU_TENSOR_MAP_SWIZZLE_128B);
+    if (rc == ASER_OK) rc = encode_map_2d(&maps.s, f16, 2, p.S16, p.M, p.r, kBox, 64, CU_TENSOR_MAP_SWIZZLE_128B);
     if (rc == ASER_OK) rc = encode_map_2d(&maps.b, f16, 2, p.B, (uint64_t)p.n_slots * p.N, p.r, kCols, 64, CU_TENSOR_MAP_SWIZZLE_128B);
     if (rc != ASER_OK) return rc;
     rc = encode_map_2d_ld(&maps.out, f16, 2, p.out, p.M, p.N, p.ldo, kBox, kCols, CU_TENSOR_MAP_SWIZZLE_128B);
@@ -558,7 +570,7 @@ int launch_adapters_up(const AdapterParams& p, cudaStream_t st) {
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, adapters_up_kernel, maps, p, resident, down_ctas(num_sms));
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, adapters_up_kernel, maps, p, resident);
     if (e != cudaSuccess) return record_cuda_error(e, "adapters_up_kernel");
     return check_launch("adapters_up_kernel");
 }
