@@ -402,18 +402,12 @@ bool adapters_many(int M, int n_slots) {
     return M > 24 * used;
 }
 
-// Sums of S in up to kMaxParts parts: as many as make no more CTAs than kMaxDownCtas, of 128 tokens each.
-size_t adapters_workspace_bytes(int M, int r, int n_slots) {
-    if (!adapters_many(M, n_slots)) return 0;
-    const size_t split = (size_t)M * kMaxParts, most = (size_t)kMaxDownCtas * kTileMany, rows = split < most ? split : (size_t)M > most ? (size_t)M : most;
-    return (size_t)M * 2 * r + ((size_t)M + 3) / 4 * 16 + rows * r * 4;
-}
+size_t adapters_workspace_bytes(int M, int r, int n_slots) { return adapters_many(M, n_slots) ? (size_t)M * (2 * r + 4) : 0; }
 
 int launch_adapters(AdapterParams p, void* workspace, cudaStream_t st) {
     if (!adapters_many(p.M, p.n_slots)) return launch_few(p, st);
-    p.S16 = static_cast<__half*>(workspace);
+    p.S = static_cast<__half*>(workspace);
     p.row_scale = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + (size_t)p.M * 2 * p.r);
-    p.S = p.row_scale + ((size_t)p.M + 3) / 4 * 4;
     const int rc = launch_adapters_down(p, st);
     return rc != ASER_OK ? rc : launch_adapters_up(p, st);
 }

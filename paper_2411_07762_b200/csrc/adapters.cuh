@@ -10,7 +10,6 @@
 namespace aser {
 
 constexpr int kTileFew = 16, kTileMany = 128;
-constexpr int kMaxParts = 16, kMaxDownCtas = 160;      // many tokens: parts of K, CTAs that they are dealt to
 
 constexpr int kFewWords = 4 + kTileFew;
 
@@ -44,8 +43,7 @@ struct AdapterParams {
     const int32_t* plan;
     const __half* Y;
     __half* out;
-    float* S;                 // between the kernels for many tokens: [parts of K][tokens with an adapter][r],
-    __half* S16;              // then [M, r] by place in the plan's list, scaled,
+    __half* S;                // between the two kernels for many tokens: [M, r] by place in the plan's list, scaled,
     float* row_scale;         // and [M] what its rows are to be multiplied by
     size_t ldx, ldy, ldo;
     int M, N, K, r, n_slots;
@@ -54,10 +52,10 @@ struct AdapterParams {
 
 size_t adapters_plan_bytes(int M, int n_slots);
 int launch_adapters_plan(const int32_t* slot, int M, int n_slots, void* plan, cudaStream_t st);
-// Whether a call runs the three kernels for many tokens, and the workspace that it then needs.
+// Whether a call runs the two kernels for many tokens, and the workspace that it then needs.
 bool adapters_many(int M, int n_slots);
 size_t adapters_workspace_bytes(int M, int r, int n_slots);
-// (p.S, p.S16 and p.row_scale are set from `workspace`.)
+// (p.S and p.row_scale are set from `workspace`.)
 int launch_adapters(AdapterParams p, void* workspace, cudaStream_t st);
 int launch_adapters_down(const AdapterParams& p, cudaStream_t st);
 int launch_adapters_up(const AdapterParams& p, cudaStream_t st);

@@ -21,7 +21,7 @@ namespace aser {
 
 namespace {
 
-constexpr int kTok = kTileMany, kBox = 32;
+constexpr int kTok = kTileMany, kMaxCL = 8, kBox = 32;
 constexpr int kCols = 64;                            // columns or channels of a stage: 128 bytes a row
 constexpr int kRowsBytes = kTok * kCols * 2;
 constexpr int kMaxStages = 8;
@@ -100,24 +100,21 @@ constexpr int kDownThreads = 256, kDownWarps = 8;
 struct DownMaps { CUtensorMap x, x_one, a; };
 
 __host__ __device__ constexpr int down_stage_bytes(int r) { return kRowsBytes + r * kCols * 2; }
-// A CTA has an SM to itself: two of them side by side left other SMs idle.
+// The ring also holds the partial sums at the end, [128][rank + 4] floats.  Up to rank 128 two CTAs fit on an SM, so that clusters
+// beyond those that have SMs of their own need not wait for a second turn (CTAs with an SM's shared memory each, 36 clusters of four
+// where 35 fit: 41.5 us instead of 35.2 for the call above), and a CTA of the second kernel fits beside one of these.
 constexpr int kDownTail = 2 * kMaxStages * 8 + 32;   // barriers, tensor memory's address, flag
-constexpr int kDownSmem = 224 * 1024;
+constexpr int down_smem(int r) { return (r <= 128 ? 112 : 224) * 1024; }
 constexpr int down_stages(int r) {
-    const int fit = (kDownSmem - kDownTail - 1024) / down_stage_bytes(r);
+    const int fit = (down_smem(r) - kDownTail - 1024) / down_stage_bytes(r);
     return fit < kMaxStages ? fit : kMaxStages;
 }
-static_assert(down_stages(256) >= 4, "a ring");
+static_assert(down_stages(128) >= 3 && down_stages(256) >= 4, "a ring");
+static_assert(2 * (down_smem(128) + 1024) <= 228 * 1024, "two CTAs to an SM");
+static_assert(3 * down_stage_bytes(128) >= kTok * 132 * 4 && 4 * down_stage_bytes(256) >= kTok * 260 * 4, "partial sums");
 
-// Parts of K that a tile's sums are made in, at least two steps each: as many as `ctas` serve at once.
-__device__ __forceinline__ int down_parts(int tiles, int ctas, int K) {
-    const int steps = K / kCols, by_ctas = ctas / tiles, by_steps = steps / 2;
-    const int parts = by_ctas < by_steps ? by_ctas : by_steps;
-    return parts < 1 ? 1 : parts > kMaxParts ? kMaxParts : parts;
-}
-
-__global__ void __launch_bounds__(kDownThreads, 1)
-adapters_down_kernel(const __grid_constant__ DownMaps maps, const AdapterParams p, int stages, int ctas, uint32_t tmem_cols) {
+__global__ void __launch_bounds__(kDownThreads, 2)
+adapters_down_kernel(const __grid_constant__ DownMaps maps, const AdapterParams p, int stages, uint32_t tmem_cols) {
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const int stage_bytes = down_stage_bytes(p.r);
@@ -146,16 +143,15 @@ adapters_down_kernel(const __grid_constant__ DownMaps maps, const AdapterParams 
     grid_dep_wait();
     grid_dep_launch();
     warm_ranks(p);
+    const int CL = (int)cluster_size(), rank = (int)cluster_rank(), tile = (int)blockIdx.x / CL;
     const PlanView plan = plan_view(p.plan, p.M, p.n_slots);
-    const int4 head = *reinterpret_cast<const int4*>(p.plan), more = *reinterpret_cast<const int4*>(p.plan + 4);
-    const int tiles = head.x == p.M && head.y == p.n_slots ? more.x : 0, parts = tiles > 0 ? down_parts(tiles, ctas, p.K) : 1;
-    const int tile = (int)blockIdx.x / parts, part = (int)blockIdx.x - tile * parts;
-    int4 t4 = make_int4(-1, 0, 0, 0);
-    if (tile < tiles) t4 = plan.tiles_many[tile];
-    const int slot = t4.x, first = t4.y, count = t4.z;
+    const int4 head = *reinterpret_cast<const int4*>(p.plan);
+    const int4 t4 = plan.tiles_many[tile];
+    const bool real = head.x == p.M && head.y == p.n_slots && tile < head.w;
+    const int slot = real ? t4.x : -1, first = t4.y, count = t4.z;
     const int rk = slot < 0 ? 0 : adapter_rank(p, slot);
-    if (rk > 0) {
-        const int steps = p.K / kCols, s0 = part * steps / parts, n = (part + 1) * steps / parts - s0;
+    if (rk > 0) {                     // (the whole cluster)
+        const int steps = p.K / kCols, s0 = rank * steps / CL, n = (rank + 1) * steps / CL - s0;
         if (warp == 0) {              // copies
             const TileRows rows = tile_rows(t4, plan.tokens, lane);
             const uint32_t bytes = (uint32_t)(rows.rows() + rk) * 128u;
@@ -186,90 +182,105 @@ adapters_down_kernel(const __grid_constant__ DownMaps maps, const AdapterParams 
                 if (++s == stages) { s = 0; ++turn; }
             }
         }
-        const bool ok = warp_wait(smem_u32(done), 0u, stop, lane);
+        bool ok = true;
+        if (n > 0) ok = warp_wait(smem_u32(done), 0u, stop, lane);
+        __syncthreads();                  // the ring is free
+        if (*stop) { ok = false; let_copies_land(); }
         tc_fence_after();
-        // the sums leave as they are: a token to a thread, 16 ranks at a time
-        const int row = (warp & 3) * 32 + lane;
-        float* to = p.S + ((size_t)part * more.y + first + row) * p.r;
+        // partial sums [128 tokens][rk + 4]
+        float* part = reinterpret_cast<float*>(smem);
+        const int stride = rk + 4;
         for (int c = (warp >> 2) * 16; c < rk; c += 32) {
             uint32_t v[16];
-            tmem_ld16(tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)c, v);
-            tmem_wait_ld(v);
-            if (row < count)
 #pragma unroll
-                for (int e = 0; e < 16; e += 4)
-                    *reinterpret_cast<uint4*>(to + c + e) = ok ? make_uint4(v[e], v[e + 1], v[e + 2], v[e + 3])
-                                                               : make_uint4(0x7fffffffu, 0x7fffffffu, 0x7fffffffu, 0x7fffffffu);
+            for (int e = 0; e < 16; ++e) v[e] = 0u;
+            if (n > 0) {
+                tmem_ld16(tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)c, v);
+                tmem_wait_ld(v);
+            }
+            uint4* q = reinterpret_cast<uint4*>(part + ((warp & 3) * 32 + lane) * stride + c);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t nan = 0x7fffffffu;
+                q[e] = ok ? make_uint4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]) : make_uint4(nan, nan, nan, nan);
+            }
         }
         tc_fence_before();
-        __syncthreads();
-        if (*stop) let_copies_land();
+        cluster_arrive();
+        cluster_wait();
+        const int per = (kTok + CL - 1) / CL;
+        const float alpha = p.scale ? __ldg(p.scale + slot) : 1.f;
+        auto gather = [&](int row, int j) {
+            const uint32_t at = smem_u32(part + row * stride + j);
+            float4 a[kMaxCL], v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int q = 0; q < kMaxCL; ++q) a[q] = q < CL ? ld_cluster_f32x4(map_to_rank(at, q)) : v;
+#pragma unroll
+            for (int q = 0; q < kMaxCL; ++q) { v.x += a[q].x; v.y += a[q].y; v.z += a[q].z; v.w += a[q].w; }
+            return v;
+        };
+        auto gather2 = [&](int row, int step, int j, const bool (&mine)[2], float4 (&v)[2]) {
+            float4 a[2][kMaxCL];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const uint32_t at = smem_u32(part + (mine[u] ? row + u * step : 0) * stride + j);
+#pragma unroll
+                for (int q = 0; q < kMaxCL; ++q)
+                    a[u][q] = q < CL && mine[u] ? ld_cluster_f32x4(map_to_rank(at, q)) : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int q = 0; q < kMaxCL; ++q) { v[u].x += a[u][q].x; v[u].y += a[u][q].y; v[u].z += a[u][q].z; v[u].w += a[u][q].w; }
+            }
+        };
+        if (rk <= 64) {                   // two tokens side by side, twice
+            const int j = (lane & 15) * 4;
+            for (int i0 = warp * 2; i0 < per; i0 += 4 * kDownWarps) {
+                float4 v[2];
+                bool mine[2];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int i = i0 + u * 2 * kDownWarps + (lane >> 4);
+                    mine[u] = i < per && rank * per + i < count && j < rk;
+                }
+                gather2(rank * per + i0 + (lane >> 4), 2 * kDownWarps, j, mine, v);
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int row = rank * per + i0 + u * 2 * kDownWarps + (lane >> 4);
+                    float top = max4_abs(v[u]);
+#pragma unroll
+                    for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                    const RowFactor f = row_factor(top);
+                    if (mine[u]) *reinterpret_cast<uint2*>(p.S + (size_t)(first + row) * p.r + j) = scaled_f16(v[u], f.up);
+                    if (mine[u] && j == 0) p.row_scale[first + row] = f.down * alpha;
+                }
+            }
+        } else {
+            for (int i = warp; i < per && rank * per + i < count; i += kDownWarps) {
+                const int row = rank * per + i;
+                float4 v[2];
+                float top = 0.f;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    v[h] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (h * 128 + lane * 4 < rk) v[h] = gather(row, h * 128 + lane * 4);
+                    top = fmaxf(top, max4_abs(v[h]));
+                }
+                const RowFactor f = row_factor(warp_max(top));
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    if (h * 128 + lane * 4 < rk)
+                        *reinterpret_cast<uint2*>(p.S + (size_t)(first + row) * p.r + h * 128 + lane * 4) = scaled_f16(v[h], f.up);
+                if (lane == 0) p.row_scale[first + row] = f.down * alpha;
+            }
+        }
+        cluster_arrive();                 // nobody leaves while a peer may still read its sums
+        cluster_wait();
         tc_fence_after();
     }
     if (warp == 0) tmem_free(tmem, tmem_cols);
-}
-
-// ---------------------------------------------------------------------------
-// S from its parts
-// ---------------------------------------------------------------------------
-// In a launch of its own, 16 tokens to a CTA and two to a warp: every CTA of the second product adding them up for itself took 5 to
-// 10 us, most of it the same loads again.
-constexpr int kSumThreads = 256, kSumTokens = 16;
-
-__global__ void __launch_bounds__(kSumThreads)
-adapters_sum_kernel(const AdapterParams p, int ctas) {
-    grid_dep_wait();
-    grid_dep_launch();
-    warm_ranks(p);
-    const int tile = (int)blockIdx.x / (kTok / kSumTokens), r0 = ((int)blockIdx.x % (kTok / kSumTokens)) * kSumTokens;
-    const PlanView plan = plan_view(p.plan, p.M, p.n_slots);
-    const int4 head = *reinterpret_cast<const int4*>(p.plan), more = *reinterpret_cast<const int4*>(p.plan + 4);
-    const int4 t4 = plan.tiles_many[tile];
-    if (head.x != p.M || head.y != p.n_slots || tile >= more.x || r0 >= t4.z) return;
-    const int slot = t4.x, first = t4.y, count = t4.z, rk = adapter_rank(p, slot);
-    if (rk == 0) return;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, parts = down_parts(more.x, ctas, p.K);
-    const float alpha = p.scale ? __ldg(p.scale + slot) : 1.f;
-    const size_t part_step = (size_t)more.y * p.r;
-    // eight parts in flight, added in their order
-    auto sum = [&](int row, int j, bool there) {
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        const float* from = p.S + (size_t)(first + row) * p.r + j;
-        for (int part = 0; part < parts; part += 8) {
-            float4 a[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                a[e] = there && part + e < parts ? *reinterpret_cast<const float4*>(from + (part + e) * part_step) : make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) { v.x += a[e].x; v.y += a[e].y; v.z += a[e].z; v.w += a[e].w; }
-        }
-        return v;
-    };
-    if (rk <= 64) {                   // two tokens side by side
-        const int row = r0 + warp * 2 + (lane >> 4), j = (lane & 15) * 4;
-        const bool there = row < count && j < rk;
-        const float4 v = sum(row, j, there);
-        float top = max4_abs(v);
-#pragma unroll
-        for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        const RowFactor f = row_factor(top);
-        if (there) *reinterpret_cast<uint2*>(p.S16 + (size_t)(first + row) * p.r + j) = scaled_f16(v, f.up);
-        if (there && j == 0) p.row_scale[first + row] = f.down * alpha;
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int row = r0 + warp * 2 + i;
-        float4 v[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) v[h] = sum(row, h * 128 + lane * 4, row < count && h * 128 + lane * 4 < rk);
-        const RowFactor f = row_factor(warp_max(fmaxf(max4_abs(v[0]), max4_abs(v[1]))));
-        if (row >= count) continue;
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-            if (h * 128 + lane * 4 < rk) *reinterpret_cast<uint2*>(p.S16 + (size_t)(first + row) * p.r + h * 128 + lane * 4) = scaled_f16(v[h], f.up);
-        if (lane == 0) p.row_scale[first + row] = f.down * alpha;
-    }
 }
 
 // ---------------------------------------------------------------------------
@@ -494,8 +505,8 @@ adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, i
     if (warp == 0) tmem_free(tmem, kUpTmem);
 }
 
-// CTAs that the tiles of the first kernel are dealt to (the bound is the workspace's).
-int down_ctas(int num_sms) { return num_sms < kMaxDownCtas ? num_sms : kMaxDownCtas; }
+// Tiles that a call probably has (the host does not know which adapters are in use): a quarter of them leave a short one.
+int likely_tiles(const AdapterParams& p) { return (p.M + kTok - 1) / kTok + (p.n_slots < p.M ? p.n_slots : p.M) / 4; }
 
 template <typename Kernel>
 int opt_in(Kernel* kernel, int bytes, bool (&configured)[kMaxDevices], int* num_sms) {
@@ -514,7 +525,7 @@ int opt_in(Kernel* kernel, int bytes, bool (&configured)[kMaxDevices], int* num_
 int launch_adapters_down(const AdapterParams& p, cudaStream_t st) {
     static bool configured[kMaxDevices] = {false};
     int num_sms = 0;
-    int rc = opt_in(adapters_down_kernel, kDownSmem, configured, &num_sms);
+    int rc = opt_in(adapters_down_kernel, down_smem(256), configured, &num_sms);
     if (rc != ASER_OK) return rc;
     DownMaps maps;
     const CUtensorMapDataType f16 = CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
@@ -522,26 +533,27 @@ int launch_adapters_down(const AdapterParams& p, cudaStream_t st) {
     if (rc == ASER_OK) rc = encode_map_2d_ld(&maps.x_one, f16, 2, p.X, p.M, p.K, p.ldx, 1, kCols, CU_TENSOR_MAP_SWIZZLE_128B);
     if (rc == ASER_OK) rc = encode_map_2d(&maps.a, f16, 2, p.A, (uint64_t)p.n_slots * p.r, p.K, 16, kCols, CU_TENSOR_MAP_SWIZZLE_128B);
     if (rc != ASER_OK) return rc;
+    // about as many CTAs as there are SMs; each has two steps of K at least
+    int CL = (num_sms + num_sms / 10) / likely_tiles(p);
+    CL = CL > kMaxCL ? kMaxCL : CL;
+    CL = CL > p.K / kCols / 2 ? p.K / kCols / 2 : CL;
+    CL = CL < 1 ? 1 : CL;
     uint32_t cols = 32;
     while ((int)cols < p.r) cols *= 2;
     cudaLaunchConfig_t cfg = {};
-    const int ctas = down_ctas(num_sms), bound = plan_tiles(p.M, p.n_slots, kTok);
-    cfg.gridDim = dim3(ctas > bound ? ctas : bound, 1, 1);
+    cfg.gridDim = dim3(plan_tiles(p.M, p.n_slots, kTok) * CL, 1, 1);
     cfg.blockDim = dim3(kDownThreads, 1, 1);
-    cfg.dynamicSmemBytes = kDownSmem;
+    cfg.dynamicSmemBytes = down_smem(p.r);
     cfg.stream = st;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = CL; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    cudaError_t e = cudaLaunchKernelEx(&cfg, adapters_down_kernel, maps, p, down_stages(p.r), ctas, cols);
+    cfg.numAttrs = 2;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, adapters_down_kernel, maps, p, down_stages(p.r), cols);
     if (e != cudaSuccess) return record_cuda_error(e, "adapters_down_kernel");
-    cfg.gridDim = dim3(bound * (kTok / kSumTokens), 1, 1);
-    cfg.blockDim = dim3(kSumThreads, 1, 1);
-    cfg.dynamicSmemBytes = 0;
-    e = cudaLaunchKernelEx(&cfg, adapters_sum_kernel, p, ctas);
-    if (e != cudaSuccess) return record_cuda_error(e, "adapters_sum_kernel");
     return check_launch("adapters_down_kernel");
 }
 
@@ -554,7 +566,7 @@ int launch_adapters_up(const AdapterParams& p, cudaStream_t st) {
     const CUtensorMapDataType f16 = CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
     rc = encode_map_2d_ld(&maps.y, f16, 2, p.Y, p.M, p.N, p.ldy, kBox, kCols, CU_TENSOR_MAP_SWIZZLE_128B);
     if (rc == ASER_OK) rc = encode_map_2d_ld(&maps.y_one, f16, 2, p.Y, p.M, p.N, p.ldy, 1, kCols, CU_TENSOR_MAP_SWIZZLE_128B);
-    if (rc == ASER_OK) rc = encode_map_2d(&maps.s, f16, 2, p.S16, p.M, p.r, kBox, 64, CU_TENSOR_MAP_SWIZZLE_128B);
+    if (rc == ASER_OK) rc = encode_map_2d(&maps.s, f16, 2, p.S, p.M, p.r, kBox, 64, CU_TENSOR_MAP_SWIZZLE_128B);
     if (rc == ASER_OK) rc = encode_map_2d(&maps.b, f16, 2, p.B, (uint64_t)p.n_slots * p.N, p.r, kCols, 64, CU_TENSOR_MAP_SWIZZLE_128B);
     if (rc != ASER_OK) return rc;
     rc = encode_map_2d_ld(&maps.out, f16, 2, p.out, p.M, p.N, p.ldo, kBox, kCols, CU_TENSOR_MAP_SWIZZLE_128B);
