@@ -99,26 +99,21 @@ constexpr int kDownThreads = 256, kDownWarps = 8;
 
 struct DownMaps { CUtensorMap x, x_one, a; };
 
-__host__ __device__ constexpr int down_stage_bytes(int r) { return kRowsBytes + r * kCols * 2; }
 // The ring also holds the partial sums at the end, [128][rank + 4] floats.  Up to rank 128 two CTAs fit on an SM, so that clusters
 // beyond those that have SMs of their own need not wait for a second turn (CTAs with an SM's shared memory each, 36 clusters of four
 // where 35 fit: 41.5 us instead of 35.2 for the call above), and a CTA of the second kernel fits beside one of these.
 constexpr int kDownTail = 2 * kMaxStages * 8 + 32;   // barriers, tensor memory's address, flag
-constexpr int down_smem(int r) { return (r <= 128 ? 112 : 224) * 1024; }
-constexpr int down_stages(int r) {
-    const int fit = (down_smem(r) - kDownTail - 1024) / down_stage_bytes(r);
-    return fit < kMaxStages ? fit : kMaxStages;
-}
-static_assert(down_stages(128) >= 3 && down_stages(256) >= 4, "a ring");
+__host__ __device__ constexpr int down_smem(int r) { return (r <= 128 ? 112 : 224) * 1024; }
+__host__ __device__ constexpr int down_room(int r) { return down_smem(r) - kDownTail - 1024; }
 static_assert(2 * (down_smem(128) + 1024) <= 228 * 1024, "two CTAs to an SM");
-static_assert(3 * down_stage_bytes(128) >= kTok * 132 * 4 && 4 * down_stage_bytes(256) >= kTok * 260 * 4, "partial sums");
+static_assert(down_room(128) >= 3 * (kRowsBytes + 128 * 128) && down_room(256) >= 4 * (kRowsBytes + 256 * 128), "a ring");
+static_assert(down_room(128) >= kTok * 132 * 4 && down_room(256) >= kTok * 260 * 4, "partial sums");
 
 __global__ void __launch_bounds__(kDownThreads, 2)
-adapters_down_kernel(const __grid_constant__ DownMaps maps, const AdapterParams p, int stages, uint32_t tmem_cols) {
+adapters_down_kernel(const __grid_constant__ DownMaps maps, const AdapterParams p, uint32_t tmem_cols) {
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    const int stage_bytes = down_stage_bytes(p.r);
-    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + stages * stage_bytes);       // [stage]: filled, free
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + down_room(p.r));             // [stage]: filled, free
     uint64_t* done = bars + 2 * kMaxStages;                                          // all products are complete
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 1);
     volatile int* stop = reinterpret_cast<volatile int*>(tmem_slot + 1);
@@ -152,6 +147,10 @@ adapters_down_kernel(const __grid_constant__ DownMaps maps, const AdapterParams 
     const int rk = slot < 0 ? 0 : adapter_rank(p, slot);
     if (rk > 0) {                     // (the whole cluster)
         const int steps = p.K / kCols, s0 = rank * steps / CL, n = (rank + 1) * steps / CL - s0;
+        // as many stages as there is room for; they are as large as the tile's tokens and the adapter's rank ask.  (The products
+        // read X as 128 rows: behind the tile's tokens whatever lies there, sums that nobody reads.)
+        const int row_bytes = (count + kBox - 1) / kBox * kBox * 128, stage_bytes = row_bytes + rk * 128;
+        const int fit = (down_room(p.r) - (kRowsBytes - row_bytes)) / stage_bytes, stages = fit < kMaxStages ? fit : kMaxStages;
         if (warp == 0) {              // copies
             const TileRows rows = tile_rows(t4, plan.tokens, lane);
             const uint32_t bytes = (uint32_t)(rows.rows() + rk) * 128u;
@@ -162,7 +161,7 @@ adapters_down_kernel(const __grid_constant__ DownMaps maps, const AdapterParams 
                 const uint32_t at = sb + (uint32_t)(s * stage_bytes);
                 const int col = (s0 + i) * kCols;
                 rows.load(at, &maps.x, &maps.x_one, col, filled(s), lane);
-                if (lane * 16 < rk) tma_load_2d(at + kRowsBytes + lane * 2048, &maps.a, col, slot * p.r + lane * 16, filled(s));
+                if (lane * 16 < rk) tma_load_2d(at + row_bytes + lane * 2048, &maps.a, col, slot * p.r + lane * 16, filled(s));
                 if (++s == stages) { s = 0; ++turn; }
             }
         } else if (warp == 1) {       // products (rows that are not there are whatever the ring holds: nobody reads their sums)
@@ -172,7 +171,7 @@ adapters_down_kernel(const __grid_constant__ DownMaps maps, const AdapterParams 
                 tc_fence_after();
                 if (elect_one()) {
                     const uint32_t at = sb + (uint32_t)(s * stage_bytes);
-                    const uint64_t xd = smem_desc_sw128(at), ad = smem_desc_sw128(at + kRowsBytes);
+                    const uint64_t xd = smem_desc_sw128(at), ad = smem_desc_sw128(at + row_bytes);
 #pragma unroll
                     for (int kk = 0; kk < 4; ++kk) mma_f16_ss(tmem, xd + 2 * kk, ad + 2 * kk, idesc, (i | kk) != 0 ? 1u : 0u);
                     tc_commit(free_(s));
@@ -552,7 +551,7 @@ int launch_adapters_down(const AdapterParams& p, cudaStream_t st) {
     attr[1].val.clusterDim.x = CL; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, adapters_down_kernel, maps, p, down_stages(p.r), cols);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, adapters_down_kernel, maps, p, cols);
     if (e != cudaSuccess) return record_cuda_error(e, "adapters_down_kernel");
     return check_launch("adapters_down_kernel");
 }
