@@ -344,8 +344,8 @@ int launch_nt(const int8_t* Xq, const float* a_scale, const __nv_bfloat16* T, in
     // 4.8).
     int tiles = 0, rows = 0;
     for (int l = 0; l < group.layers; ++l) { tiles += (group.N[l] + 31) / 32; rows += group.N[l]; }
-    if (NT == 1 && tiles > 3 * num_sms && tiles <= 4 * num_sms)
-        return launch_cfg<1, 2, 1, GLU>(Xq, a_scale, T, M, K, acc_debug, st, overlap_prev, ldt, cat, group, glu);
+    if ((tiles + 4 * num_sms - 1) / (4 * num_sms) < (tiles + 3 * num_sms - 1) / (3 * num_sms))
+        return launch_cfg<NT, 2, 1, GLU>(Xq, a_scale, T, M, K, acc_debug, st, overlap_prev, ldt, cat, group, glu);
     if (rows >= 32 * 3 * num_sms / 2)
         return launch_cfg<NT, 2, 2, GLU>(Xq, a_scale, T, M, K, acc_debug, st, overlap_prev, ldt, cat, group, glu);
     return launch_cfg<NT, 1, 4, GLU>(Xq, a_scale, T, M, K, acc_debug, st, overlap_prev, ldt, cat, group, glu);
