@@ -86,10 +86,11 @@ struct DecCfg {
 };
 
 // GLU: the channels are gate and up in turn, a lane of an even channel stores the product with its neighbour's (no dump).
-template <int NT, int R, int B, bool GROUP, bool GLU>
+// STREAM: more tiles than CTAs are resident; a CTA takes every gridDim.x-th tile, and its weights keep coming from one tile to the next.
+template <int NT, int R, int B, bool GROUP, bool GLU, bool STREAM>
 __global__ void __launch_bounds__(kDecThreads, DecCfg<NT, R, B>::MinCtas)
 linear_decode_kernel(const int8_t* Xq, const float* a_scale, const __nv_bfloat16* T, int M, int K, int ldt,
-                     int32_t* __restrict__ acc_debug, const CatSplit cat, const __grid_constant__ LinearGroup group, const GluForm glu) {
+                     int32_t* __restrict__ acc_debug, const CatSplit cat, const __grid_constant__ LinearGroup group, const GluForm glu, int tiles) {
     using C = DecCfg<NT, R, B>;
     constexpr int BATCH = C::Batch;
     // partial sums of the eight warps: integer accumulators and fp32 accumulators of the low-rank term
@@ -98,25 +99,27 @@ linear_decode_kernel(const int8_t* Xq, const float* a_scale, const __nv_bfloat16
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int g = lane >> 2, t = lane & 3;       // fragment row group / k quarter
     const int KB = K / kWkCols;
-    // this CTA's layer of the group, and its rows there (layers that share their input are one launch: a launch has its
-    // start-up and a last, emptying wave)
-    int first = 0, layer = 0;
+    // A tile's layer of the group and its rows there (layers that share their input are one launch: a launch has its start-up
+    // and a last, emptying wave)
+    auto find = [&](int tile, int& layer, int& n0) {
+        int first = 0;
+        layer = 0;
 #pragma unroll
-    for (int l = 1; GROUP && l < kMaxGroup; ++l) {
-        const int next = first + (group.N[l - 1] + C::Rows - 1) / C::Rows;
-        if (layer == l - 1 && l < group.layers && (int)blockIdx.x >= next) { layer = l; first = next; }
-    }
-    const uint8_t* __restrict__ Wk = group.Wk[layer];
-    const float* __restrict__ w_scale = group.w_scale[layer];
-    const __half* __restrict__ LB = group.LB[layer];
-    __half* __restrict__ Y = group.Y[layer];
-    const int N = group.N[layer], r = group.r[layer], n0 = ((int)blockIdx.x - first) * C::Rows;
-    T += group.t_col[layer] + cat_layer(cat, n0) * r;        // a CTA's rows lie inside one layer (16 R divides 128)
+        for (int l = 1; GROUP && l < kMaxGroup; ++l) {
+            const int next = first + (group.N[l - 1] + C::Rows - 1) / C::Rows;
+            if (layer == l - 1 && l < group.layers && tile >= next) { layer = l; first = next; }
+        }
+        n0 = (tile - first) * C::Rows;
+    };
     // Rows n0 + 16 rt + g and + 8 of sub-block t (columns 32 t .. 32 t + 31 of a block).  The
     // blocked layout pads the last 128-row tile with zero codes, so rows past N inside that tile
     // read as zeros; a CTA never reaches past the tile (16 R divides 128).
-    const uint8_t* wbase = Wk + ((size_t)(n0 >> 7) * KB) * kWkBlockBytes + t * (kWkRows * 16) +
-                           ((n0 & 127) + g) * 16;
+    auto weights = [&](int layer, int n0) {
+        return group.Wk[layer] + ((size_t)(n0 >> 7) * KB) * kWkBlockBytes + t * (kWkRows * 16) + ((n0 & 127) + g) * 16;
+    };
+    int layer, n0;
+    find((int)blockIdx.x, layer, n0);
+    const uint8_t* wbase = weights(layer, n0);
 
     uint4 wa[BATCH][R][2];
 #pragma unroll
@@ -129,6 +132,20 @@ linear_decode_kernel(const int8_t* Xq, const float* a_scale, const __nv_bfloat16
                 wa[i][rt][1] = ld_stream16(wbase + (size_t)kbi * kWkBlockBytes + rt * 256 + 128);
             }
         }
+    }
+    for (int tile = (int)blockIdx.x;;) {
+    const float* __restrict__ w_scale = group.w_scale[layer];
+    const __half* __restrict__ LB = group.LB[layer];
+    __half* __restrict__ Y = group.Y[layer];
+    const int N = group.N[layer], r = group.r[layer];
+    const __nv_bfloat16* Tl = T + group.t_col[layer] + cat_layer(cat, n0) * r;        // a CTA's rows lie inside one layer (16 R divides 128)
+    // the tile after this one, whose first blocks are asked for as this one's last leave their registers
+    const int tile_next = tile + (int)gridDim.x;
+    int layer_next = 0, n0_next = 0;
+    const uint8_t* wnext = nullptr;
+    if (STREAM && tile_next < tiles) {
+        find(tile_next, layer_next, n0_next);
+        wnext = weights(layer_next, n0_next);
     }
     // L_B fragments of the low-rank term (constant data: may precede the dependency wait)
     uint2 la[2][R][2];
@@ -145,7 +162,7 @@ linear_decode_kernel(const int8_t* Xq, const float* a_scale, const __nv_bfloat16
             }
         }
     }
-    dep_wait();
+    if (!STREAM || tile == (int)blockIdx.x) dep_wait();
 
     // ---- low-rank term, while the weight loads are in flight: warp w takes the 16-wide slices
     // w and w + 8 of r; a thread's k positions inside a slice are 4 t .. 4 t + 3 ----
@@ -159,7 +176,7 @@ linear_decode_kernel(const int8_t* Xq, const float* a_scale, const __nv_bfloat16
             for (int nt = 0; nt < NT; ++nt) {
                 tv[u][nt] = make_uint2(0, 0);
                 if (k0 < r && g + 8 * nt < M)
-                    tv[u][nt] = *reinterpret_cast<const uint2*>(T + (size_t)(g + 8 * nt) * ldt + k0);
+                    tv[u][nt] = *reinterpret_cast<const uint2*>(Tl + (size_t)(g + 8 * nt) * ldt + k0);
             }
         }
 #pragma unroll
@@ -232,6 +249,9 @@ linear_decode_kernel(const int8_t* Xq, const float* a_scale, const __nv_bfloat16
                     if (kbn < KB) {
                         wa[i][rt][0] = ld_stream16(wbase + (size_t)kbn * kWkBlockBytes + rt * 256);
                         wa[i][rt][1] = ld_stream16(wbase + (size_t)kbn * kWkBlockBytes + rt * 256 + 128);
+                    } else if (STREAM && wnext) {
+                        wa[i][rt][0] = ld_stream16(wnext + (size_t)(warp + i * kDecWarps) * kWkBlockBytes + rt * 256);
+                        wa[i][rt][1] = ld_stream16(wnext + (size_t)(warp + i * kDecWarps) * kWkBlockBytes + rt * 256 + 128);
                     }
                 }
             }
@@ -296,15 +316,24 @@ linear_decode_kernel(const int8_t* Xq, const float* a_scale, const __nv_bfloat16
             if (acc_debug) acc_debug[(size_t)om * N + on] = sums[o] >> 4;
         }
     }
+    if (!STREAM || tile_next >= tiles) break;
+    tile = tile_next;
+    layer = layer_next;
+    n0 = n0_next;
+    wbase = wnext;
+    __syncthreads();            // the sums of this tile have been read
+    }
 }
 
 template <int NT, int R, int B, bool GLU = false>
-int launch_cfg(const int8_t* Xq, const float* a_scale, const __nv_bfloat16* T, int M, int K, int32_t* acc_debug,
+int launch_cfg(const int8_t* Xq, const float* a_scale, const __nv_bfloat16* T, int M, int K, int32_t* acc_debug, int num_sms,
                cudaStream_t st, bool overlap_prev, int ldt, const CatSplit& cat, const LinearGroup& group, const GluForm& glu) {
+    using C = DecCfg<NT, R, B>;
     int tiles = 0;
-    for (int l = 0; l < group.layers; ++l) tiles += (group.N[l] + DecCfg<NT, R, B>::Rows - 1) / DecCfg<NT, R, B>::Rows;
+    for (int l = 0; l < group.layers; ++l) tiles += (group.N[l] + C::Rows - 1) / C::Rows;
+    const int resident = C::MinCtas * num_sms;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(tiles, 1, 1);
+    cfg.gridDim = dim3(tiles < resident ? tiles : resident, 1, 1);
     cfg.blockDim = dim3(kDecThreads, 1, 1);
     cfg.dynamicSmemBytes = 0;
     cfg.stream = st;
@@ -317,10 +346,12 @@ int launch_cfg(const int8_t* Xq, const float* a_scale, const __nv_bfloat16* T, i
     // faster (alone / as a group of one, us: 12 x 4096 x 14336 9.6 / 10.5, 16 x 4096 x 14336 11.0 / 11.7); for the others the opposite
     // holds (1 x 4096 x 14336 8.9 / 8.2, 16 x 8192 x 8192 11.2 / 10.9, 8 x 8192 x 8192 8.9 / 8.7).
     cudaError_t e;
-    if (NT == 2 && R == 1 && group.layers == 1)
-        e = cudaLaunchKernelEx(&cfg, linear_decode_kernel<NT, R, B, NT != 2 || R != 1, GLU>, Xq, a_scale, T, M, K, ldt, acc_debug, cat, group, glu);
+    if (tiles > resident)
+        e = cudaLaunchKernelEx(&cfg, linear_decode_kernel<NT, R, B, true, GLU, true>, Xq, a_scale, T, M, K, ldt, acc_debug, cat, group, glu, tiles);
+    else if (NT == 2 && R == 1 && group.layers == 1)
+        e = cudaLaunchKernelEx(&cfg, linear_decode_kernel<NT, R, B, NT != 2 || R != 1, GLU, false>, Xq, a_scale, T, M, K, ldt, acc_debug, cat, group, glu, tiles);
     else
-        e = cudaLaunchKernelEx(&cfg, linear_decode_kernel<NT, R, B, true, GLU>, Xq, a_scale, T, M, K, ldt, acc_debug, cat, group, glu);
+        e = cudaLaunchKernelEx(&cfg, linear_decode_kernel<NT, R, B, true, GLU, false>, Xq, a_scale, T, M, K, ldt, acc_debug, cat, group, glu, tiles);
     if (e != cudaSuccess) return record_cuda_error(e, "linear_decode_kernel");
     return check_launch("linear_decode_kernel");
 }
@@ -345,10 +376,10 @@ int launch_nt(const int8_t* Xq, const float* a_scale, const __nv_bfloat16* T, in
     int tiles = 0, rows = 0;
     for (int l = 0; l < group.layers; ++l) { tiles += (group.N[l] + 31) / 32; rows += group.N[l]; }
     if ((tiles + 4 * num_sms - 1) / (4 * num_sms) < (tiles + 3 * num_sms - 1) / (3 * num_sms))
-        return launch_cfg<NT, 2, 1, GLU>(Xq, a_scale, T, M, K, acc_debug, st, overlap_prev, ldt, cat, group, glu);
+        return launch_cfg<NT, 2, 1, GLU>(Xq, a_scale, T, M, K, acc_debug, num_sms, st, overlap_prev, ldt, cat, group, glu);
     if (rows >= 32 * 3 * num_sms / 2)
-        return launch_cfg<NT, 2, 2, GLU>(Xq, a_scale, T, M, K, acc_debug, st, overlap_prev, ldt, cat, group, glu);
-    return launch_cfg<NT, 1, 4, GLU>(Xq, a_scale, T, M, K, acc_debug, st, overlap_prev, ldt, cat, group, glu);
+        return launch_cfg<NT, 2, 2, GLU>(Xq, a_scale, T, M, K, acc_debug, num_sms, st, overlap_prev, ldt, cat, group, glu);
+    return launch_cfg<NT, 1, 4, GLU>(Xq, a_scale, T, M, K, acc_debug, num_sms, st, overlap_prev, ldt, cat, group, glu);
 }
 
 }  // namespace
