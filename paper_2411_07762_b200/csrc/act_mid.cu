@@ -31,8 +31,9 @@ __device__ __forceinline__ void mid_mma(float (&d)[4], uint32_t a0, uint32_t a1,
 
 // Grid: t_tiles * CL projecting CTAs (clusters of CL along K), then the quantizing CTAs, R rows each.
 // A sum (register 4 (4 mt + nt) + e of lane 4 g + t) is token 16 mt + g + 8 (e / 2), L_A row 8 nt + 2 t + e % 2.
-template <int CPT, int R>
-__global__ void __launch_bounds__(kMThreads, 2)
+// TH threads: 256, or 512 for rows that would fill a thread's registers; the projection takes eight warps of them either way.
+template <int CPT, int R, int TH = kMThreads>
+__global__ void __launch_bounds__(TH, 512 / TH)
 quant_act_mid_kernel(const __half* __restrict__ X, const float* __restrict__ s, const __half* __restrict__ LA, int M, int K,
                      int r, int t_tiles, int CL, int8_t* __restrict__ Xq, float* __restrict__ a_scale,
                      __nv_bfloat16* __restrict__ T, int ldt, int lo_off, float qmax) {
@@ -70,7 +71,7 @@ quant_act_mid_kernel(const __half* __restrict__ X, const float* __restrict__ s, 
         xp[i] = X + (size_t)(x_ok[i] ? m0 + g + 8 * i : 0) * K + t * 8;
         lp[i] = LA + (size_t)(l_ok[i] ? j0 + g + 8 * i : 0) * K + t * 8;
     }
-    for (int u = rank * kMWarps + warp; u < K / 64; u += CL * kMWarps) {
+    for (int u = warp < kMWarps ? rank * kMWarps + warp : K; u < K / 64; u += CL * kMWarps) {
         uint4 xv[2][4], lv[2][4];
         float4 s0[2], s1[2];
 #pragma unroll
@@ -120,14 +121,16 @@ quant_act_mid_kernel(const __half* __restrict__ X, const float* __restrict__ s, 
             }
         }
     }
+    if (warp < kMWarps) {
 #pragma unroll
-    for (int mt = 0; mt < 2; ++mt)
+        for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-        for (int nt = 0; nt < 4; ++nt)
+            for (int nt = 0; nt < 4; ++nt)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sh.red[warp][(mt * 4 + nt) * 4 + e][lane] = acc[mt][nt][e];
+                for (int e = 0; e < 4; ++e) sh.red[warp][(mt * 4 + nt) * 4 + e][lane] = acc[mt][nt][e];
+    }
     __syncthreads();
-    for (int i = tid; i < kMAcc * 32; i += kMThreads) {
+    for (int i = tid; i < kMAcc * 32; i += TH) {
         float v = 0.f;
 #pragma unroll
         for (int w = 0; w < kMWarps; ++w) v += sh.red[w][i >> 5][i & 31];
@@ -137,7 +140,7 @@ quant_act_mid_kernel(const __half* __restrict__ X, const float* __restrict__ s, 
     else __syncthreads();
     const int per = kMAcc * 32 / CL;        // sums that this CTA finishes
     const uint32_t mine = smem_u32(&part[0][0]);
-    for (int i = rank * per + tid; i < (rank + 1) * per; i += kMThreads) {
+    for (int i = rank * per + tid; i < (rank + 1) * per; i += TH) {
         float v[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q) v[q] = q < CL ? (CL > 1 ? ld_cluster_f32(map_to_rank(mine + 4u * i, q)) : part[i >> 5][i & 31]) : 0.f;
@@ -155,13 +158,13 @@ quant_act_mid_kernel(const __half* __restrict__ X, const float* __restrict__ s, 
 int mid_cluster(int K) { return K >= 4096 ? 8 : K >= 2048 ? 4 : K >= 1024 ? 2 : 1; }
 
 template <typename Kernel>
-int launch_mid_cfg(Kernel* kernel, int R, const __half* X, const float* s, const __half* LA, int M, int K, int r, int8_t* Xq,
+int launch_mid_cfg(Kernel* kernel, int threads, int R, const __half* X, const float* s, const __half* LA, int M, int K, int r, int8_t* Xq,
                    float* a_scale, __nv_bfloat16* T, int ldt, int lo_off, float qmax, cudaStream_t st) {
     const int CL = mid_cluster(K);
     const int t_tiles = (M + kMTok - 1) / kMTok * ((r + kMRank - 1) / kMRank), rows = (M + R - 1) / R;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(t_tiles * CL + (rows + CL - 1) / CL * CL, 1, 1);
-    cfg.blockDim = dim3(kMThreads, 1, 1);
+    cfg.blockDim = dim3(threads, 1, 1);
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -200,13 +203,13 @@ int launch_quant_act_mid(const __half* X, const float* s, const __half* LA, int 
                          __nv_bfloat16* T, int ldt, int lo_off, float qmax, cudaStream_t st) {
     // chunks of eight columns per thread by the row length, one, two or four rows per quantizing CTA
     const int chunks = (K / 8 + kMThreads - 1) / kMThreads, rows = mid_rows(M, K);
-    auto go = [&](auto* kernel) { return launch_mid_cfg(kernel, rows, X, s, LA, M, K, r, Xq, a_scale, T, ldt, lo_off, qmax, st); };
+    auto go = [&](auto* kernel, int threads = kMThreads) { return launch_mid_cfg(kernel, threads, rows, X, s, LA, M, K, r, Xq, a_scale, T, ldt, lo_off, qmax, st); };
     if (rows == 4) return go(quant_act_mid_kernel<1, 4>);        // up to 2048 columns
     if (chunks <= 1) return rows == 2 ? go(quant_act_mid_kernel<1, 2>) : go(quant_act_mid_kernel<1, 1>);
     if (chunks <= 2) return rows == 2 ? go(quant_act_mid_kernel<2, 2>) : go(quant_act_mid_kernel<2, 1>);
     if (chunks <= 4) return rows == 2 ? go(quant_act_mid_kernel<4, 2>) : go(quant_act_mid_kernel<4, 1>);
     if (chunks <= 8) return go(quant_act_mid_kernel<8, 1>);
-    return go(quant_act_mid_kernel<16, 1>);
+    return go(quant_act_mid_kernel<8, 1, 512>, 512);
 }
 
 }  // namespace aser
