@@ -58,7 +58,9 @@ __device__ __forceinline__ float rcp_approx(float v) {
 // registers, and a projection CTA uses the L_A chunks it loads for TOK tokens (one token per CTA read L_A
 // from L2 M times: 16 tokens x 384 rows 10.9 us; K = 14336 took 9.1 us at one token because 256 threads went
 // through seven dependent rounds).
-template <int TH, int CPT, int TOK>
+// TH threads, of which the first PT make the projection: between 8192 and 16384 columns twice as many quantize, with half the chunks each (8 x 14336,
+// rank 64: 6.2 -> 5.0 us), where the projection of four tokens does not need their registers.
+template <int TH, int PT, int CPT, int TOK>
 __global__ void __launch_bounds__(TH)
 quant_act_small_kernel(const __half* __restrict__ X, const float* __restrict__ s,
                        const __half* __restrict__ LA, int M, int K, int r,
@@ -119,7 +121,7 @@ quant_act_small_kernel(const __half* __restrict__ X, const float* __restrict__ s
         for (int k = 0; k < TOK; ++k) acc[jj][k] = 0.f;
     float nearest = 1.f, farthest = 1.f;        // magnitudes of the divisors met, from zero
 #pragma unroll 2
-    for (int c = threadIdx.x; c < chunks; c += TH) {
+    for (int c = (int)threadIdx.x < PT ? (int)threadIdx.x : chunks; c < chunks; c += PT) {
         RawChunk rc[TOK];
         rc[0] = load_raw(X + (size_t)m0 * K, s, c * 8, true);
 #pragma unroll
@@ -179,7 +181,7 @@ quant_act_small_kernel(const __half* __restrict__ X, const float* __restrict__ s
             for (int jj = 0; jj < kRowsPerCta; ++jj) acc[jj][k] = 0.f;
             if (m0 + k >= M) continue;
             const __half* row = X + (size_t)(m0 + k) * K;
-            for (int col = threadIdx.x * 8; col < K; col += (col & 7) == 7 ? TH * 8 - 7 : 1) {
+            for (int col = (int)threadIdx.x < PT ? threadIdx.x * 8 : K; col < K; col += (col & 7) == 7 ? PT * 8 - 7 : 1) {
                 const float v = __fdiv_rn(__half2float(row[col]), __ldg(s + col));
 #pragma unroll
                 for (int jj = 0; jj < kRowsPerCta; ++jj)
@@ -199,12 +201,12 @@ quant_act_small_kernel(const __half* __restrict__ X, const float* __restrict__ s
         const int j = j0 + (int)threadIdx.x / TOK, m = m0 + (int)threadIdx.x % TOK;
         float t = 0.f;
 #pragma unroll
-        for (int i = 0; i < kWarps; ++i) t += red[threadIdx.x][i];
+        for (int i = 0; i < PT / 32; ++i) t += red[threadIdx.x][i];
         if (j < r && m < M) store_t(T + (size_t)m * ldt, j, t, lo_off);
     }
 }
 
-template <int TH, int CPT>
+template <int TH, int PT, int CPT>
 int launch_small(const __half* X, const float* s, const __half* LA, int M, int K, int r, int8_t* Xq, float* a_scale,
                  __nv_bfloat16* T, int ldt, int lo_off, float qmax, cudaStream_t st) {
     // tokens per projection CTA: as many as leave about a CTA for every SM
@@ -213,7 +215,7 @@ int launch_small(const __half* X, const float* s, const __half* LA, int M, int K
     const int tok = (M > 2 && ctas(4) >= 128) ? 4 : (M > 1 && ctas(2) >= 128) ? 2 : 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(M + ctas(tok), 1, 1);
-    cfg.blockDim = dim3(TH, 1, 1);
+    cfg.blockDim = dim3(tok == 4 ? PT : TH, 1, 1);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -221,9 +223,9 @@ int launch_small(const __half* X, const float* s, const __half* LA, int M, int K
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     cudaError_t e;
-    if (tok == 4) e = cudaLaunchKernelEx(&cfg, quant_act_small_kernel<TH, CPT, 4>, X, s, LA, M, K, r, Xq, a_scale, T, ldt, lo_off, qmax);
-    else if (tok == 2) e = cudaLaunchKernelEx(&cfg, quant_act_small_kernel<TH, CPT, 2>, X, s, LA, M, K, r, Xq, a_scale, T, ldt, lo_off, qmax);
-    else e = cudaLaunchKernelEx(&cfg, quant_act_small_kernel<TH, CPT, 1>, X, s, LA, M, K, r, Xq, a_scale, T, ldt, lo_off, qmax);
+    if (tok == 4) e = cudaLaunchKernelEx(&cfg, quant_act_small_kernel<PT, PT, CPT * (TH / PT), 4>, X, s, LA, M, K, r, Xq, a_scale, T, ldt, lo_off, qmax);
+    else if (tok == 2) e = cudaLaunchKernelEx(&cfg, quant_act_small_kernel<TH, PT, CPT, 2>, X, s, LA, M, K, r, Xq, a_scale, T, ldt, lo_off, qmax);
+    else e = cudaLaunchKernelEx(&cfg, quant_act_small_kernel<TH, PT, CPT, 1>, X, s, LA, M, K, r, Xq, a_scale, T, ldt, lo_off, qmax);
     if (e != cudaSuccess) return record_cuda_error(e, "quant_act_small_kernel");
     return check_launch("quant_act_small_kernel");
 }
@@ -1215,10 +1217,10 @@ int launch_quant_act(const __half* X, const float* s, const __half* LA, int M, i
     const int ldt = t_pair ? 2 * r : r, lo_off = t_pair ? r : 0;
     if (M <= 32) {
         // threads by the row length: two chunks of eight columns each up to 8192, then four and eight (K <= 32768)
-        if (K <= 4096) return launch_small<256, 2>(X, s, LA, M, K, r, Xq, a_scale, T, ldt, lo_off, qmax, st);
-        if (K <= 8192) return launch_small<512, 2>(X, s, LA, M, K, r, Xq, a_scale, T, ldt, lo_off, qmax, st);
-        if (K <= 16384) return launch_small<512, 4>(X, s, LA, M, K, r, Xq, a_scale, T, ldt, lo_off, qmax, st);
-        return launch_small<512, 8>(X, s, LA, M, K, r, Xq, a_scale, T, ldt, lo_off, qmax, st);
+        if (K <= 4096) return launch_small<256, 256, 2>(X, s, LA, M, K, r, Xq, a_scale, T, ldt, lo_off, qmax, st);
+        if (K <= 8192) return launch_small<512, 512, 2>(X, s, LA, M, K, r, Xq, a_scale, T, ldt, lo_off, qmax, st);
+        if (K <= 16384) return launch_small<1024, 512, 2>(X, s, LA, M, K, r, Xq, a_scale, T, ldt, lo_off, qmax, st);
+        return launch_small<512, 512, 8>(X, s, LA, M, K, r, Xq, a_scale, T, ldt, lo_off, qmax, st);
     }
     bool unsupported = false;
     if (M_pass == 0) M_pass = M;
