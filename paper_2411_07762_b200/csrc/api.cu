@@ -140,11 +140,11 @@ int linear_common(const int8_t* Xq, const float* a_scale, const void* Wk, const 
                             static_cast<cudaStream_t>(stream), overlap_prev, ldt, cat, glu);
 }
 
-// act(g) = g / (1 + exp(-g (c0 + c1 g^2))), see glu_math.cuh; false for an activation that is not known.
+// The numbers of glu_math.cuh; false for an activation that is not known.
 bool glu_form(int activation, GluForm* f) {
-    constexpr double kC0 = 1.5957691216057308;         // sqrt(8 / pi)
-    if (activation == ASER_ACT_SILU) { f->c0 = 1.f; f->c1 = 0.f; return true; }
-    if (activation == ASER_ACT_GELU_TANH) { f->c0 = (float)kC0; f->c1 = (float)(0.044715 * kC0); return true; }
+    constexpr double kLog2e = 1.4426950408889634, kC0 = 1.5957691216057308;         // sqrt(8 / pi)
+    if (activation == ASER_ACT_SILU) { f->k0 = (float)-kLog2e; f->k1 = 0.f; return true; }
+    if (activation == ASER_ACT_GELU_TANH) { f->k0 = (float)(-kC0 * kLog2e); f->k1 = (float)(-0.044715 * kC0 * kLog2e); return true; }
     return false;
 }
 

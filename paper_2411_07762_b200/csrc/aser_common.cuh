@@ -71,9 +71,9 @@ __host__ __device__ inline int cat_layer(const CatSplit& c, int row) {
     return (row >= c.b1 ? 1 : 0) + (row >= c.b2 ? 1 : 0) + (row >= c.b3 ? 1 : 0);
 }
 // A linear launch whose N channels are gate and up in turn writes H = act(gate) * up [M, N / 2] instead of Y (glu_math.cuh);
-// act(g) = g / (1 + exp(-g (c0 + c1 g^2))).
+// act(g) = g / (1 + 2^(g (k0 + k1 g^2))).
 struct GluForm {
-    float c0 = 0.f, c1 = 0.f;
+    float k0 = 0.f, k1 = 0.f;
 };
 // `glu`: the gated form (Y is then H; single layers without accumulator dump).
 // `ldt`: elements between rows of T (0 = r; larger when T is a column range of a wider matrix).

@@ -304,7 +304,7 @@ linear_decode_kernel(const int8_t* Xq, const float* a_scale, const __nv_bfloat16
             const float own_y = __half2float(__float2half_rn(y));
             const float up = __shfl_xor_sync(0xffffffffu, own_y, 1);
             if (om < M && on < N && !(row & 1))
-                Y[(size_t)om * (N / 2) + on / 2] = __float2half_rn(gated_product(own_y, up, glu));
+                Y[(size_t)om * (N / 2) + on / 2] = __float2half_rn((glu.k1 == 0.f ? gated_product<true>(own_y, up, glu) : gated_product<false>(own_y, up, glu)));
         } else if (om < M && on < N) {
             const int reg = ((row >> 4) * NT + (om >> 3)) * 4 + ((row >> 3) & 1) * 2 + (col & 1);
             const int ln = (row & 7) * 4 + (col >> 1);

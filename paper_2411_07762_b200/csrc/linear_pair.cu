@@ -567,10 +567,17 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                 if (h >= w.halves || !ok) continue;
                 if (GLU) {              // rows of 64 products; a lane has one of the two tokens of a register
                     uint16_t* out = reinterpret_cast<uint16_t*>(smem + kOffLr) + ((h * 2 + side) * kHw + (lane & 1)) * 64 + (q * 32 + lane) / 2;
+                    if (p.glu.k1 == 0.f) {
 #pragma unroll
-                    for (int c = 0; c < 4; ++c)
+                        for (int c = 0; c < 4; ++c)
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) out[(c * 16 + 2 * j) * 64] = gated_exchange(y[h][c][j], lane, p.glu);
+                            for (int j = 0; j < 8; ++j) out[(c * 16 + 2 * j) * 64] = gated_exchange<true>(y[h][c][j], lane, p.glu);
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c)
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) out[(c * 16 + 2 * j) * 64] = gated_exchange<false>(y[h][c][j], lane, p.glu);
+                    }
                     continue;
                 }
                 uint16_t* stage = reinterpret_cast<uint16_t*>(smem + kOffLr) + ((h * 2 + side) * kHw) * (kYRow / 2) + q * 32 + lane;

@@ -416,7 +416,7 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
                     for (int e = 0; e < 8; e += 2) {
                         const float y0 = fmaf((float)(int)v[e], scales[c + e] * ws16, chunks > 0 ? __uint_as_float(f[e]) : 0.f);
                         const float y1 = fmaf((float)(int)v[e + 1], scales[c + e + 1] * ws16, chunks > 0 ? __uint_as_float(f[e + 1]) : 0.f);
-                        out[e * 64] = gated_exchange(pack_f16(y0, y1), lane, p.glu);
+                        out[e * 64] = p.glu.k1 == 0.f ? gated_exchange<true>(pack_f16(y0, y1), lane, p.glu) : gated_exchange<false>(pack_f16(y0, y1), lane, p.glu);
                     }
                     continue;
                 }

@@ -803,7 +803,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
                         for (int j = 0; j < 16; j += 2) {
                             const float y0 = fmaf((float)(int)vi[j], as[j] * ws16, w.has_lr ? __uint_as_float(vf[j]) : 0.f);
                             const float y1 = fmaf((float)(int)vi[j + 1], as[j + 1] * ws16, w.has_lr ? __uint_as_float(vf[j + 1]) : 0.f);
-                            const unsigned short h = gated_exchange(pack_f16(y0, y1), lane, p.glu);
+                            const unsigned short h = gated_exchange<false>(pack_f16(y0, y1), lane, p.glu);
                             const int tok = c0 + j + (lane & 1);
                             if (tok < valid && n_ok)
                                 __stcs(reinterpret_cast<unsigned short*>(p.Y + (size_t)(tok0 + tok) * (p.N / 2) + n / 2), h);
@@ -927,7 +927,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
                                     const float as = c0 + j + e < valid ? __ldg(p.a_scale + tok0 + c0 + j + e) : 0.f;
                                     y[e] = fmaf((float)sum[j + e], as * ws16, p.r > 0 ? __uint_as_float(lrw[j + e]) : 0.f);
                                 }
-                                const unsigned short h = gated_exchange(pack_f16(y[0], y[1]), lane, p.glu);
+                                const unsigned short h = gated_exchange<false>(pack_f16(y[0], y[1]), lane, p.glu);
                                 const int tok = c0 + j + (lane & 1);
                                 if (tok < valid && n_ok)
                                     __stcs(reinterpret_cast<unsigned short*>(p.Y + (size_t)(tok0 + tok) * (p.N / 2) + n / 2), h);
