@@ -310,10 +310,10 @@ int aser_forward_ffn(const void* X_f16, const float* s, const void* LA_f16, cons
  * aser_adapters_add -- the update above.  Y [M, N] and out [M, N] may be one matrix (in place: rows without an adapter are then
  * not touched; else they are copied); other overlaps of out with Y, X or the adapters are not allowed.  ldx, ldy, ldo: elements between rows,
  * multiples of 8 (0: K, N, N), so a projection of a fused group is a column range.  plan must be one of these M and
- * n_slots, made by work that precedes the call on `stream` (a plan of other sizes makes the call write nothing).  Where there are
- * many tokens to an adapter (more than 24 for each of the n_slots) the call is two launches with a workspace between them, of
- * aser_adapters_workspace_bytes(M, r, n_slots) bytes, contents irrelevant (else 0 bytes: workspace may be NULL); calls that overlap in time need
- * one each.
+ * n_slots, made by work that precedes the call on `stream` (a plan of other sizes makes the call write nothing).  Where
+ * there are many tokens to an adapter the call is two launches with a workspace between them, of aser_adapters_workspace_bytes(M, N, K,
+ * r, n_slots) bytes, contents irrelevant (else one launch and 0 bytes: workspace may be NULL); calls that overlap in time need one
+ * each.
  *
  * aser_forward_adapters -- aser_forward, then the adapters of its tokens added to Y in place, enqueued together.  All
  * arguments are checked before anything is.  adapter_workspace: that of aser_adapters_add, apart from the layer's own.
@@ -324,7 +324,7 @@ int aser_adapters_add(const void* X_f16, int ldx, const void* A_f16, const void*
                       const float* scale, const void* plan, size_t plan_bytes, int M, int N, int K, int r, int n_slots,
                       const void* Y_f16, int ldy, void* out_f16, int ldo, void* workspace, size_t workspace_bytes,
                       void* stream);
-size_t aser_adapters_workspace_bytes(int M, int r, int n_slots);
+size_t aser_adapters_workspace_bytes(int M, int N, int K, int r, int n_slots);
 int aser_forward_adapters(const void* X_f16, const float* s, const void* LA_f16, const void* Wk, const float* w_scale,
                           const void* LB_f16, int M, int N, int K, int r, int8_t* Xq, float* a_scale, void* T_bf16,
                           void* Y_f16, void* workspace, size_t workspace_bytes, const void* A_f16, const void* B_f16,

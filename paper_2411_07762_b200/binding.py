@@ -71,7 +71,7 @@ lib.aser_forward_ffn.argtypes = [_P] * 11 + [_I] * 7 + [_P, _P, _Z, _P]
 lib.aser_adapters_plan_bytes.argtypes = [_I, _I]
 lib.aser_adapters_plan_bytes.restype = _Z
 lib.aser_adapters_plan.argtypes = [_P, _I, _I, _P, _Z, _P]
-lib.aser_adapters_workspace_bytes.argtypes = [_I, _I, _I]
+lib.aser_adapters_workspace_bytes.argtypes = [_I, _I, _I, _I, _I]
 lib.aser_adapters_workspace_bytes.restype = _Z
 lib.aser_adapters_add.argtypes = [_P, _I, _P, _P, _P, _P, _P, _Z, _I, _I, _I, _I, _I, _P, _I, _P, _I, _P, _Z, _P]
 lib.aser_forward_adapters.argtypes = [_P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _P, _P, _P, _P, _P, _Z,
@@ -614,7 +614,7 @@ class AserAdapters:
 
     def _workspace(self, M: int):
         """What a call of many tokens keeps between its two launches: torch's memory of the current stream."""
-        nbytes = lib.aser_adapters_workspace_bytes(M, self.r, self.n_slots)
+        nbytes = lib.aser_adapters_workspace_bytes(M, self.N, self.K, self.r, self.n_slots)
         return None if nbytes == 0 else torch.empty((nbytes,), dtype=torch.uint8, device=self.A.device)
 
     def add(self, X: torch.Tensor, Y: torch.Tensor, plan: AdapterPlan, out: torch.Tensor | None = None) -> torch.Tensor:

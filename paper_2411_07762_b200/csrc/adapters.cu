@@ -397,15 +397,26 @@ int launch_adapters_plan(const int32_t* slot, int M, int n_slots, void* plan, cu
     return check_launch("adapters_plan_kernel");
 }
 
-bool adapters_many(int M, int n_slots) {
-    const int used = n_slots < M ? n_slots : M;
-    return M > 24 * used;
+// Estimates of both ways, in us, with half of the adapters in use, each with a short tile in two of 16 tokens and one of 128 at
+// least (fitted to 90 points: 1 to 48 adapters of 8 to 128 tokens, five shapes).  Few | many, tokens to an adapter: 4096 x 4096,
+// rank 64, 4 adapters: 32 9.1 | 12.0, 128 13.8 | 14.0, 16 adapters: 16 11.0 | 16.7, 32 18.3 | 17.5, 128 48.7 | 25.8; 28672 x 4096, rank 32, 4
+// adapters: 32 16.3 | 19.2, 64 30.4 | 21.3; 4096 x 14336, rank 128, 16 adapters: 8 36.4 | 30.9; 1024 x 1024, rank 32, 16 adapters:
+// 32 9.6 | 10.6, 64 14.0 | 10.7.
+bool adapters_many(int M, int N, int K, int r, int n_slots) {
+    if (M <= 32) return false;
+    const float used = 0.5f * (n_slots < M ? n_slots : M), wide = (float)(K + N) / 8192;
+    const float few_tiles = M / 16.f + 0.5f * used, many_tiles = fmaxf(used, M / 128.f + 0.5f * used);
+    const float few = few_tiles * (0.07f + wide * (0.24f + 0.1f * r / 64));
+    const float many = 5.f + 0.42f * many_tiles * fmaxf(0.5f, wide) + 5.6e-7f * M * (K + N);
+    return many < few;
 }
 
-size_t adapters_workspace_bytes(int M, int r, int n_slots) { return adapters_many(M, n_slots) ? (size_t)M * (2 * r + 4) : 0; }
+size_t adapters_workspace_bytes(int M, int N, int K, int r, int n_slots) {
+    return adapters_many(M, N, K, r, n_slots) ? (size_t)M * (2 * r + 4) : 0;
+}
 
 int launch_adapters(AdapterParams p, void* workspace, cudaStream_t st) {
-    if (!adapters_many(p.M, p.n_slots)) return launch_few(p, st);
+    if (!adapters_many(p.M, p.N, p.K, p.r, p.n_slots)) return launch_few(p, st);
     p.S = static_cast<__half*>(workspace);
     p.row_scale = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + (size_t)p.M * 2 * p.r);
     const int rc = launch_adapters_down(p, st);

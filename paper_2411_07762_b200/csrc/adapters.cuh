@@ -53,8 +53,8 @@ struct AdapterParams {
 size_t adapters_plan_bytes(int M, int n_slots);
 int launch_adapters_plan(const int32_t* slot, int M, int n_slots, void* plan, cudaStream_t st);
 // Whether a call runs the two kernels for many tokens, and the workspace that it then needs.
-bool adapters_many(int M, int n_slots);
-size_t adapters_workspace_bytes(int M, int r, int n_slots);
+bool adapters_many(int M, int N, int K, int r, int n_slots);
+size_t adapters_workspace_bytes(int M, int N, int K, int r, int n_slots);
 // (p.S and p.row_scale are set from `workspace`.)
 int launch_adapters(AdapterParams p, void* workspace, cudaStream_t st);
 int launch_adapters_down(const AdapterParams& p, cudaStream_t st);

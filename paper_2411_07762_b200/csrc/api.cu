@@ -191,7 +191,7 @@ int adapters_check(const void* X_f16, int ldx, const void* A_f16, const void* B_
         ASER_REQUIRE_PTR(B_f16);
     }
     if (plan_bytes < adapters_plan_bytes(M, n_slots)) return fail(ASER_ERR_WORKSPACE, "plan too small for M and n_slots");
-    const size_t need = adapters_workspace_bytes(M, r, n_slots);
+    const size_t need = adapters_workspace_bytes(M, N, K, r, n_slots);
     if (need > 0 && (workspace == nullptr || misaligned16(workspace) || workspace_bytes < need))
         return fail(ASER_ERR_WORKSPACE, "workspace missing, misaligned or too small");
     return ASER_OK;
@@ -598,9 +598,9 @@ int aser_adapters_plan(const int32_t* slot, int M, int n_slots, void* plan, size
     return launch_adapters_plan(slot, M, n_slots, plan, static_cast<cudaStream_t>(stream));
 }
 
-size_t aser_adapters_workspace_bytes(int M, int r, int n_slots) {
-    if (M < 0 || M > kMaxAdapterTokens || !shape_ok(0, 0, 128, r) || n_slots < 1 || n_slots > kMaxSlots) return 0;
-    return adapters_workspace_bytes(M, r, n_slots);
+size_t aser_adapters_workspace_bytes(int M, int N, int K, int r, int n_slots) {
+    if (M > kMaxAdapterTokens || !shape_ok(M, N, K, r) || n_slots < 1 || n_slots > kMaxSlots) return 0;
+    return adapters_workspace_bytes(M, N, K, r, n_slots);
 }
 
 int aser_adapters_add(const void* X_f16, int ldx, const void* A_f16, const void* B_f16, const int32_t* ranks, const float* scale,

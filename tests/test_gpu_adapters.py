@@ -74,10 +74,15 @@ def make(g, M, K, N, r, slots, bare=0.2, spread=True):
     return A, B, ranks, scale, slot
 
 
+def launches_two(aser, M, K, N, r, slots):
+    return aser.lib.aser_adapters_workspace_bytes(M, N, K, r, slots) > 0
+
+
 # one token to many, odd sizes, every number of 16-rank steps' remainder, one adapter to more than there are tokens
 SHAPES = [(1, 128, 8, 16, 1), (1, 4096, 4096, 16, 8), (1, 640, 264, 256, 3), (2, 256, 40, 32, 70), (5, 1152, 1000, 48, 4), (16, 512, 512, 64, 1),
           (17, 128, 24, 16, 2), (33, 4096, 1024, 80, 5), (64, 2048, 4104, 128, 40), (100, 384, 88, 112, 300), (130, 14336, 72, 64, 3),
-          (257, 1024, 2056, 32, 2), (501, 512, 8, 256, 6), (1000, 640, 1032, 48, 1), (1025, 256, 264, 16, 4096), (2050, 1024, 520, 144, 3)]
+          (257, 1024, 2056, 32, 2), (501, 512, 8, 256, 6), (1000, 640, 1032, 48, 1), (1025, 256, 264, 16, 4096), (2050, 1024, 520, 144, 3),
+          (33, 4096, 4096, 128, 1), (700, 512, 1024, 256, 2), (4100, 128, 64, 16, 9)]
 
 
 @pytest.mark.parametrize("bare,spread", [(0.2, True), (0.0, False)])
@@ -100,6 +105,72 @@ def test_update(aser, M, K, N, r, slots, bare, spread):
     assert torch.equal(inplace, out[:M])
     idle = (slot < 0) | (slot >= slots)
     assert torch.equal(inplace[idle], Y[idle])
+
+
+# prompts: runs of tokens that follow one another, of lengths around the tiles' and the copies' sizes, with adapters of many ranks
+RUNS = [(200, 14336, 72, 64, (128, 72)), (300, 128, 16384, 32, (255, 45)), (1021, 1024, 136, 128, (127, 1, 129, 33, 500, 31, 200)), (640, 4096, 512, 256, (320, 320)),
+        (900, 256, 4104, 16, (32, 96, 64, 700, 8)), (1500, 14336, 200, 96, (1, 2, 3, 1494)), (2500, 512, 1032, 48, (1250, 1250))]
+
+
+@pytest.mark.parametrize("mixed", [False, True])
+@pytest.mark.parametrize("M,K,N,r,lengths", RUNS)
+def test_prompts(aser, M, K, N, r, lengths, mixed):
+    """Tokens that follow one another and the same ones scattered; rows of X, Y and out apart from one another."""
+    assert launches_two(aser, M, K, N, r, len(lengths))
+    g = gen(M + r)
+    A, B, ranks, scale, _ = make(g, M, K, N, r, len(lengths), spread=False)
+    ranks[1::2] = torch.tensor([max(16, r // 32 * 16)], device="cuda", dtype=torch.int32)
+    slot = torch.cat([torch.full((n,), a, device="cuda", dtype=torch.int32) for a, n in enumerate(lengths)])
+    slot = torch.cat([slot[:M // 2], torch.full((M - slot.numel(),), -1, device="cuda", dtype=torch.int32), slot[M // 2:]])
+    if mixed:
+        slot = slot[torch.randperm(M, device="cuda", generator=g)].contiguous()
+    X = normal(g, M, K + 8)[:, :K]
+    wide = normal(g, M, 2 * N + 16)
+    Y = wide[:, 8:8 + N]
+    keep = wide.clone()
+    pool = aser.AserAdapters(A, B, scale=scale, ranks=ranks)
+    plan = pool.plan(slot)
+    ref, bound = expected(X, Y, A, B, ranks, scale, slot)
+    guard = torch.full((M + 2, N + 24), 5.0, device="cuda", dtype=torch.float16)
+    out = guard[1:M + 1, 16:16 + N]
+    pool.add(X, Y, plan, out=out)
+    assert_close(out, ref, bound)
+    assert torch.equal(wide, keep)
+    pool.add(X, Y, plan)
+    assert torch.equal(Y, out)
+    wide[:, 8:8 + N] = keep[:, 8:8 + N]
+    assert torch.equal(wide, keep)                  # nothing beside the range
+    out.fill_(5.0)
+    assert (guard == 5.0).all()
+
+
+def test_prompts_on_two_streams_and_in_a_graph(aser):
+    """One pool and one plan from two streams at once, and captured; every call has a workspace of its own."""
+    g = gen(31)
+    M, K, N, r = 1200, 2048, 1024, 64
+    assert launches_two(aser, M, K, N, r, 4)
+    A, B, ranks, scale, slot = make(g, M, K, N, r, 4)
+    pool = aser.AserAdapters(A, B, scale=scale, ranks=ranks)
+    plan = pool.plan(slot)
+    Xs, Ys = [normal(g, M, K) for _ in range(2)], [normal(g, M, N) for _ in range(2)]
+    want = [pool.add(x, y, plan, out=torch.empty_like(y)) for x, y in zip(Xs, Ys)]
+    streams, outs = [torch.cuda.Stream() for _ in range(2)], [torch.empty_like(y) for y in Ys]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                pool.add(Xs[i], Ys[i], plan, out=outs[i])
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(outs, want))
+    graph = torch.cuda.CUDAGraph()
+    x, y = Xs[0].clone(), Ys[0].clone()
+    with torch.cuda.graph(graph):
+        pool.add(x, y, plan, out=outs[0])
+    for i in (1, 0, 1):
+        x.copy_(Xs[i])
+        y.copy_(Ys[i])
+        graph.replay()
+        assert torch.equal(outs[0], want[i])
 
 
 def test_defaults_and_layout(aser):

@@ -74,10 +74,10 @@ def test_adapters_are_refused(lib):
     assert call(X=None) == NULL and call(A=None) == NULL and call(B=None) == NULL and call(plan=None) == NULL
     assert call(Y=None) == NULL and call(out=None) == NULL and call(ranks=ODD) == ALIGN and call(out=ODD) == ALIGN
     assert call(nbytes=lib.aser_adapters_plan_bytes(8, 4) - 1) == WORKSPACE
-    need = lib.aser_adapters_workspace_bytes(500, 16, 4)
-    assert need == 500 * (2 * 16 + 4) and lib.aser_adapters_workspace_bytes(96, 16, 4) == 0
-    assert lib.aser_adapters_workspace_bytes(500, 24, 4) == 0 and lib.aser_adapters_workspace_bytes(-1, 16, 4) == 0
-    assert call(M=500, ws=None) == WORKSPACE and call(M=500, wbytes=need - 1) == WORKSPACE and call(M=500, ws=ODD) == WORKSPACE
+    need = lib.aser_adapters_workspace_bytes(5000, 64, 256, 16, 4)
+    assert need == 5000 * (2 * 16 + 4) and lib.aser_adapters_workspace_bytes(32, 64, 256, 16, 1) == 0
+    assert lib.aser_adapters_workspace_bytes(5000, 64, 256, 24, 4) == 0 and lib.aser_adapters_workspace_bytes(-1, 64, 256, 16, 4) == 0
+    assert call(M=5000, ws=None) == WORKSPACE and call(M=5000, wbytes=need - 1) == WORKSPACE and call(M=5000, ws=ODD) == WORKSPACE
 
 
 def test_projection_with_adapters_is_refused(lib):
