@@ -7,17 +7,22 @@
 // barriers and no cross-CTA reduction:
 //   * a CTA owns 16 or 32 output channels for the WHOLE of K, its eight warps take every eighth
 //     128-column block; the only exchange is one shared-memory sum over the eight warps;
-//   * every thread keeps 128 bytes of packed weights in flight as 16-byte loads into registers
-//     (issued before anything else, refilled as they are consumed); the loads of a warp cover
-//     whole 128-byte lines of the blocked weight layout (eight rows x 16 bytes per 32-column
-//     sub-block).  A per-thread cp.async ring in shared memory (twice the bytes in flight) was
+//   * every thread keeps 128 bytes of packed weights in flight as 8-byte loads into registers
+//     (issued before anything else, refilled as they are consumed).  What bounds the kernel beside HBM is the
+//     number of lines that the lanes of a load touch in L1, half a warp at a time: a thread takes 16 neighbouring columns
+//     of either half of a block (two lines per half warp; its activations are then 16 contiguous bytes twice, 64 a row),
+//     not the 32 of one sub-block (16-byte loads, four lines per quarter warp: 16 cycles for 512 bytes instead of 8, L1 83 %
+//     busy; 28672 x 4096, 8 / 16 tokens 15.4 / 20.6 -> 13.6 / 17.8 us, 14336 x 4096 9.4 / 12.2 -> 8.0 / 10.5, 4096 x 4096, one token 5.2 ->
+//     4.7);  A per-thread cp.async ring in shared memory (twice the bytes in flight) was
 //     measured 20-50 % slower: the shared memory it takes is L1 capacity that the activation
 //     fragments then miss;
 //   * the packed word is turned into two int8x4 registers (16 * q) by two logic operations and
 //     fed to mma.sync m16n8k32 (weights on the 16-row side, tokens on the 8-column side).  An
 //     integer dot product does not care about the order of k, so a thread's k positions are
 //     simply the 32 columns it loaded; the activation fragment reads the same 32 columns of
-//     its token's row of Xq (32 contiguous bytes, served by L1/L2: Xq is at most 16 x K bytes);
+//     its token's row of Xq (served by L1/L2: Xq is at most 16 x K bytes);
+//   * more tiles than CTAs are resident: a CTA takes several, and asks for the next one's first weights while it finishes
+//     the sums of this one (28672 x 4096, one token 14.7 -> 13.7 us);
 //   * the low-rank term is a (16 or 32) x M x r product per CTA: warp w takes the 16-wide slices
 //     w and w + 8 of r on mma.sync m16n8k16 (L_B rows from global memory, T converted bf16 ->
 //     fp16 in registers); its few loads are issued right behind the first weight loads and it is
@@ -37,11 +42,11 @@ namespace {
 constexpr int kDecWarps = 8;
 constexpr int kDecThreads = kDecWarps * 32;
 
+// A row's 32 columns of a thread: 8 bytes of a block's first half (words 2 (t & 1) and + 1 of sub-block t / 2) and 8 of its second.
 __device__ __forceinline__ uint4 ld_stream16(const uint8_t* p) {
     uint4 v;
-    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
-                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-                 : "l"(p));
+    asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
+    asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(v.z), "=r"(v.w) : "l"(p + 2 * kWkRows * 16));
     return v;
 }
 __device__ __forceinline__ void dep_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
@@ -111,11 +116,11 @@ linear_decode_kernel(const int8_t* Xq, const float* a_scale, const __nv_bfloat16
         }
         n0 = (tile - first) * C::Rows;
     };
-    // Rows n0 + 16 rt + g and + 8 of sub-block t (columns 32 t .. 32 t + 31 of a block).  The
+    // Rows n0 + 16 rt + g and + 8, columns 16 t .. 16 t + 15 of either half of a block.  The
     // blocked layout pads the last 128-row tile with zero codes, so rows past N inside that tile
     // read as zeros; a CTA never reaches past the tile (16 R divides 128).
     auto weights = [&](int layer, int n0) {
-        return group.Wk[layer] + ((size_t)(n0 >> 7) * KB) * kWkBlockBytes + t * (kWkRows * 16) + ((n0 & 127) + g) * 16;
+        return group.Wk[layer] + ((size_t)(n0 >> 7) * KB) * kWkBlockBytes + (t >> 1) * (kWkRows * 16) + ((n0 & 127) + g) * 16 + (t & 1) * 8;
     };
     int layer, n0;
     find((int)blockIdx.x, layer, n0);
@@ -207,13 +212,13 @@ linear_decode_kernel(const int8_t* Xq, const float* a_scale, const __nv_bfloat16
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int e = 0; e < 4; ++e) c[rt][nt][e] = 0;
-    // activation fragment: 32 bytes of token g (+ 8 nt) at the columns this thread loaded
+    // activation fragment: twice 16 bytes of token g (+ 8 nt) at the columns this thread loaded
     const int8_t* xrow[NT];
     bool x_ok[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         x_ok[nt] = g + 8 * nt < M;
-        xrow[nt] = Xq + (size_t)(x_ok[nt] ? g + 8 * nt : 0) * K + t * 32;
+        xrow[nt] = Xq + (size_t)(x_ok[nt] ? g + 8 * nt : 0) * K + t * 16;
     }
     for (int kb0 = warp; kb0 < KB; kb0 += kDecWarps * BATCH) {
 #pragma unroll
@@ -227,7 +232,7 @@ linear_decode_kernel(const int8_t* Xq, const float* a_scale, const __nv_bfloat16
                     if (x_ok[nt]) {
                         const uint4* xp = reinterpret_cast<const uint4*>(xrow[nt] + kbi * kWkCols);
                         lo = xp[0];
-                        hi = xp[1];
+                        hi = xp[4];
                     }
                     b[nt][0] = lo.x; b[nt][1] = lo.y; b[nt][2] = lo.z; b[nt][3] = lo.w;
                     b[nt][4] = hi.x; b[nt][5] = hi.y; b[nt][6] = hi.z; b[nt][7] = hi.w;
@@ -239,7 +244,7 @@ linear_decode_kernel(const int8_t* Xq, const float* a_scale, const __nv_bfloat16
                     const uint32_t w1[4] = {wa[i][rt][1].x, wa[i][rt][1].y, wa[i][rt][1].z, wa[i][rt][1].w};
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        // word j: columns 8 j .. 8 j + 3 in the low nibbles, 8 j + 4 .. 8 j + 7 in the high
+                        // word j: four columns in the low nibbles, the next four in the high
                         const uint32_t a0 = (w0[j] << 4) & 0xF0F0F0F0u, a2 = w0[j] & 0xF0F0F0F0u;
                         const uint32_t a1 = (w1[j] << 4) & 0xF0F0F0F0u, a3 = w1[j] & 0xF0F0F0F0u;
 #pragma unroll
