@@ -552,16 +552,16 @@ class AserSharedInputCat(AserSharedInput):
         return self._views(M)
 
 
-def _rows(v: torch.Tensor, M: int, cols: int, name: str) -> int:
-    """Elements between the rows of an fp16 matrix [M, cols] whose rows are contiguous."""
-    if not v.is_cuda or v.dtype != torch.float16 or v.dim() != 2 or v.shape[0] != M or v.shape[1] != cols:
-        raise TypeError("%s: need a CUDA tensor of torch.float16, [%d, %d]" % (name, M, cols))
+def _rows(v: torch.Tensor, shape: tuple, name: str) -> int:
+    """Elements between the rows of an fp16 matrix of that shape whose rows are contiguous."""
+    if v.shape != shape or v.dtype is not torch.float16 or not v.is_cuda:
+        raise TypeError("%s: need a CUDA tensor of torch.float16, [%d, %d]" % (name, *shape))
     ld, step = v.stride()
-    if M <= 1 and (cols <= 1 or step == 1):
-        return cols                                     # (the stride of a dimension of one element says nothing)
-    if step != 1 or ld < cols:
-        raise TypeError("%s: rows need to be contiguous and apart" % name)
-    return ld
+    if step == 1 and ld >= shape[1]:
+        return ld
+    if shape[0] <= 1 and (step == 1 or shape[1] <= 1):
+        return shape[1]                                 # (the stride of a dimension of one element says nothing)
+    raise TypeError("%s: rows need to be contiguous and apart" % name)
 
 
 class AdapterPlan:
@@ -603,6 +603,7 @@ class AserAdapters:
             if v is not None and _dev(v, dtype, name).shape != (self.n_slots,):
                 raise ValueError("%s needs one element per adapter" % name)
         self.A, self.B, self.scale, self.ranks = A, B, scale, ranks
+        self._ws_bytes = {}
 
     def plan(self, slot: torch.Tensor) -> AdapterPlan:
         """slot int32 [M]: the adapter of each token, anything outside 0 .. slots - 1 for none."""
@@ -614,23 +615,31 @@ class AserAdapters:
 
     def _workspace(self, M: int):
         """What a call of many tokens keeps between its two launches: torch's memory of the current stream."""
-        nbytes = lib.aser_adapters_workspace_bytes(M, self.N, self.K, self.r, self.n_slots)
+        nbytes = self._ws_bytes.get(M)
+        if nbytes is None:
+            nbytes = self._ws_bytes[M] = lib.aser_adapters_workspace_bytes(M, self.N, self.K, self.r, self.n_slots)
         return None if nbytes == 0 else torch.empty((nbytes,), dtype=torch.uint8, device=self.A.device)
 
     def add(self, X: torch.Tensor, Y: torch.Tensor, plan: AdapterPlan, out: torch.Tensor | None = None) -> torch.Tensor:
         """out = Y + scale B (A x) by each token's adapter; X fp16 [M, K], Y and out fp16 [M, N], rows of which may be apart
         (a column range of a fused projection).  Without `out` in place."""
-        if out is None:
-            out = Y
+        # (a call of a few tokens is shorter on the GPU than from here, as everywhere in this file)
         M = X.shape[0]
-        ldx, ldy, ldo = _rows(X, M, self.K, "X"), _rows(Y, M, self.N, "Y"), _rows(out, M, self.N, "out")
-        self._check_plan(plan, M)
-        scale, ranks, ws = self.scale, self.ranks, self._workspace(M)
+        ldx = _rows(X, (M, self.K), "X")
+        ldy = _rows(Y, (M, self.N), "Y")
+        y_at = Y.data_ptr()
+        if out is None:
+            out, ldo, out_at = Y, ldy, y_at
+        else:
+            ldo, out_at = _rows(out, (M, self.N), "out"), out.data_ptr()
+        if plan is None or plan.M != M or plan.n_slots != self.n_slots:
+            self._check_plan(plan, M)
+        scale, ranks = self.scale, self.ranks
+        ws = self._workspace(M) if M > 32 else None
         rc = lib.aser_adapters_add(X.data_ptr(), ldx, self.A.data_ptr(), self.B.data_ptr(),
                                    None if ranks is None else ranks.data_ptr(), None if scale is None else scale.data_ptr(),
-                                   plan.data.data_ptr(), plan.nbytes, M, self.N, self.K, self.r, self.n_slots, Y.data_ptr(),
-                                   ldy, out.data_ptr(), ldo, None if ws is None else ws.data_ptr(),
-                                   0 if ws is None else ws.numel(), _stream())
+                                   plan.data.data_ptr(), plan.nbytes, M, self.N, self.K, self.r, self.n_slots, y_at, ldy, out_at,
+                                   ldo, None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), _stream())
         if rc != 0:
             raise AserError(rc, "aser_adapters_add")
         return out
@@ -640,7 +649,7 @@ class AserAdapters:
         if M > layer.max_tokens or (layer.K, layer.N) != (self.K, self.N):
             raise ValueError("%d tokens of a [%d, %d] layer and adapters of [%d, %d]: they do not fit"
                              % (M, layer.N, layer.K, self.N, self.K))
-        if _rows(X, M, self.K, "X") != self.K:
+        if _rows(X, (M, self.K), "X") != self.K:
             raise TypeError("X: rows need to be adjacent")
         self._check_plan(plan, M)
         r = layer.r if lowrank else 0
