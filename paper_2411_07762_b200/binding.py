@@ -286,6 +286,8 @@ def linear_w4a8_lr_glu(Xq, a_scale, Wk, w_scale, T, L_B, N: int, ws: torch.Tenso
     r = 0 if L_B is None else L_B.shape[1]
     if H is None:
         H = torch.empty((M, N // 2), dtype=torch.float16, device=Xq.device)
+    elif _dev(H, torch.float16, "H").dim() != 2 or H.shape[0] < M or H.shape[1] != N // 2:
+        raise ValueError("H needs %d rows of %d" % (M, N // 2))
     _chk(lib.aser_linear_w4a8_lr_glu(_ptr(Xq), _ptr(a_scale), _ptr(Wk), _ptr(w_scale), _ptr(T) if r else None,
                                      _ptr(L_B) if r else None, M, N, K, r, _activation(activation), _ptr(H), _ptr(ws),
                                      ws.numel(), _stream()), "aser_linear_w4a8_lr_glu")
@@ -424,6 +426,8 @@ class AserLinear:
         M = X.shape[0]
         if adapters is not None:
             return adapters._forward(self, X, plan, lowrank)
+        if plan is not None:
+            raise ValueError("a plan without adapters")
         assert M <= self.max_tokens
         r = self.r if lowrank else 0       # the plain W4A8 control: the same entry point at rank 0
         s, Y, ws = self.s, self.Y, self.ws
@@ -552,15 +556,15 @@ class AserSharedInputCat(AserSharedInput):
         return self._views(M)
 
 
-def _rows(v: torch.Tensor, shape: tuple, name: str) -> int:
-    """Elements between the rows of an fp16 matrix of that shape whose rows are contiguous."""
-    if v.shape != shape or v.dtype is not torch.float16 or not v.is_cuda:
-        raise TypeError("%s: need a CUDA tensor of torch.float16, [%d, %d]" % (name, *shape))
+def _rows(v: torch.Tensor, shape: tuple, name: str, device: int) -> int:
+    """Elements between the rows of an fp16 matrix of that shape on that GPU whose rows are contiguous."""
+    if v.shape != shape or v.dtype is not torch.float16 or v.get_device() != device:
+        raise TypeError("%s: need a tensor of torch.float16, [%d, %d], on the current GPU" % (name, *shape))
     ld, step = v.stride()
-    if step == 1 and ld >= shape[1]:
-        return ld
     if shape[0] <= 1 and (step == 1 or shape[1] <= 1):
         return shape[1]                                 # (the stride of a dimension of one element says nothing)
+    if step == 1 and ld >= shape[1]:
+        return ld
     raise TypeError("%s: rows need to be contiguous and apart" % name)
 
 
@@ -574,6 +578,7 @@ class AdapterPlan:
         if nbytes == 0:
             raise ValueError("unsupported number of tokens or adapters")
         self.nbytes = nbytes
+        self.device = slot.get_device()
         self.data = torch.empty((nbytes,), dtype=torch.uint8, device=slot.device)
         self.update(slot)
 
@@ -581,6 +586,8 @@ class AdapterPlan:
         _dev(slot, torch.int32, "slot")
         if slot.dim() != 1 or slot.numel() != self.M:
             raise ValueError("slot needs one dimension of %d tokens" % self.M)
+        if slot.get_device() != self.device or self.device != torch._C._cuda_getDevice():
+            raise ValueError("slot and plan need to be on the current GPU")
         _chk(lib.aser_adapters_plan(_ptr(slot), self.M, self.n_slots, _ptr(self.data), self.nbytes, _stream()),
              "aser_adapters_plan")
         return self
@@ -603,15 +610,20 @@ class AserAdapters:
             if v is not None and _dev(v, dtype, name).shape != (self.n_slots,):
                 raise ValueError("%s needs one element per adapter" % name)
         self.A, self.B, self.scale, self.ranks = A, B, scale, ranks
+        self.device = A.get_device()
+        if any(v is not None and v.get_device() != self.device for v in (B, scale, ranks)):
+            raise ValueError("a pool's tensors need to be on one GPU")
         self._ws_bytes = {}
 
     def plan(self, slot: torch.Tensor) -> AdapterPlan:
         """slot int32 [M]: the adapter of each token, anything outside 0 .. slots - 1 for none."""
         return AdapterPlan(slot, self.n_slots)
 
-    def _check_plan(self, plan, M: int):
+    def _check_plan(self, plan, M: int, device: int):
         if plan is None or plan.M != M or plan.n_slots != self.n_slots:
             raise ValueError("need a plan of %d tokens and %d adapters" % (M, self.n_slots))
+        if not plan.device == self.device == device:
+            raise ValueError("adapters and plan need to be on the current GPU")
 
     def _workspace(self, M: int):
         """What a call of many tokens keeps between its two launches: torch's memory of the current stream."""
@@ -624,16 +636,15 @@ class AserAdapters:
         """out = Y + scale B (A x) by each token's adapter; X fp16 [M, K], Y and out fp16 [M, N], rows of which may be apart
         (a column range of a fused projection).  Without `out` in place."""
         # (a call of a few tokens is shorter on the GPU than from here, as everywhere in this file)
-        M = X.shape[0]
-        ldx = _rows(X, (M, self.K), "X")
-        ldy = _rows(Y, (M, self.N), "Y")
+        M, device = X.shape[0], torch._C._cuda_getDevice()
+        ldx = _rows(X, (M, self.K), "X", device)
+        ldy = _rows(Y, (M, self.N), "Y", device)
         y_at = Y.data_ptr()
         if out is None:
             out, ldo, out_at = Y, ldy, y_at
         else:
-            ldo, out_at = _rows(out, (M, self.N), "out"), out.data_ptr()
-        if plan is None or plan.M != M or plan.n_slots != self.n_slots:
-            self._check_plan(plan, M)
+            ldo, out_at = _rows(out, (M, self.N), "out", device), out.data_ptr()
+        self._check_plan(plan, M, device)
         scale, ranks = self.scale, self.ranks
         ws = self._workspace(M) if M > 32 else None
         rc = lib.aser_adapters_add(X.data_ptr(), ldx, self.A.data_ptr(), self.B.data_ptr(),
@@ -649,9 +660,12 @@ class AserAdapters:
         if M > layer.max_tokens or (layer.K, layer.N) != (self.K, self.N):
             raise ValueError("%d tokens of a [%d, %d] layer and adapters of [%d, %d]: they do not fit"
                              % (M, layer.N, layer.K, self.N, self.K))
-        if _rows(X, (M, self.K), "X") != self.K:
+        device = torch._C._cuda_getDevice()
+        if _rows(X, (M, self.K), "X", device) != self.K:
             raise TypeError("X: rows need to be adjacent")
-        self._check_plan(plan, M)
+        self._check_plan(plan, M, device)
+        if layer.Wk.get_device() != device:
+            raise ValueError("the layer needs to be on the current GPU")
         r = layer.r if lowrank else 0
         ws = self._workspace(M)
         rc = lib.aser_forward_adapters(X.data_ptr(), _ptr(layer.s), layer.L_A.data_ptr() if r else None, layer.Wk.data_ptr(),
@@ -711,8 +725,11 @@ class AserGatedFFN:
 
     def __call__(self, X: torch.Tensor) -> torch.Tensor:
         """Y [M, N] (a view of a preallocated buffer) of X fp16 [M, K], M up to max_tokens."""
-        if X.dtype != torch.float16 or not X.is_cuda or not X.is_contiguous() or X.dim() != 2 or X.shape[1] != self.K:
-            raise TypeError("X: need a contiguous CUDA tensor of torch.float16, [M, %d]" % self.K)
+        device = torch._C._cuda_getDevice()
+        if X.dtype != torch.float16 or X.get_device() != device or not X.is_contiguous() or X.dim() != 2 or X.shape[1] != self.K:
+            raise TypeError("X: need a contiguous tensor of torch.float16, [M, %d], on the current GPU" % self.K)
+        if self.Y.get_device() != device:
+            raise ValueError("the block needs to be on the current GPU")
         M = X.shape[0]
         if M > self.max_tokens:
             raise ValueError("%d tokens, but the block was made for %d" % (M, self.max_tokens))

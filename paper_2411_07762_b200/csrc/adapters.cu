@@ -403,7 +403,7 @@ int launch_adapters_plan(const int32_t* slot, int M, int n_slots, void* plan, cu
 // adapters: 32 16.3 | 19.2, 64 30.4 | 21.3; 4096 x 14336, rank 128, 16 adapters: 8 36.4 | 30.9; 1024 x 1024, rank 32, 16 adapters:
 // 32 9.6 | 10.6, 64 14.0 | 10.7.
 bool adapters_many(int M, int N, int K, int r, int n_slots) {
-    if (M <= 32) return false;
+    if (M <= 32 || r == 0) return false;
     const float used = 0.5f * (n_slots < M ? n_slots : M), wide = (float)(K + N) / 8192;
     const float few_tiles = M / 16.f + 0.5f * used, many_tiles = fmaxf(used, M / 128.f + 0.5f * used);
     const float few = few_tiles * (0.07f + wide * (0.24f + 0.1f * r / 64));

@@ -300,7 +300,8 @@ constexpr int kUpSums = 4;                            // blocks whose sums are i
 constexpr uint32_t kUpTmem = kUpSums * kCols;
 
 // Blocks of 64 channels [c n / chunks, (c + 1) n / chunks) of a tile; `resident` CTAs are dealt over the tiles that there are.  What wrote Y and the plan is known to be complete when this
-// kernel starts, because the first kernel waited for it; S is waited for.
+// kernel starts, because the first kernel waited for it; S is waited for.  Whatever a CTA of a tile has to do, it waits for the first
+// kernel before it ends: who waits for this kernel has waited for both.
 __global__ void __launch_bounds__(kUpThreads, 2)
 adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, int resident) {
     extern __shared__ uint8_t smem_raw[];
@@ -309,7 +310,7 @@ adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, i
     const PlanView plan = plan_view(p.plan, p.M, p.n_slots);
     const int4 head = *reinterpret_cast<const int4*>(p.plan), more = *reinterpret_cast<const int4*>(p.plan + 4);
     const int tiles = p.Y == p.out ? more.x : head.w;        // (in place, those without an adapter, the last ones, have nothing to do)
-    if (head.x != p.M || head.y != p.n_slots || tiles == 0) return;
+    if (head.x != p.M || head.y != p.n_slots || tiles == 0) { grid_dep_wait(); return; }
     const int blocks = (p.N + kCols - 1) / kCols;
     int chunks = resident / tiles;                           // (two blocks and more for a CTA)
     chunks = chunks < 1 ? 1 : chunks > (blocks + 1) / 2 ? (blocks + 1) / 2 : chunks;
@@ -327,6 +328,7 @@ adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, i
                 for (int c = b0 * kCols + lane * 8; c < (b0 + n) * kCols && c < p.N; c += 256)
                     *reinterpret_cast<uint4*>(p.out + tok * p.ldo + c) = *reinterpret_cast<const uint4*>(p.Y + tok * p.ldy + c);
             }
+        grid_dep_wait();
         return;
     }
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -507,6 +509,11 @@ adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, i
 // Tiles that a call probably has (the host does not know which adapters are in use): a quarter of them leave a short one.
 int likely_tiles(const AdapterParams& p) { return (p.M + kTok - 1) / kTok + (p.n_slots < p.M ? p.n_slots : p.M) / 4; }
 
+// Boxes of `box` rows by 64 columns, 128 bytes a row, of an fp16 matrix.
+int rows_map(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint64_t ld, uint32_t box) {
+    return encode_map_2d_ld(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, base, rows, cols, ld, box, kCols, CU_TENSOR_MAP_SWIZZLE_128B, /*keep=*/false);
+}
+
 template <typename Kernel>
 int opt_in(Kernel* kernel, int bytes, bool (&configured)[kMaxDevices], int* num_sms) {
     int dev = 0;
@@ -527,10 +534,9 @@ int launch_adapters_down(const AdapterParams& p, cudaStream_t st) {
     int rc = opt_in(adapters_down_kernel, down_smem(256), configured, &num_sms);
     if (rc != ASER_OK) return rc;
     DownMaps maps;
-    const CUtensorMapDataType f16 = CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-    rc = encode_map_2d_ld(&maps.x, f16, 2, p.X, p.M, p.K, p.ldx, kBox, kCols, CU_TENSOR_MAP_SWIZZLE_128B);
-    if (rc == ASER_OK) rc = encode_map_2d_ld(&maps.x_one, f16, 2, p.X, p.M, p.K, p.ldx, 1, kCols, CU_TENSOR_MAP_SWIZZLE_128B);
-    if (rc == ASER_OK) rc = encode_map_2d(&maps.a, f16, 2, p.A, (uint64_t)p.n_slots * p.r, p.K, 16, kCols, CU_TENSOR_MAP_SWIZZLE_128B);
+    rc = rows_map(&maps.x, p.X, p.M, p.K, p.ldx, kBox);
+    if (rc == ASER_OK) rc = rows_map(&maps.x_one, p.X, p.M, p.K, p.ldx, 1);
+    if (rc == ASER_OK) rc = rows_map(&maps.a, p.A, (uint64_t)p.n_slots * p.r, p.K, p.K, 16);
     if (rc != ASER_OK) return rc;
     // about as many CTAs as there are SMs; each has two steps of K at least
     int CL = (num_sms + num_sms / 10) / likely_tiles(p);
@@ -562,13 +568,11 @@ int launch_adapters_up(const AdapterParams& p, cudaStream_t st) {
     int rc = opt_in(adapters_up_kernel, up_smem(256), configured, &num_sms);
     if (rc != ASER_OK) return rc;
     UpMaps maps;
-    const CUtensorMapDataType f16 = CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-    rc = encode_map_2d_ld(&maps.y, f16, 2, p.Y, p.M, p.N, p.ldy, kBox, kCols, CU_TENSOR_MAP_SWIZZLE_128B);
-    if (rc == ASER_OK) rc = encode_map_2d_ld(&maps.y_one, f16, 2, p.Y, p.M, p.N, p.ldy, 1, kCols, CU_TENSOR_MAP_SWIZZLE_128B);
-    if (rc == ASER_OK) rc = encode_map_2d(&maps.s, f16, 2, p.S, p.M, p.r, kBox, 64, CU_TENSOR_MAP_SWIZZLE_128B);
-    if (rc == ASER_OK) rc = encode_map_2d(&maps.b, f16, 2, p.B, (uint64_t)p.n_slots * p.N, p.r, kCols, 64, CU_TENSOR_MAP_SWIZZLE_128B);
-    if (rc != ASER_OK) return rc;
-    rc = encode_map_2d_ld(&maps.out, f16, 2, p.out, p.M, p.N, p.ldo, kBox, kCols, CU_TENSOR_MAP_SWIZZLE_128B);
+    rc = rows_map(&maps.y, p.Y, p.M, p.N, p.ldy, kBox);
+    if (rc == ASER_OK) rc = rows_map(&maps.y_one, p.Y, p.M, p.N, p.ldy, 1);
+    if (rc == ASER_OK) rc = rows_map(&maps.s, p.S, p.M, p.r, p.r, kBox);
+    if (rc == ASER_OK) rc = rows_map(&maps.b, p.B, (uint64_t)p.n_slots * p.N, p.r, p.r, kCols);
+    if (rc == ASER_OK) rc = rows_map(&maps.out, p.out, p.M, p.N, p.ldo, kBox);
     if (rc != ASER_OK) return rc;
     const int resident = (p.r <= 128 ? 2 : 1) * num_sms, bound = plan_tiles(p.M, p.n_slots, kTok);
     cudaLaunchConfig_t cfg = {};

@@ -377,15 +377,7 @@ struct MapKey {
     uint32_t dtype, rank, swizzle;
 };
 
-inline int encode_tiled(CUtensorMap* map, const MapKey& key, const char* what) {
-    struct Entry { MapKey key; CUtensorMap map; bool used; };
-    constexpr int kEntries = 256;
-    static thread_local Entry table[kEntries];
-    uint64_t h = 1469598103934665603ull;
-    const unsigned char* kb = reinterpret_cast<const unsigned char*>(&key);
-    for (size_t i = 0; i < sizeof(MapKey); ++i) h = (h ^ kb[i]) * 1099511628211ull;
-    Entry& e = table[(h ^ (h >> 32)) % kEntries];
-    if (e.used && memcmp(&e.key, &key, sizeof(MapKey)) == 0) { *map = e.map; return ASER_OK; }
+inline int encode_now(CUtensorMap* map, const MapKey& key, const char* what) {
     EncodeTiledFn fn = get_encode_fn();
     if (!fn) return record_cuda_error(cudaErrorUnknown, "cuTensorMapEncodeTiled unavailable");
     cuuint64_t dims[3] = {key.dims[0], key.dims[1], key.dims[2]};
@@ -395,7 +387,19 @@ inline int encode_tiled(CUtensorMap* map, const MapKey& key, const char* what) {
     CUresult r = fn(map, (CUtensorMapDataType)key.dtype, key.rank, const_cast<void*>(key.base), dims,
                     strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, (CUtensorMapSwizzle)key.swizzle,
                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    if (r != CUDA_SUCCESS) return record_cuda_error(cudaErrorInvalidValue, what);
+    return r == CUDA_SUCCESS ? ASER_OK : record_cuda_error(cudaErrorInvalidValue, what);
+}
+
+inline int encode_tiled(CUtensorMap* map, const MapKey& key, const char* what) {
+    struct Entry { MapKey key; CUtensorMap map; bool used; };
+    constexpr int kEntries = 256;
+    static thread_local Entry table[kEntries];
+    uint64_t h = 1469598103934665603ull;
+    const unsigned char* kb = reinterpret_cast<const unsigned char*>(&key);
+    for (size_t i = 0; i < sizeof(MapKey); ++i) h = (h ^ kb[i]) * 1099511628211ull;
+    Entry& e = table[(h ^ (h >> 32)) % kEntries];
+    const int rc = encode_now(map, key, what);
+    if (rc != ASER_OK) return rc;
     e.key = key; e.map = *map; e.used = true;
     return ASER_OK;
 }
@@ -410,14 +414,15 @@ inline MapKey make_key(const void* base, CUtensorMapDataType dt, uint32_t rank, 
 // 2-D row-major tensor [rows, cols] of `esize`-byte elements whose rows are `ld` elements apart
 // (a column range of a wider matrix), box = [box_rows, box_cols] with the given shared-memory
 // swizzle; out-of-range elements read as zero and are not written.
+// `keep`: by encode_tiled (a tensor whose address changes from call to call has no use for it).
 inline int encode_map_2d_ld(CUtensorMap* map, CUtensorMapDataType dt, int esize, const void* base,
                             uint64_t rows, uint64_t cols, uint64_t ld, uint32_t box_rows,
-                            uint32_t box_cols, CUtensorMapSwizzle swizzle) {
+                            uint32_t box_cols, CUtensorMapSwizzle swizzle, bool keep = true) {
     MapKey k = make_key(base, dt, 2, swizzle);
     k.dims[0] = cols; k.dims[1] = rows;
     k.strides[0] = ld * (uint64_t)esize;
     k.box[0] = box_cols; k.box[1] = box_rows;
-    return encode_tiled(map, k, "cuTensorMapEncodeTiled");
+    return keep ? encode_tiled(map, k, "cuTensorMapEncodeTiled") : encode_now(map, k, "cuTensorMapEncodeTiled");
 }
 
 // The same with contiguous rows.

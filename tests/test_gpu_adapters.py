@@ -357,6 +357,41 @@ def test_refusals(aser):
     layer = aser.AserLinear(normal(g, 128, 256, scale=0.03), None, None, None, 8)
     with pytest.raises(ValueError):
         layer(X, adapters=pool, plan=plan)                   # another number of channels
+    with pytest.raises(ValueError):
+        layer(X, plan=plan)
+
+
+@pytest.mark.parametrize("M", [1, 20, 300, 3000])
+def test_no_rank(aser, M):
+    """A pool of rank 0 copies, or leaves alone."""
+    g = gen(M)
+    pool = aser.AserAdapters(torch.empty(3, 0, 256, device="cuda", dtype=torch.float16), torch.empty(3, 136, 0, device="cuda", dtype=torch.float16))
+    X, Y = normal(g, M, 256), normal(g, M, 136)
+    plan = pool.plan(torch.randint(-1, 3, (M,), device="cuda", generator=g, dtype=torch.int32))
+    out = torch.full((M + 1, 136), 7.0, device="cuda", dtype=torch.float16)
+    assert torch.equal(pool.add(X, Y, plan, out=out[:M]), Y) and (out[M] == 7.0).all()
+    keep = Y.clone()
+    assert torch.equal(pool.add(X, Y, plan), keep)
+
+
+@pytest.mark.parametrize("M", [40, 1500])
+def test_no_token_has_an_adapter(aser, M):
+    """Nor a rank: with other adapters' tokens in the next call, one call after the other on a stream."""
+    g = gen(M)
+    A, B, ranks, scale, slot = make(g, M, 1024, 1032, 32, 3, spread=False)
+    X, Y = normal(g, M, 1024), normal(g, M, 1032)
+    pool = aser.AserAdapters(A, B, scale=scale, ranks=ranks)
+    ref, bound = expected(X, Y, A, B, ranks, scale, slot)
+    none, some = torch.full_like(slot, -1), slot.clone()
+    empty = aser.AserAdapters(A, B, scale=scale, ranks=torch.zeros_like(ranks))
+    plan = pool.plan(none)
+    for rep in range(3):
+        out = torch.full_like(Y, 3.0)
+        plan.update(none)
+        assert torch.equal(pool.add(X, Y, plan, out=out), Y)
+        plan.update(some)
+        assert torch.equal(empty.add(X, Y, plan, out=out), Y)
+        assert_close(pool.add(X, Y, plan, out=out), ref, bound)
 
 
 def test_no_tokens(aser):

@@ -1,0 +1,115 @@
+"""A decoder layer's projections as a serving step runs them: a fused query/key/value projection with the adapters of many
+requests on its column ranges, an output projection with its own, and a gated feed-forward block, planned once; and layers
+of a group with more tiles than the GPU holds at once."""
+import math
+
+import pytest
+import torch
+
+from test_gpu_adapters import assert_close, expected, make
+from test_gpu_ffn import assert_product_close, Steps
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def aser():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    import paper_2411_07762_b200 as aser
+    return aser
+
+
+def gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def normal(g, *shape, scale=1.0):
+    return torch.randn(*shape, device="cuda", dtype=torch.float16, generator=g) * scale
+
+
+def divisors(g, K):
+    s = torch.ones(K, device="cuda")
+    s[torch.randperm(K, device="cuda", generator=g)[:4]] = 9.0
+    return s
+
+
+class Block:
+    """Heads of 128: 8 for queries, 2 for keys and values; the values stand in for attention's result."""
+
+    def __init__(self, aser, g, M, K=1024, F=1024, slots=5):
+        self.aser, self.M, self.K = aser, M, K
+        s, q, kv = divisors(g, K), K, 256
+        self.layers = [aser.AserLinear(normal(g, n, K, scale=1 / math.sqrt(K)), s, normal(g, 32, K, scale=0.02), normal(g, n, 32, scale=0.02), M)
+                       for n in (q, kv, kv)]
+        self.qkv = aser.AserSharedInputCat(self.layers, M)
+        self.o = aser.AserLinear(normal(g, K, kv, scale=1 / math.sqrt(kv)), divisors(g, kv), normal(g, 16, kv, scale=0.02), normal(g, K, 16, scale=0.02), M)
+        W = [normal(g, F, K, scale=1 / math.sqrt(K)) for _ in range(2)]
+        self.ffn_ops = (W[0], W[1], divisors(g, K), normal(g, 32, K, scale=0.02), normal(g, 2 * F, 32, scale=0.02),
+                        normal(g, K, F, scale=1 / math.sqrt(F)), divisors(g, F), normal(g, 32, F, scale=0.02), normal(g, K, 32, scale=0.02))
+        self.ffn = aser.AserGatedFFN(*self.ffn_ops, M)
+        self.pools = []
+        for k, n, r in ((K, q, 16), (K, kv, 64), (kv, K, 128)):             # queries, values, output
+            A, B, ranks, scale, _ = make(g, M, k, n, r, slots)
+            self.pools.append(aser.AserAdapters(A, B, scale=scale, ranks=ranks))
+
+    def __call__(self, X, slot, plan):
+        plan.update(slot)
+        q, k, v = self.qkv(X)
+        self.pools[0].add(X, q, plan)
+        self.pools[1].add(X, v, plan)
+        h = v.contiguous()
+        o = self.o(h, adapters=self.pools[2], plan=plan)
+        return q, k, v, h, o, self.ffn(o)
+
+
+@pytest.mark.parametrize("M", [1, 7, 16, 48, 700])
+def test_a_step_of_a_decoder_layer(aser, M):
+    g = gen(M)
+    block = Block(aser, g, M)
+    X = normal(g, M, block.K)
+    slot = torch.randint(-1, 5, (M,), device="cuda", generator=g, dtype=torch.int32)
+    plan = aser.AdapterPlan(slot, 5)
+    q, k, v, h, o, y = [t.clone() for t in block(X, slot, plan)]
+    base = [t.clone() for t in block.qkv(X)]
+    assert torch.equal(k, base[1])
+    for pool, x, before, after in ((block.pools[0], X, base[0], q), (block.pools[1], X, base[2], v), (block.pools[2], h, block.o(h).clone(), o)):
+        ranks = pool.ranks.clamp(0, pool.r)
+        assert_close(after, *expected(x, before, pool.A, pool.B, ranks, pool.scale, slot))
+    steps = Steps(aser, block.ffn_ops, M)
+    GU, H, want = steps(o, "silu")
+    assert_product_close(H, GU[:, 0::2], GU[:, 1::2], "silu")
+    assert torch.equal(want, y)
+
+    # captured, replayed with other requests and activations; a padded batch
+    graph = torch.cuda.CUDAGraph()
+    x_in, slot_in = X.clone(), slot.clone()
+    with torch.cuda.graph(graph):
+        outs = block(x_in, slot_in, plan)
+    for rep in range(3):
+        x_in.copy_(normal(g, M, block.K))
+        slot_in.copy_(torch.randint(-1, 6, (M,), device="cuda", generator=g))
+        slot_in[M - rep:] = -1
+        graph.replay()
+        got = [t.clone() for t in outs]
+        eager = block(x_in, slot_in, plan)
+        assert all(torch.equal(a, b) for a, b in zip(got, eager))
+
+
+@pytest.mark.parametrize("M", [1, 8, 9, 16])
+@pytest.mark.parametrize("N,K,r", [((14336, 14344), 512, (32, 32)), ((8192, 8192, 8200), 640, (16, 48, 0)), ((28672, 128), 128, (256, 16))])
+def test_groups_of_more_tiles_than_the_gpu_holds(aser, M, N, K, r):
+    """A CTA goes from one layer's tile to another's; the layers one by one have the same bits."""
+    g = gen(M + K)
+    s = divisors(g, K)
+    layers = [aser.AserLinear(normal(g, n, K, scale=0.05), s, normal(g, max(rr, 16), K, scale=0.02)[:rr] if rr else None,
+                              normal(g, n, rr, scale=0.05) if rr else None, M) for n, rr in zip(N, r)]
+    for layer in layers:
+        assert aser.lib.aser_linear_kernel(M, layer.N, K) == 0
+    X = normal(g, M, K)
+    group = aser.AserSharedInput(layers, M)
+    out = [y.clone() for y in group(X)]
+    for layer, y in zip(layers, out):
+        assert torch.equal(layer(X), y)

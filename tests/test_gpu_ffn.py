@@ -271,3 +271,8 @@ def test_refusals(aser):
             aser.AserGatedFFN(*bad, 4)
     with pytest.raises(ValueError):
         aser.AserGatedFFN(*ops, 4, activation="relu")
+    f = Steps(aser, ops, 4).first
+    f.quant(X)
+    for rows, cols in ((3, 512), (4, 504)):
+        with pytest.raises(ValueError):
+            aser.linear_w4a8_lr_glu(f.Xq, f.a_scale, f.Wk, f.w_scale, f.T, f.L_B, 1024, f.ws, H=normal(g, rows, cols))

@@ -88,3 +88,50 @@ def test_projection_with_adapters_is_refused(lib):
     assert call(K=100) == SHAPE and call(ra=8) == SHAPE and call(r=8) == SHAPE and call(N=12) == SHAPE
     assert call(X=None) == NULL and call(LA=None) == NULL and call(A=None) == NULL and call(plan=None) == NULL
     assert call(ws=None) == WORKSPACE and call(nbytes=8) == WORKSPACE
+
+
+def test_adapters_of_no_rank_need_no_workspace(lib):
+    """Without a rank there is nothing to multiply: the launch that copies serves any number of tokens."""
+    for M in (1, 33, 200, 5000, 1 << 20):
+        assert lib.aser_adapters_workspace_bytes(M, 4096, 4096, 0, 4) == 0
+
+
+class Placed:
+    """What the argument checks see of a tensor that lies on some GPU."""
+
+    def __init__(self, device, shape=(4, 64), dtype=None, stride=None):
+        import torch
+        self.shape, self.dtype, self.device = torch.Size(shape), dtype or torch.float16, device
+        self.strides = stride or (shape[1], 1)
+
+    def get_device(self):
+        return self.device
+
+    def stride(self):
+        return self.strides
+
+
+def test_rows_are_on_the_current_gpu(lib):
+    """(no GPU: the check alone, on what it reads)"""
+    import torch
+    from paper_2411_07762_b200.binding import _rows
+    assert _rows(Placed(1), (4, 64), "X", 1) == 64
+    assert _rows(Placed(1, stride=(80, 1)), (4, 64), "X", 1) == 80
+    assert _rows(Placed(0, shape=(1, 64), stride=(1, 1)), (1, 64), "X", 0) == 64
+    assert _rows(Placed(0, shape=(1, 64), stride=(640, 1)), (1, 64), "X", 0) == 64
+    for bad in (Placed(0), Placed(-1), Placed(1, shape=(4, 72)), Placed(1, dtype=torch.bfloat16), Placed(1, stride=(0, 1)),
+                Placed(1, stride=(32, 1)), Placed(1, stride=(1, 4)), Placed(1, stride=(128, 2))):
+        with pytest.raises(TypeError):
+            _rows(bad, (4, 64), "X", 1)
+
+
+def test_a_plan_and_a_pool_are_on_the_current_gpu(lib):
+    from types import SimpleNamespace
+    from paper_2411_07762_b200.binding import AserAdapters
+    pool = AserAdapters.__new__(AserAdapters)
+    pool.n_slots, pool.device = 3, 1
+    pool._check_plan(SimpleNamespace(M=4, n_slots=3, device=1), 4, 1)
+    for plan, device in ((SimpleNamespace(M=4, n_slots=3, device=0), 1), (SimpleNamespace(M=4, n_slots=3, device=1), 0),
+                         (SimpleNamespace(M=5, n_slots=3, device=1), 1), (SimpleNamespace(M=4, n_slots=2, device=1), 1), (None, 1)):
+        with pytest.raises(ValueError):
+            pool._check_plan(plan, 4, device)
