@@ -8,9 +8,10 @@
 //    and used by all layers of a step, lists the tokens by adapter and cuts each adapter's into tiles of 16 and of 128;
 //  * few tokens per adapter (this file): one launch, a cluster of eight CTAs per tile of 16, which split K for the first
 //    product and N for the second.  What bounds it is the chain of loads, so operands go from global memory straight into
-//    registers (the first rows of B to shared memory, ahead of the first product): an inner product does not care about the order of k, so a thread's k positions are the 8 columns of one
-//    16-byte load, the same for both operands; likewise the 32 rows of B that a warp takes are dealt so that a thread's outputs
-//    are 8 neighbours.  Up to 64 ranks each CTA sends its sums to the others, so that one barrier is all that S waits for;
+//    registers (the first rows of B to shared memory, ahead of the first product): an inner product does not care about the
+//    order of k, so a thread's k positions are the 8 columns of one 16-byte load, the same for both operands; likewise the 32 rows of B that a warp takes are dealt so that a thread's outputs
+//    are 8 neighbours.  Up to 64 ranks each CTA sends its sums to the others, so that one barrier is all that S waits for.  One
+//    token, 4096 x 4096, rank 16: 4.5 us; 64 tokens of 32 adapters, ranks to 64: 11.4 (bytes: 3.3);
 //  * many tokens per adapter: two launches (adapters_many.cu).
 // S is summed and exchanged in fp32, in a fixed order; nothing depends on the order of tokens in a tile.  For the second product it
 // is rounded to fp16 (2^-11 of each number, where the output has 2^-11 of the whole sum) after a scaling by a power of two that

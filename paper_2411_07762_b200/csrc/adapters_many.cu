@@ -10,8 +10,9 @@
 //                  it lies in shared memory, a token to a thread, and write whole 128-byte lines from there.
 //
 // A tile's tokens lie anywhere in the batch.  Where they follow one another (a prompt), copies take 32 rows at a time, else four
-// rows by number (tile::gather4).  Before, threads fetched the rows 16 bytes at a time: 15 cycles an instruction and
-// SM, which bound both kernels (4096 tokens of 6 adapters, rank 64, 4096 x 4096: 47 us).
+// rows by number (tile::gather4).  Threads that fetched the rows 16 bytes at a time took 15 cycles an instruction and SM, which
+// bound both kernels (4096 tokens of 6 adapters, ranks to 64, 4096 x 4096: 47 us, now 32.9, where the bytes take 16.2; 2048 tokens of
+// 5, ranks to 128, 14336 -> 4096: 46.6, bytes 14.9; 501 tokens of 8, ranks to 32, 4096 -> 28672: 27.6, bytes 11.3).
 //
 // Every wait is bounded; a warp that gives up leaves NaN in what it would have written.
 #include "adapters.cuh"
