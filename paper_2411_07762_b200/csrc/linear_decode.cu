@@ -34,6 +34,7 @@
 //     they overlap the activation kernel; Xq, a_scale and T are read after it.
 #include "aser_common.cuh"
 #include "glu_math.cuh"
+#include "sm100_ptx.cuh"
 
 namespace aser {
 
@@ -41,6 +42,9 @@ namespace {
 
 constexpr int kDecWarps = 8;
 constexpr int kDecThreads = kDecWarps * 32;
+// A CTA of a cluster that splits K, and how many an SM holds.  The sums have the order of one CTA of eight warps: integers, and the
+// low-rank term's slices w and w + 8 by warp w of the cluster's first eight.
+constexpr int kSplitThreads = 128, kSplitCtas = 7;
 
 // A row's 32 columns of a thread: 8 bytes of a block's first half (words 2 (t & 1) and + 1 of sub-block t / 2) and 8 of its second.
 __device__ __forceinline__ uint4 ld_stream16(const uint8_t* p) {
@@ -48,6 +52,9 @@ __device__ __forceinline__ uint4 ld_stream16(const uint8_t* p) {
     asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
     asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(v.z), "=r"(v.w) : "l"(p + 2 * kWkRows * 16));
     return v;
+}
+__device__ __forceinline__ void st_cluster_u32(uint32_t addr, uint32_t v) {
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
 }
 __device__ __forceinline__ void dep_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
@@ -92,16 +99,22 @@ struct DecCfg {
 
 // GLU: the channels are gate and up in turn, a lane of an even channel stores the product with its neighbour's (no dump).
 // STREAM: more tiles than CTAs are resident; a CTA takes every gridDim.x-th tile, and its weights keep coming from one tile to the next.
-template <int NT, int R, int B, bool GROUP, bool GLU, bool STREAM>
-__global__ void __launch_bounds__(kDecThreads, DecCfg<NT, R, B>::MinCtas)
+// CL > 1: a cluster of CTAs of four warps shares a tile's K.  Its first CTA gets the others' sums and finishes the tile.
+template <int NT, int R, int B, bool GROUP, bool GLU, bool STREAM, int CL = 1>
+__global__ void __launch_bounds__(CL > 1 ? kSplitThreads : kDecThreads, CL > 1 ? kSplitCtas : DecCfg<NT, R, B>::MinCtas)
 linear_decode_kernel(const int8_t* Xq, const float* a_scale, const __nv_bfloat16* T, int M, int K, int ldt,
                      int32_t* __restrict__ acc_debug, const CatSplit cat, const __grid_constant__ LinearGroup group, const GluForm glu, int tiles) {
     using C = DecCfg<NT, R, B>;
-    constexpr int BATCH = C::Batch;
-    // partial sums of the eight warps: integer accumulators and fp32 accumulators of the low-rank term
-    __shared__ int red[kDecWarps][C::Regs][32];
+    static_assert(CL == 1 || !STREAM, "a cluster has one tile");
+    constexpr int BATCH = C::Batch, kThreads = CL > 1 ? kSplitThreads : kDecThreads, kWarps = kThreads / 32, kAll = kWarps * CL;
+    constexpr int kOutPerThread = (C::Rows * 8 * NT + kThreads - 1) / kThreads;
+    // partial sums of the warps: integer accumulators and fp32 accumulators of the low-rank term
+    __shared__ int red[kWarps][C::Regs][32];
     __shared__ float red_lr[kDecWarps][C::Regs][32];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    __shared__ int part[CL][kOutPerThread][CL > 1 ? kThreads : 1];      // the CTAs' sums, in the first CTA
+    const int rank = CL > 1 ? (int)cluster_rank() : 0, first_tile = (int)blockIdx.x / CL;
+    const int lane = threadIdx.x & 31, local = threadIdx.x >> 5, warp = rank * kWarps + local;
+    if (CL > 1) cluster_arrive_relaxed();        // (waited for before anything is sent)
     const int g = lane >> 2, t = lane & 3;       // fragment row group / k quarter
     const int KB = K / kWkCols;
     // A tile's layer of the group and its rows there (layers that share their input are one launch: a launch has its start-up
@@ -123,13 +136,13 @@ linear_decode_kernel(const int8_t* Xq, const float* a_scale, const __nv_bfloat16
         return group.Wk[layer] + ((size_t)(n0 >> 7) * KB) * kWkBlockBytes + (t >> 1) * (kWkRows * 16) + ((n0 & 127) + g) * 16 + (t & 1) * 8;
     };
     int layer, n0;
-    find((int)blockIdx.x, layer, n0);
+    find(first_tile, layer, n0);
     const uint8_t* wbase = weights(layer, n0);
 
     uint4 wa[BATCH][R][2];
 #pragma unroll
     for (int i = 0; i < BATCH; ++i) {
-        const int kbi = warp + i * kDecWarps;
+        const int kbi = warp + i * kAll;
         if (kbi < KB) {
 #pragma unroll
             for (int rt = 0; rt < R; ++rt) {
@@ -138,7 +151,7 @@ linear_decode_kernel(const int8_t* Xq, const float* a_scale, const __nv_bfloat16
             }
         }
     }
-    for (int tile = (int)blockIdx.x;;) {
+    for (int tile = first_tile;;) {
     const float* __restrict__ w_scale = group.w_scale[layer];
     const __half* __restrict__ LB = group.LB[layer];
     __half* __restrict__ Y = group.Y[layer];
@@ -161,17 +174,18 @@ linear_decode_kernel(const int8_t* Xq, const float* a_scale, const __nv_bfloat16
         for (int rt = 0; rt < R; ++rt) {
             const int row0 = n0 + rt * 16 + g;
             la[u][rt][0] = la[u][rt][1] = make_uint2(0, 0);
-            if (k0 < r) {
+            if (k0 < r && warp < kDecWarps) {
                 if (row0 < N) la[u][rt][0] = __ldg(reinterpret_cast<const uint2*>(LB + (size_t)row0 * r + k0));
                 if (row0 + 8 < N) la[u][rt][1] = __ldg(reinterpret_cast<const uint2*>(LB + (size_t)(row0 + 8) * r + k0));
             }
         }
     }
-    if (!STREAM || tile == (int)blockIdx.x) dep_wait();
+    if (!STREAM || tile == first_tile) dep_wait();
 
     // ---- low-rank term, while the weight loads are in flight: warp w takes the 16-wide slices
     // w and w + 8 of r; a thread's k positions inside a slice are 4 t .. 4 t + 3 ----
     const int lr_warps = (r / 16 < kDecWarps) ? r / 16 : kDecWarps;
+    if (CL > 1) cluster_wait();
     if (warp < lr_warps) {
         uint2 tv[2][NT];
 #pragma unroll
@@ -200,7 +214,11 @@ linear_decode_kernel(const int8_t* Xq, const float* a_scale, const __nv_bfloat16
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) red_lr[warp][(rt * NT + nt) * 4 + e][lane] = cf[nt][e];
+                for (int e = 0; e < 4; ++e) {
+                    float* to = &red_lr[warp][(rt * NT + nt) * 4 + e][lane];
+                    if (CL > 1 && rank > 0) st_cluster_u32(map_to_rank(smem_u32(to), 0), __float_as_uint(cf[nt][e]));
+                    else *to = cf[nt][e];
+                }
         }
     }
 
@@ -220,10 +238,10 @@ linear_decode_kernel(const int8_t* Xq, const float* a_scale, const __nv_bfloat16
         x_ok[nt] = g + 8 * nt < M;
         xrow[nt] = Xq + (size_t)(x_ok[nt] ? g + 8 * nt : 0) * K + t * 16;
     }
-    for (int kb0 = warp; kb0 < KB; kb0 += kDecWarps * BATCH) {
+    for (int kb0 = warp; kb0 < KB; kb0 += kAll * BATCH) {
 #pragma unroll
         for (int i = 0; i < BATCH; ++i) {
-            const int kbi = kb0 + i * kDecWarps;
+            const int kbi = kb0 + i * kAll;
             if (kbi < KB) {
                 uint32_t b[NT][8];
 #pragma unroll
@@ -237,7 +255,7 @@ linear_decode_kernel(const int8_t* Xq, const float* a_scale, const __nv_bfloat16
                     b[nt][0] = lo.x; b[nt][1] = lo.y; b[nt][2] = lo.z; b[nt][3] = lo.w;
                     b[nt][4] = hi.x; b[nt][5] = hi.y; b[nt][6] = hi.z; b[nt][7] = hi.w;
                 }
-                const int kbn = kbi + kDecWarps * BATCH;
+                const int kbn = kbi + kAll * BATCH;
 #pragma unroll
                 for (int rt = 0; rt < R; ++rt) {
                     const uint32_t w0[4] = {wa[i][rt][0].x, wa[i][rt][0].y, wa[i][rt][0].z, wa[i][rt][0].w};
@@ -255,8 +273,8 @@ linear_decode_kernel(const int8_t* Xq, const float* a_scale, const __nv_bfloat16
                         wa[i][rt][0] = ld_stream16(wbase + (size_t)kbn * kWkBlockBytes + rt * 256);
                         wa[i][rt][1] = ld_stream16(wbase + (size_t)kbn * kWkBlockBytes + rt * 256 + 128);
                     } else if (STREAM && wnext) {
-                        wa[i][rt][0] = ld_stream16(wnext + (size_t)(warp + i * kDecWarps) * kWkBlockBytes + rt * 256);
-                        wa[i][rt][1] = ld_stream16(wnext + (size_t)(warp + i * kDecWarps) * kWkBlockBytes + rt * 256 + 128);
+                        wa[i][rt][0] = ld_stream16(wnext + (size_t)(warp + i * kAll) * kWkBlockBytes + rt * 256);
+                        wa[i][rt][1] = ld_stream16(wnext + (size_t)(warp + i * kAll) * kWkBlockBytes + rt * 256 + 128);
                     }
                 }
             }
@@ -265,35 +283,44 @@ linear_decode_kernel(const int8_t* Xq, const float* a_scale, const __nv_bfloat16
 
     // Output element (channel row, token column) of tile rt sits in accumulator register
     // (row % 16 / 8) * 2 + column % 2 of lane (row % 8) * 4 + (column % 8) / 2, token group
-    // column / 8.  A thread finishes the elements idx = tid, tid + 256, ...; idx % (16 R) is the
+    // column / 8.  A thread finishes the elements idx = tid, tid + threads, ...; idx % (16 R) is the
     // channel, so consecutive threads store consecutive channels.
-    constexpr int kOutPerThread = (C::Rows * 8 * NT + kDecThreads - 1) / kDecThreads;
     int sums[kOutPerThread];
 #pragma unroll
     for (int rt = 0; rt < R; ++rt)
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) red[warp][(rt * NT + nt) * 4 + e][lane] = c[rt][nt][e];
+            for (int e = 0; e < 4; ++e) red[local][(rt * NT + nt) * 4 + e][lane] = c[rt][nt][e];
     __syncthreads();
 #pragma unroll
     for (int o = 0; o < kOutPerThread; ++o) {
-        const int idx = threadIdx.x + o * kDecThreads;
+        const int idx = threadIdx.x + o * kThreads;
         const int row = idx % C::Rows, om = idx / C::Rows, col = om & 7;
         const int reg = ((row >> 4) * NT + (om >> 3)) * 4 + ((row >> 3) & 1) * 2 + (col & 1);
         const int ln = (row & 7) * 4 + (col >> 1);
         int sum = 0;
         if (om < 8 * NT) {
 #pragma unroll
-            for (int w = 0; w < kDecWarps; ++w) sum += red[w][reg][ln];
+            for (int w = 0; w < kWarps; ++w) sum += red[w][reg][ln];
         }
         sums[o] = sum;
+        if (CL > 1 && rank > 0) st_cluster_u32(map_to_rank(smem_u32(&part[rank][o][threadIdx.x]), 0), (uint32_t)sum);
+    }
+    if (CL > 1) {
+        cluster_arrive();
+        cluster_wait();
+        if (rank > 0) return;
+#pragma unroll
+        for (int o = 0; o < kOutPerThread; ++o)
+#pragma unroll
+            for (int q = 1; q < CL; ++q) sums[o] += part[q][o][threadIdx.x];
     }
 
     // ---- scale, add, store ----
 #pragma unroll
     for (int o = 0; o < kOutPerThread; ++o) {
-        const int idx = threadIdx.x + o * kDecThreads;
+        const int idx = threadIdx.x + o * kThreads;
         const int row = idx % C::Rows, om = idx / C::Rows, col = om & 7;
         const int on = n0 + row;
         if (GLU) {
@@ -361,6 +388,25 @@ int launch_cfg(const int8_t* Xq, const float* a_scale, const __nv_bfloat16* T, i
     return check_launch("linear_decode_kernel");
 }
 
+template <int NT, int B, int CL, bool GLU>
+int launch_split_k(const int8_t* Xq, const float* a_scale, const __nv_bfloat16* T, int M, int K, int32_t* acc_debug, int tiles,
+                   cudaStream_t st, bool overlap_prev, int ldt, const CatSplit& cat, const LinearGroup& group, const GluForm& glu) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(tiles * CL, 1, 1);
+    cfg.blockDim = dim3(kSplitThreads, 1, 1);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = CL; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = overlap_prev ? 2 : 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, linear_decode_kernel<NT, 1, B, true, GLU, false, CL>, Xq, a_scale, T, M, K, ldt, acc_debug, cat, group, glu, tiles);
+    if (e != cudaSuccess) return record_cuda_error(e, "linear_decode_kernel");
+    return check_launch("linear_decode_kernel");
+}
+
 template <int NT, bool GLU>
 int launch_nt(const int8_t* Xq, const float* a_scale, const __nv_bfloat16* T, int M, int K, int32_t* acc_debug,
               cudaStream_t st, bool overlap_prev, int ldt, const CatSplit& cat, const LinearGroup& group, const GluForm& glu) {
@@ -378,8 +424,22 @@ int launch_nt(const int8_t* Xq, const float* a_scale, const __nv_bfloat16* T, in
     // too many for three CTAs per SM, four with half the bytes in flight each take them in one wave (kernel alone, one /
     // eight tokens: 14336 x 4096, 448 tiles for 444 places, 11.5 / 11.5 -> 7.6 / 8.9 us; 16384 x 1024, 512 tiles, 6.5 / 6.3 -> 4.5 /
     // 4.8).
-    int tiles = 0, rows = 0;
-    for (int l = 0; l < group.layers; ++l) { tiles += (group.N[l] + 31) / 32; rows += group.N[l]; }
+    int tiles = 0, rows = 0, tiles16 = 0;
+    for (int l = 0; l < group.layers; ++l) { tiles += (group.N[l] + 31) / 32; rows += group.N[l]; tiles16 += (group.N[l] + 15) / 16; }
+    // K split over a cluster of small CTAs (seven to an SM) where 16-row tiles of whole rows would leave SMs unevenly filled, and a
+    // warp's blocks follow one another for long.  Two CTAs to a tile where that is one wave and the choice without is 32 rows (one /
+    // sixteen tokens, us: 8192 x 8192 9.5 / 13.1 -> 8.5 / 11.6, 8192 x 14336 14.4 / 20.1 -> 12.4 / 16.7, 8192 x 4096 6.3 / 8.4 -> 5.8 / 8.4; with
+    // 16-row tiles it loses, 6144 x 8192 7.4 / 10.0 -> 7.9 / 10.3).  Three and four for long rows, while a tenth of the places stays
+    // free (clusters wait for places side by side, 329 of three and 246 of four in an empty GPU: 256 tiles by four 11.7 us, 320 by
+    // three behind an activation kernel 13.3 -> 17.6): 4096 x 14336 9.9 / 13.2 -> 8.9 / 11.9 (by three), 2048 x 14336 9.3 / 12.9 -> 6.7 / 8.6,
+    // 1024 x 8192 5.8 / 8.0 -> 4.5 / 5.9 (by four); 4096 x 8192 by three 6.8 / 8.8 -> 6.5 / 8.8, 1024 x 4096 by four 3.7 / 4.6 -> 3.7 / 4.3.
+    const int places = kSplitCtas * num_sms;
+    if (K >= 4096 && rows >= 32 * 3 * num_sms / 2 && tiles16 * 2 <= places)
+        return launch_split_k<NT, 2, 2, GLU>(Xq, a_scale, T, M, K, acc_debug, tiles16, st, overlap_prev, ldt, cat, group, glu);
+    if (K >= 8192 && tiles16 * 4 <= places * 9 / 10)
+        return launch_split_k<NT, NT == 1 ? 4 : 2, 4, GLU>(Xq, a_scale, T, M, K, acc_debug, tiles16, st, overlap_prev, ldt, cat, group, glu);
+    if (K >= 10240 && tiles16 * 3 <= places * 9 / 10)
+        return launch_split_k<NT, NT == 1 ? 4 : 2, 3, GLU>(Xq, a_scale, T, M, K, acc_debug, tiles16, st, overlap_prev, ldt, cat, group, glu);
     if ((tiles + 4 * num_sms - 1) / (4 * num_sms) < (tiles + 3 * num_sms - 1) / (3 * num_sms))
         return launch_cfg<NT, 2, 1, GLU>(Xq, a_scale, T, M, K, acc_debug, num_sms, st, overlap_prev, ldt, cat, group, glu);
     if (rows >= 32 * 3 * num_sms / 2)

@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from test_gpu_adapters import assert_close, expected, make
-from test_gpu_ffn import assert_product_close, Steps
+from test_gpu_ffn import assert_product_close, dequantized, Steps
 
 pytestmark = pytest.mark.gpu
 
@@ -111,5 +111,64 @@ def test_groups_of_more_tiles_than_the_gpu_holds(aser, M, N, K, r):
     X = normal(g, M, K)
     group = aser.AserSharedInput(layers, M)
     out = [y.clone() for y in group(X)]
+    for layer, y in zip(layers, out):
+        assert torch.equal(layer(X), y)
+
+
+# few tokens by clusters along K: two, three and four CTAs to 16 channels, whole and ragged, with every share of a low-rank term
+SPLIT = [(8192, 4096, 64), (7176, 8192, 0), (8200, 4224, 256), (7168, 6144, 16), (4096, 14336, 64), (4616, 10240, 128), (4000, 11008, 0), (1024, 8192, 192),
+         (8, 8192, 16), (2048, 14336, 256), (3720, 8320, 48), (40, 16384, 112)]
+
+
+@pytest.mark.parametrize("M", [1, 3, 8, 9, 16])
+@pytest.mark.parametrize("N,K,r", SPLIT)
+def test_long_rows_of_few_tokens(aser, M, N, K, r):
+    """Integer sums are exact.  Y = fp16(sum a_scale w_scale + T L_B^T) in fp32: r / 16 slices of 16 exact products, each addition
+    off by at most 2^-22 of the sum of magnitudes (r / 16 + 16 of them), the scale's two products, the conversion of the sum
+    and the last addition by 2^-22 together, and the store by 2^-11 or 2^-25."""
+    g = gen(M + N + K)
+    layer = aser.AserLinear(normal(g, N, K, scale=0.03), None, normal(g, r, K, scale=0.02) if r else None,
+                            normal(g, N, r, scale=0.05) if r else None, M)
+    assert aser.lib.aser_linear_kernel(M, N, K) == 0
+    layer.quant(normal(g, M, K))
+    acc = torch.zeros(M, N, device="cuda", dtype=torch.int32)
+    layer.Y.fill_(7.0)
+    layer.linear(M, acc_debug=acc)
+    w = dequantized(layer) / layer.w_scale.double()[:, None].clamp_min(1e-30)
+    want = layer.Xq.double() @ w.round().T
+    assert torch.equal(acc.double(), want)
+    ref = want * layer.a_scale.double()[:, None] * layer.w_scale.double()
+    bound = 2.0 ** -22 * ref.abs()
+    if r:
+        T, LB = layer.T[:, :r].double(), layer.L_B.double()
+        ref = ref + T @ LB.T
+        bound = bound + (r / 16 + 16) * 2.0 ** -22 * (T.abs() @ LB.abs().T) + 2.0 ** -22 * ref.abs()
+    bound = bound + 2.0 ** -11 * (ref.abs() + bound) + 2.0 ** -25
+    assert ((layer.Y.double() - ref).abs() <= bound).all()
+    again = layer.Y.clone()
+    layer.linear(M)
+    assert torch.equal(layer.Y, again)
+
+
+@pytest.mark.parametrize("M", [2, 16])
+@pytest.mark.parametrize("F,K,r,act", [(4096, 4096, 64, "silu"), (512, 8192, 32, "gelu_tanh"), (2048, 14336, 0, "silu"), (1800, 8192, 128, "silu")])
+def test_product_of_long_rows(aser, M, F, K, r, act):
+    g = gen(M + F)
+    layer = aser.AserLinear(normal(g, 2 * F, K, scale=2.0 / math.sqrt(K)), None, normal(g, r, K, scale=0.02) if r else None,
+                            normal(g, 2 * F, r, scale=0.05) if r else None, M)
+    layer.quant(normal(g, M, K))
+    layer.linear(M)
+    H = aser.linear_w4a8_lr_glu(layer.Xq, layer.a_scale, layer.Wk, layer.w_scale, layer.T, layer.L_B, 2 * F, layer.ws, act)
+    assert_product_close(H, layer.Y[:, 0::2], layer.Y[:, 1::2], act)
+
+
+@pytest.mark.parametrize("M", [1, 16])
+def test_a_group_of_long_rows(aser, M):
+    g = gen(M)
+    s = divisors(g, 8192)
+    layers = [aser.AserLinear(normal(g, n, 8192, scale=0.05), s, normal(g, rr, 8192, scale=0.02), normal(g, n, rr, scale=0.05), M)
+              for n, rr in ((1032, 32), (512, 16), (640, 128))]
+    X = normal(g, M, 8192)
+    out = [y.clone() for y in aser.AserSharedInput(layers, M)(X)]
     for layer, y in zip(layers, out):
         assert torch.equal(layer(X), y)
