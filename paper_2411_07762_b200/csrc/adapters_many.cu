@@ -11,8 +11,8 @@
 //
 // A tile's tokens lie anywhere in the batch.  Where they follow one another (a prompt), copies take 32 rows at a time, else four
 // rows by number (tile::gather4).  Threads that fetched the rows 16 bytes at a time took 15 cycles an instruction and SM, which
-// bound both kernels (4096 tokens of 6 adapters, ranks to 64, 4096 x 4096: 47 us, now 32.9, where the bytes take 16.2; 2048 tokens of
-// 5, ranks to 128, 14336 -> 4096: 46.6, bytes 14.9; 501 tokens of 8, ranks to 32, 4096 -> 28672: 27.6, bytes 11.3).
+// bound both kernels (4096 tokens of 6 adapters, ranks to 64, 4096 x 4096: 47 us, now 31.2, where the bytes take 16.2; 2048 tokens of
+// 5, ranks to 128, 14336 -> 4096: 43.9, bytes 14.9; 501 tokens of 8, ranks to 32, 4096 -> 28672: 27.6, bytes 11.3).
 //
 // Every wait is bounded; a warp that gives up leaves NaN in what it would have written.
 #include "adapters.cuh"
@@ -22,7 +22,7 @@ namespace aser {
 
 namespace {
 
-constexpr int kTok = kTileMany, kMaxCL = 8, kBox = 32;
+constexpr int kTok = kTileMany, kMaxCL = 12, kGather = 8, kBox = 32;
 constexpr int kCols = 64;                            // columns or channels of a stage: 128 bytes a row
 constexpr int kRowsBytes = kTok * kCols * 2;
 constexpr int kMaxStages = 8;
@@ -98,7 +98,7 @@ __device__ __forceinline__ void tmem_free(uint32_t tmem, uint32_t cols) {
 // ---------------------------------------------------------------------------
 constexpr int kDownThreads = 256, kDownWarps = 8;
 
-struct DownMaps { CUtensorMap x, x_one, a; };
+struct DownMaps { CUtensorMap x, x_one, a, a_big; };
 
 // The ring also holds the partial sums at the end, [128][rank + 4] floats.  Up to rank 128 two CTAs fit on an SM, so that clusters
 // beyond those that have SMs of their own need not wait for a second turn (CTAs with an SM's shared memory each, 36 clusters of four
@@ -162,7 +162,12 @@ adapters_down_kernel(const __grid_constant__ DownMaps maps, const AdapterParams 
                 const uint32_t at = sb + (uint32_t)(s * stage_bytes);
                 const int col = (s0 + i) * kCols;
                 rows.load(at, &maps.x, &maps.x_one, col, filled(s), lane);
-                if (lane * 16 < rk) tma_load_2d(at + row_bytes + lane * 2048, &maps.a, col, slot * p.r + lane * 16, filled(s));
+                // A in boxes of 64 ranks, then of 16 (600 x 14336 x 4096, rank 256: 35.3 -> 30.0 us; of 16 alone, a stage is that many more copies)
+                const int big = rk >> 6;
+                if (lane < big + ((rk >> 4) & 3)) {
+                    const int j = lane < big ? lane * 64 : big * 64 + (lane - big) * 16;
+                    tma_load_2d(at + row_bytes + j * 128, lane < big ? &maps.a_big : &maps.a, col, slot * p.r + j, filled(s));
+                }
                 if (++s == stages) { s = 0; ++turn; }
             }
         } else if (warp == 1) {       // products (rows that are not there are whatever the ring holds: nobody reads their sums)
@@ -212,27 +217,31 @@ adapters_down_kernel(const __grid_constant__ DownMaps maps, const AdapterParams 
         const float alpha = p.scale ? __ldg(p.scale + slot) : 1.f;
         auto gather = [&](int row, int j) {
             const uint32_t at = smem_u32(part + row * stride + j);
-            float4 a[kMaxCL], v = make_float4(0.f, 0.f, 0.f, 0.f);
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int q0 = 0; q0 < CL; q0 += kGather) {
+                float4 a[kGather];
 #pragma unroll
-            for (int q = 0; q < kMaxCL; ++q) a[q] = q < CL ? ld_cluster_f32x4(map_to_rank(at, q)) : v;
+                for (int q = 0; q < kGather; ++q) a[q] = q0 + q < CL ? ld_cluster_f32x4(map_to_rank(at, q0 + q)) : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-            for (int q = 0; q < kMaxCL; ++q) { v.x += a[q].x; v.y += a[q].y; v.z += a[q].z; v.w += a[q].w; }
+                for (int q = 0; q < kGather; ++q) { v.x += a[q].x; v.y += a[q].y; v.z += a[q].z; v.w += a[q].w; }
+            }
             return v;
         };
         auto gather2 = [&](int row, int step, int j, const bool (&mine)[2], float4 (&v)[2]) {
-            float4 a[2][kMaxCL];
+            v[0] = v[1] = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int q0 = 0; q0 < CL; q0 += kGather) {
+                float4 a[2][kGather];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const uint32_t at = smem_u32(part + (mine[u] ? row + u * step : 0) * stride + j);
+                for (int u = 0; u < 2; ++u) {
+                    const uint32_t at = smem_u32(part + (mine[u] ? row + u * step : 0) * stride + j);
 #pragma unroll
-                for (int q = 0; q < kMaxCL; ++q)
-                    a[u][q] = q < CL && mine[u] ? ld_cluster_f32x4(map_to_rank(at, q)) : make_float4(0.f, 0.f, 0.f, 0.f);
-            }
+                    for (int q = 0; q < kGather; ++q)
+                        a[u][q] = q0 + q < CL && mine[u] ? ld_cluster_f32x4(map_to_rank(at, q0 + q)) : make_float4(0.f, 0.f, 0.f, 0.f);
+                }
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int q = 0; q < kMaxCL; ++q) { v[u].x += a[u][q].x; v[u].y += a[u][q].y; v[u].z += a[u][q].z; v[u].w += a[u][q].w; }
+                    for (int q = 0; q < kGather; ++q) { v[u].x += a[u][q].x; v[u].y += a[u][q].y; v[u].z += a[u][q].z; v[u].w += a[u][q].w; }
             }
         };
         if (rk <= 64) {                   // two tokens side by side, twice
@@ -521,7 +530,8 @@ int opt_in(Kernel* kernel, int bytes, bool (&configured)[kMaxDevices], int* num_
     int rc = current_device(&dev);
     if (rc == ASER_OK) rc = device_sm_count(num_sms);
     if (rc != ASER_OK || configured[dev]) return rc;
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e != cudaSuccess) return record_cuda_error(e, "adapters smem attribute");
     configured[dev] = true;
     return ASER_OK;
@@ -537,11 +547,16 @@ int launch_adapters_down(const AdapterParams& p, cudaStream_t st) {
     DownMaps maps;
     rc = rows_map(&maps.x, p.X, p.M, p.K, p.ldx, kBox);
     if (rc == ASER_OK) rc = rows_map(&maps.x_one, p.X, p.M, p.K, p.ldx, 1);
+    if (rc == ASER_OK) rc = rows_map(&maps.a_big, p.A, (uint64_t)p.n_slots * p.r, p.K, p.K, 64);
     if (rc == ASER_OK) rc = rows_map(&maps.a, p.A, (uint64_t)p.n_slots * p.r, p.K, p.K, 16);
     if (rc != ASER_OK) return rc;
-    // about as many CTAs as there are SMs; each has two steps of K at least
-    int CL = (num_sms + num_sms / 10) / likely_tiles(p);
-    CL = CL > kMaxCL ? kMaxCL : CL;
+    // CTAs for one and a half times the SMs that there are (two share one up to rank 128, and what bounds a CTA is the bytes that it
+    // has in flight; more, and the last clusters of a few hundred wait for places: 4096 tokens of 6, 4096 x 4096, rank 64, 1.1 times 32.9
+    // us, 1.5 30.9, 2 37.6), from 2 steps of K each; clusters above eight for long K only (2048 x 14336 x 4096, rank 128: by 8 45.4, by 12 43.6;
+    // 1500 x 8192 x 1024, rank 64, 34.6 / 29.3; 1024 x 4096 x 4096 17.4 / 18.2).
+    int CL = (p.r <= 128 ? num_sms * 3 / 2 : num_sms * 11 / 10) / likely_tiles(p);
+    const int most = p.K >= 7680 ? kMaxCL : 8;
+    CL = CL > most ? most : CL;
     CL = CL > p.K / kCols / 2 ? p.K / kCols / 2 : CL;
     CL = CL < 1 ? 1 : CL;
     uint32_t cols = 32;

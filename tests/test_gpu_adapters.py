@@ -109,7 +109,8 @@ def test_update(aser, M, K, N, r, slots, bare, spread):
 
 # prompts: runs of tokens that follow one another, of lengths around the tiles' and the copies' sizes, with adapters of many ranks
 RUNS = [(200, 14336, 72, 64, (128, 72)), (300, 128, 16384, 32, (255, 45)), (1021, 1024, 136, 128, (127, 1, 129, 33, 500, 31, 200)), (640, 4096, 512, 256, (320, 320)),
-        (900, 256, 4104, 16, (32, 96, 64, 700, 8)), (1500, 14336, 200, 96, (1, 2, 3, 1494)), (2500, 512, 1032, 48, (1250, 1250))]
+        (900, 256, 4104, 16, (32, 96, 64, 700, 8)), (1500, 14336, 200, 96, (1, 2, 3, 1494)), (2500, 512, 1032, 48, (1250, 1250)), (600, 14336, 264, 256, (333, 267)),
+        (390, 7680, 520, 144, (129, 128, 133))]
 
 
 @pytest.mark.parametrize("mixed", [False, True])
