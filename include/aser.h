@@ -79,8 +79,8 @@ int aser_unrepack_w4(const void* Wk, int N, int K, uint8_t* Wq, void* stream);
  *   x~ = fp32(X[m,k]) / s[k]                       (fp32 division; s == NULL means ones)
  *   a_scale[m] = max_k |x~| / 127                  (fp32 division; zero row -> 0, codes 0)
  *   Xq[m,k] = clamp(rne(x~ / a_scale[m]), -127, 127)
- *   T[m,j]  = bf16( sum_k L_A[j,k] * x~[m,k] )     (fp32 accumulation; x~ may be rounded to
- *                                                   fp16 first when tensor cores are used)
+ *   T[m,j]  = bf16( sum_k L_A[j,k] * x~[m,k] )     (fp32 accumulation; from a few hundred tokens
+ *                                                   on x~ may be rounded to fp16 first)
  * Xq and a_scale are bit-exact with the definition.  r == 0: LA_f16 and T_bf16 are ignored.
  */
 int aser_quant_act(const void* X_f16, const float* s, const void* LA_f16,

@@ -8,7 +8,8 @@
 //  * a projecting cluster takes 32 tokens x 32 rows of L_A, its CTAs' warps 64 columns of K at a time.  mma.sync m16n8k16:
 //    an inner product does not care about the order of k, so a thread's k positions are the 8 columns that one 16-byte
 //    load brings, the same for X and L_A, and neither goes through shared memory.  X is divided where the divisor is
-//    not 1 (fp32, then fp16, as in the other kernels).  The warps' sums meet in shared memory, the CTAs' in distributed
+//    not 1 (fp32), and the quotient multiplied as the sum of two fp16 numbers: rounded to one, 2 % of T's bf16 values came out a
+//    step off, and in a feed-forward block a step of T moves codes of H (a few tokens' outputs by 2 %).  The warps' sums meet in shared memory, the CTAs' in distributed
 //    shared memory, both in a fixed order; the order depends on K alone, not on the number of tokens.
 #include "act_math.cuh"
 #include "aser_common.cuh"
@@ -61,15 +62,13 @@ quant_act_mid_kernel(const __half* __restrict__ X, const float* __restrict__ s, 
         for (int nt = 0; nt < 4; ++nt)
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[mt][nt][e] = 0.f;
-    const __half* xp[4];
-    const __half* lp[4];
+    const __half* const xp = X + (size_t)(m0 + g) * K + t * 8;
+    const __half* const lp = LA + (size_t)(j0 + g) * K + t * 8;
     bool x_ok[4], l_ok[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {           // token rows g + 8 i, L_A rows g + 8 i
         x_ok[i] = m0 + g + 8 * i < M;
         l_ok[i] = j0 + g + 8 * i < r;
-        xp[i] = X + (size_t)(x_ok[i] ? m0 + g + 8 * i : 0) * K + t * 8;
-        lp[i] = LA + (size_t)(l_ok[i] ? j0 + g + 8 * i : 0) * K + t * 8;
     }
     for (int u = warp < kMWarps ? rank * kMWarps + warp : K; u < K / 64; u += CL * kMWarps) {
         uint4 xv[2][4], lv[2][4];
@@ -79,8 +78,8 @@ quant_act_mid_kernel(const __half* __restrict__ X, const float* __restrict__ s, 
             const int c = u * 64 + h * 32;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                xv[h][i] = x_ok[i] ? *reinterpret_cast<const uint4*>(xp[i] + c) : make_uint4(0, 0, 0, 0);
-                lv[h][i] = l_ok[i] ? __ldg(reinterpret_cast<const uint4*>(lp[i] + c)) : make_uint4(0, 0, 0, 0);
+                xv[h][i] = x_ok[i] ? *reinterpret_cast<const uint4*>(xp + 8 * i * K + c) : make_uint4(0, 0, 0, 0);
+                lv[h][i] = l_ok[i] ? __ldg(reinterpret_cast<const uint4*>(lp + 8 * i * K + c)) : make_uint4(0, 0, 0, 0);
             }
             s0[h] = s1[h] = make_float4(1.f, 1.f, 1.f, 1.f);
             if (s) {
@@ -94,19 +93,32 @@ quant_act_mid_kernel(const __half* __restrict__ X, const float* __restrict__ s, 
             uint32_t xw[4][4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) { xw[i][0] = xv[h][i].x; xw[i][1] = xv[h][i].y; xw[i][2] = xv[h][i].z; xw[i][3] = xv[h][i].w; }
-            bool ones = true;
+            unsigned tags = 0;               // columns where a lane has a divisor
 #pragma unroll
-            for (int e = 0; e < 8; ++e) ones = ones && sv[e] == 1.f;
-            if (!ones) {
+            for (int e = 0; e < 8; ++e) tags |= sv[e] != 1.f ? 1u << e : 0u;
+            tags = __reduce_or_sync(0xffffffffu, tags);
+            if (tags) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    if (sv[e] == 1.f) continue;
+                    if (!(tags >> e & 1)) continue;
+                    uint32_t lo[4];          // what fp16 leaves of the quotients, multiplied at once: in the place of its word, zeros beside it
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const uint32_t word = xw[i][e >> 1];
                         const __half hv = __ushort_as_half((unsigned short)((e & 1) ? (word >> 16) : (word & 0xffffu)));
-                        const uint32_t hb = (uint32_t)__half_as_ushort(__float2half_rn(__fdiv_rn(__half2float(hv), sv[e])));
+                        const float q = __fdiv_rn(__half2float(hv), sv[e]);
+                        const __half hi = __float2half_rn(fminf(fmaxf(q, -65504.f), 65504.f));
+                        const uint32_t hb = (uint32_t)__half_as_ushort(hi), lb = (uint32_t)__half_as_ushort(__float2half_rn(q - __half2float(hi)));
                         xw[i][e >> 1] = (e & 1) ? ((word & 0x0000ffffu) | (hb << 16)) : ((word & 0xffff0000u) | hb);
+                        lo[i] = (e & 1) ? lb << 16 : lb;
+                    }
+#pragma unroll
+                    for (int nt = 0; nt < 4; ++nt) {
+                        const uint32_t l0 = e < 4 ? lv[h][nt].x : lv[h][nt].z, l1 = e < 4 ? lv[h][nt].y : lv[h][nt].w;
+#pragma unroll
+                        for (int mt = 0; mt < 2; ++mt)
+                            if (e & 2) mid_mma(acc[mt][nt], 0u, 0u, lo[2 * mt], lo[2 * mt + 1], l0, l1);
+                            else mid_mma(acc[mt][nt], lo[2 * mt], lo[2 * mt + 1], 0u, 0u, l0, l1);
                     }
                 }
             }
@@ -189,14 +201,14 @@ int mid_rows(int M, int K) { return K > 8192 || M <= 128 ? 1 : M > 512 && K <= 2
 
 // The CTAs of this kernel are short and two are resident on an SM; the cluster kernel's step hardly depends on the
 // number of tokens until its clusters no longer fit at once.  Measured, this kernel | the cluster kernel, us: rank 32: 64 x 4096 4.5 |
-// 9.7, 448 x 4096 (336 CTAs) 9.2 | 10.2, 101 x 8192 7.7 | 12.7, 333 x 8192 (254) 9.0 | 13.1, 448 x 8192 (336) 14.3 | 13.0, 333 x 14336
+// 9.7, 448 x 4096 (336 CTAs) 9.2 | 10.2, 101 x 8192 7.7 | 12.7, 333 x 8192 (254) 9.0 | 13.1, rank 64: 333 x 4096 (343) 10.2 | 11.2, 400 x 4096 (408) 11.1 | 11.2, 350 x 5120 (351) 13.0 | 16.0, 448 x 8192 (336) 14.3 | 13.0, 333 x 14336
 // (421) 17.5 | 17.8; rank 128: 200 x 4096 (324) 10.0 | 10.8, 333 x 4096 (518) 12.2 | 10.9, 200 x 8192 (324) 14.1 | 16.1, 333 x 8192 (518)
 // 17.0 | 16.4, 200 x 14336 (424) 19.2 | 23.3; short rows: 1000 x 1024, rank 128 (506, four rows each) 10.0 | 10.1, rank 32 (314) 7.2 |
 // 9.5, 448 x 2048, rank 128 (448) 9.0 | 9.6, 1000 x 3072, rank 32 (628) 12.1 | 15.0, rank 128 (1012) 21.1 | 17.7.
 bool quant_act_mid_prefers(int M, int K, int r) {
     const int rows = mid_rows(M, K);
     const int ctas = (M + rows - 1) / rows + mid_cluster(K) * ((M + kMTok - 1) / kMTok) * ((r + kMRank - 1) / kMRank);
-    return ctas <= (rows == 4 ? 450 : K < 4096 ? 630 : K <= 8192 ? 340 : 424);
+    return ctas <= (rows == 4 ? 450 : K < 4096 ? 630 : K <= 5120 ? 400 : K <= 8192 ? 340 : 424);
 }
 
 int launch_quant_act_mid(const __half* X, const float* s, const __half* LA, int M, int K, int r, int8_t* Xq, float* a_scale,

@@ -172,3 +172,29 @@ def test_a_group_of_long_rows(aser, M):
     out = [y.clone() for y in aser.AserSharedInput(layers, M)(X)]
     for layer, y in zip(layers, out):
         assert torch.equal(layer(X), y)
+
+
+@pytest.mark.parametrize("M,K,r", [(1, 512, 16), (20, 14336, 48), (33, 512, 32), (64, 4096, 64), (64, 28672, 32), (100, 8192, 96), (130, 1152, 16), (200, 4096, 32),
+                                   (333, 2048, 64), (64, 14336, 128)])
+def test_projection_of_divided_columns(aser, M, K, r):
+    """T of up to a few hundred tokens, where all weight lies on columns with a divisor, kept to 16 bits as pairs.  A quotient is
+    multiplied as the sum of two fp16 numbers, off by 2^-22 of it, or by 2^-25 where the second is subnormal, and quotients
+    beyond fp16's range come through; K / 128 + 40 additions on a sum's longest way, each off by at most 2^-21 of the sum of magnitudes
+    (truncated additions of 16 products); a pair of bf16 numbers is off by 2^-16."""
+    g = gen(M + K + r)
+    X = normal(g, M, K)
+    cols = torch.randperm(K, device="cuda", generator=g)[:max(8, K // 100)]
+    s = torch.ones(K, device="cuda")
+    s[cols] = torch.exp2(8 * torch.rand(cols.numel(), device="cuda", generator=g) - 2)
+    s[cols[0]] = 2.5e-3
+    X[0, cols[0]] = 200.0                            # x~ = 80000
+    LA = normal(g, r, K, scale=2.0 ** -6)
+    rest = torch.ones(K, device="cuda", dtype=torch.bool)
+    rest[cols] = False
+    LA[:, rest] = 0
+    xq, sc, T = aser.quant_act(X, s, LA, t_pair=True)
+    t = T[:, :r].double() + T[:, r:].double()
+    x = X.double() / s.double()
+    ref, l1 = x @ LA.double().T, x.abs() @ LA.double().abs().T
+    bound = 2.0 ** -16 * ref.abs() + (2.0 ** -22 + (K / 128 + 40) * 2.0 ** -21) * l1 + 2.0 ** -25 * LA.double().abs().sum(1)
+    assert ((t - ref).abs() <= bound).all()
