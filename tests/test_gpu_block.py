@@ -163,12 +163,13 @@ def test_product_of_long_rows(aser, M, F, K, r, act):
 
 
 @pytest.mark.parametrize("M", [1, 16])
-def test_a_group_of_long_rows(aser, M):
-    g = gen(M)
-    s = divisors(g, 8192)
-    layers = [aser.AserLinear(normal(g, n, 8192, scale=0.05), s, normal(g, rr, 8192, scale=0.02), normal(g, n, rr, scale=0.05), M)
-              for n, rr in ((1032, 32), (512, 16), (640, 128))]
-    X = normal(g, M, 8192)
+@pytest.mark.parametrize("N,K,r", [((1032, 512, 640), 8192, (32, 16, 128)), ((4096, 3208), 4096, (64, 64)), ((2048, 2048, 520), 10240, (16, 0, 256))])
+def test_a_group_of_long_rows(aser, M, N, K, r):
+    g = gen(M + K)
+    s = divisors(g, K)
+    layers = [aser.AserLinear(normal(g, n, K, scale=0.05), s, normal(g, rr, K, scale=0.02) if rr else None,
+                              normal(g, n, rr, scale=0.05) if rr else None, M) for n, rr in zip(N, r)]
+    X = normal(g, M, K)
     out = [y.clone() for y in aser.AserSharedInput(layers, M)(X)]
     for layer, y in zip(layers, out):
         assert torch.equal(layer(X), y)
