@@ -147,6 +147,17 @@ int aser_quant_act_ws(const void* X_f16, const float* s, const void* LA_f16,
                       void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * aser_quant_act_fine -- the activation step for what feeds another quantized layer, as the first layer of a feed-forward block
+ * does: aser_quant_act_ws with 8-bit codes, and with the quotients x~ in T to 22 bits at any number of tokens, as long as
+ * at most 128 columns have a divisor other than 1 (with more, parts of K may fall back to fp16 quotients).  A quotient
+ * rounded to fp16 moves 2 % of T's values by a step of bf16: as little as T's own rounding in the layer's output, but
+ * such a step also moves codes of the next layer's input.
+ * r <= 256; workspace as for aser_quant_act_ws.
+ */
+int aser_quant_act_fine(const void* X_f16, const float* s, const void* LA_f16, int M, int K, int r, int8_t* Xq,
+                        float* a_scale, void* T_bf16, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * aser_linear_w4a8_lr -- integer GEMM, dequantisation and up projection
  * (Sec. 4.2: W_q X + L_A L_B X in the paper's letters):
  *   acc[m,n] = sum_k Xq[m,k] * q[n,k]                               (exact int32)
@@ -274,7 +285,7 @@ int aser_forward(const void* X_f16, const float* s, const void* LA_f16, const vo
  *     H[m,i] = fp16( act(G[m,i]) * U[m,i] )                            (fp32, one rounding)
  * H_f16 [M, N / 2]; N % 16 == 0; workspace as for aser_linear_w4a8_lr.  r == 0 (T and L_B NULL) gives the plain product.
  *
- * aser_forward_ffn -- the whole block: activation step of X, the launch above, activation step of H, the down projection
+ * aser_forward_ffn -- the whole block: activation step of X (aser_quant_act_fine), the launch above, activation step of H, the down projection
  * (K = F, so F % 128 == 0), four to six launches in all, each a programmatic dependent of the one before.  s_down [F] or NULL,
  * LA_down [r_down, F], Wk_down / w_scale_down / LB_down of the [N, F] down projection.  The codes, scales, T and H of
  * both steps are kept in the workspace: aser_forward_ffn_workspace_bytes(...) bytes, zeroed once with aser_workspace_init (0

@@ -13,7 +13,7 @@ _BINDING_NAMES = (
     "pack_w4", "repack_w4", "unrepack_w4", "repacked_bytes", "quant_act",
     "linear_w4a8_lr", "linear_w4a8", "linear_w4a8_lr_simt", "linear_w4a8_lr_static",
     "workspace_bytes", "new_workspace", "check_status", "forward_host",
-    "AserLinear", "EXPORTED_SYMBOLS", "pad_rank", "pair_up_projection", "quant_act_ws", "quant_workspace_bytes", "quant_act_ws_launches", "forward_act_launches",
+    "AserLinear", "EXPORTED_SYMBOLS", "pad_rank", "pair_up_projection", "quant_act_ws", "quant_act_fine", "quant_workspace_bytes", "quant_act_ws_launches", "forward_act_launches",
     "linear_w4a8_lr_ld", "AserSharedInput", "AserSharedInputCat", "construct",
     "AserGatedFFN", "interleave_gate_up", "linear_w4a8_lr_glu", "ACTIVATIONS", "AserAdapters", "AdapterPlan",
 )

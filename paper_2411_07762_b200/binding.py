@@ -17,7 +17,7 @@ EXPORTED_SYMBOLS = (
     "aser_forward_shared_workspace_bytes", "aser_construct", "aser_construct_workspace_bytes", "aser_linear_w4a8_lr", "aser_linear_w4a8", "aser_linear_w4a8_lr_simt", "aser_linear_w4a8_lr_static",
     "aser_workspace_bytes", "aser_workspace_init", "aser_check_status", "aser_forward",
     "aser_forward_host", "aser_linear_w4a8_lr_glu", "aser_forward_ffn_workspace_bytes", "aser_forward_ffn",
-    "aser_adapters_plan_bytes", "aser_adapters_plan", "aser_adapters_add", "aser_adapters_workspace_bytes", "aser_forward_adapters",
+    "aser_adapters_plan_bytes", "aser_adapters_plan", "aser_quant_act_fine", "aser_adapters_add", "aser_adapters_workspace_bytes", "aser_forward_adapters",
     "aser_last_error", "aser_version",
 )
 
@@ -45,6 +45,7 @@ lib.aser_linear_kernel.argtypes = [_I, _I, _I]
 lib.aser_quant_act_ws_launches.argtypes = [_I, _I]
 lib.aser_quant_act_ws_launches.restype = _I
 lib.aser_quant_act_ws.argtypes = [_P, _P, _P, _I, _I, _I, _I, _I, _P, _P, _P, _P, _Z, _P]
+lib.aser_quant_act_fine.argtypes = [_P, _P, _P, _I, _I, _I, _P, _P, _P, _P, _Z, _P]
 lib.aser_linear_w4a8_lr_ld.argtypes = [_P, _P, _P, _P, _P, _I, _P, _I, _I, _I, _I, _P, _P, _P, _Z, _P]
 lib.aser_forward_shared_workspace_bytes.argtypes = [_I, _P, _P, _I, _I]
 lib.aser_forward_shared_workspace_bytes.restype = _Z
@@ -207,6 +208,25 @@ def quant_act_ws(X: torch.Tensor, s, L_A, ws: torch.Tensor | None = None, out=No
     _chk(lib.aser_quant_act_ws(_ptr(X), _ptr(s), _ptr(L_A) if r else None, M, K, r, act_bits,
                                1 if t_pair else 0, _ptr(Xq), _ptr(a_scale), _ptr(T) if r else None,
                                _ptr(ws), ws.numel(), _stream()), "aser_quant_act_ws")
+    return Xq, a_scale, T
+
+
+def quant_act_fine(X: torch.Tensor, s, L_A, ws: torch.Tensor | None = None, out=None):
+    """aser_quant_act_fine: quant_act for what feeds another quantized layer (the quotients X / s enter T to 22 bits), the
+    first step of a gated feed-forward block."""
+    _dev(X, torch.float16, "X")
+    M, K = X.shape
+    r = 0 if L_A is None else L_A.shape[0]
+    if ws is None:
+        ws = torch.empty((max(1024, quant_workspace_bytes(M, K, r)),), dtype=torch.uint8, device=X.device)
+    if out is None:
+        Xq = torch.empty((M, K), dtype=torch.int8, device=X.device)
+        a_scale = torch.empty((M,), dtype=torch.float32, device=X.device)
+        T = torch.empty((M, r), dtype=torch.bfloat16, device=X.device)
+    else:
+        Xq, a_scale, T = out
+    _chk(lib.aser_quant_act_fine(_ptr(X), _ptr(s), _ptr(L_A) if r else None, M, K, r, _ptr(Xq), _ptr(a_scale),
+                                 _ptr(T) if r else None, _ptr(ws), ws.numel(), _stream()), "aser_quant_act_fine")
     return Xq, a_scale, T
 
 

@@ -2,7 +2,8 @@
 //
 //   act_proj_kernel    T.  A CTA owns 128 tokens and one slice of K; TMA streams the slice of X
 //                      through a shared-memory ring together with the matching columns of L_A.  The consumer
-//                      warps write x / s back as fp16 where s != 1, one thread issues tcgen05.mma
+//                      warps write x / s back as fp16 where s != 1 (fine: what that leaves of the quotients of up to 128 columns of a
+//                      slice is multiplied at the end), one thread issues tcgen05.mma
 //                      (kind::f16) with L_A on the M side (up to four groups of 128 rows, so the
 //                      down projections of several layers that share X are computed in one pass)
 //                      and the 128 tokens on the N side.  The slices' partial T are summed in order and rounded to bf16.
@@ -56,6 +57,9 @@ constexpr bool rows_beside(int M, int K, int r) { return M >= beside_from(K, r);
 constexpr int kPMaxCluster = 8;             // CTAs of a cluster
 constexpr int kPCacheUnits = 254;           // 8-column units with a divisor whose divisors are kept in shared memory
 constexpr int kPUncached = 255;             // tag of such a unit beyond the cache: its divisors are read from global memory
+// fine: columns of a slice with a divisor whose quotients are multiplied as the sum of two fp16 numbers (more: as one, all of them).
+constexpr int kPRest = 128;
+constexpr int kPRestBytes = kPRest * 2 + 16;
 
 // Stages of the ring.  Beside act_rows_kernel they leave room on the SM for two CTAs of act_rows_kernel (K bytes of mask, 4.2
 // KB, and a KB per resident CTA); at least the 128 KB that later stage the partial T.
@@ -124,11 +128,12 @@ __device__ __forceinline__ void pj_stage_t(uint32_t tmem, int g, uint32_t buf, i
 // map_x: X as fp16 [K / 64 blocks][M][64], box 1 block x 128 rows, 128-byte swizzle (rows past
 // M read as zero).  map_la: L_A as fp16 [K / 64 blocks][r][64], box 1 block x r rows (r / 2 rows
 // above 256).
-template <bool MAXIMA>
-__global__ void __launch_bounds__(kPThreads, 1)
+// (At most 64 registers where act_rows_kernel has to find room beside it.)
+template <bool MAXIMA, bool FINE>
+__global__ void __launch_bounds__(kPThreads, FINE && !MAXIMA ? 3 : 1)
 act_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_la,
-                const float* __restrict__ s, int M, int K, int r, float* __restrict__ amax_part,
-                float* __restrict__ t_part, __nv_bfloat16* __restrict__ T, int ldt, int lo_off) {
+                const __half* __restrict__ X, const __half* __restrict__ LA, const float* __restrict__ s, int M, int K, int r,
+                float* __restrict__ amax_part, float* __restrict__ t_part, __nv_bfloat16* __restrict__ T, int ldt, int lo_off) {
     // The r rows of L_A arrive as one box (r <= 256, the largest box) or as two boxes of r / 2
     // rows; in shared memory the rows follow one another, 128 bytes each, so group g is the 16 KB
     // at g * 16 KB whatever the boxes.  Where r is not a multiple of 128 the last group's MMA also
@@ -166,7 +171,9 @@ act_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
     // per 8 columns of the slice: 0 = all divisors are 1, else 1 + the unit's place in s_cache (or kPUncached)
     uint8_t* unit_tag = tail + 256;
     float* s_cache = reinterpret_cast<float*>(tail + 256 + ((Kc / 8 + 15) & ~15));  // [kPCacheUnits][8] divisors
-    float* amax_w = s_cache + kPCacheUnits * 8;                     // MAXIMA: [8 warps][128 rows]
+    uint16_t* rest_col = reinterpret_cast<uint16_t*>(s_cache + kPCacheUnits * 8);   // [kPRest] columns of the slice with a divisor, in order
+    int* n_rest = reinterpret_cast<int*>(rest_col + kPRest);
+    float* amax_w = s_cache + kPCacheUnits * 8 + (FINE ? kPRestBytes / 4 : 0);   // MAXIMA: [8 warps][128 rows]
     int* n_cached = reinterpret_cast<int*>(tail + 25 * 8 + 16);
     const uint32_t tmem_cols = groups <= 1 ? 128u : groups == 2 ? 256u : 512u;
 
@@ -294,6 +301,34 @@ act_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
         // ================= consumers =================
         // Warp cw owns the 16-byte piece cw (8 columns) of every row; lane = rows lane, +32, +64, +96.
         const int cw = warp - 2;
+        if (FINE && warp == 2) {             // the columns with a divisor, in their order (while the ring fills)
+            int n = 0;
+            for (int g0 = 0; g0 < Kc / 8 && n <= kPRest; g0 += 32) {
+                const int g = g0 + lane, tag = g < Kc / 8 ? unit_tag[g] : 0;
+                unsigned mine = 0;
+                if (tag != 0) {
+                    const float* sp = tag != kPUncached ? s_cache + (tag - 1) * 8 : s + k0 + g * 8;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) mine |= sp[e] != 1.f ? 1u << e : 0u;
+                }
+                int at = __popc(mine);
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int up = __shfl_up_sync(0xffffffffu, at, o);
+                    if (lane >= o) at += up;
+                }
+                const int all = __shfl_sync(0xffffffffu, at, 31);
+                at += n - __popc(mine);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (mine >> e & 1) {
+                        if (at < kPRest) rest_col[at] = (uint16_t)(g * 8 + e);
+                        ++at;
+                    }
+                n += all;
+            }
+            if (lane == 0) *n_rest = n <= kPRest ? n : 0;
+        }
         float amax[4] = {0.f, 0.f, 0.f, 0.f};
         __half2 hmax[4];
 #pragma unroll
@@ -335,7 +370,7 @@ act_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
                                 const __half hv = __ushort_as_half((unsigned short)((e & 1) ? (word >> 16) : (word & 0xffffu)));
                                 const float f = __fdiv_rn(__half2float(hv), sv[e]);
                                 if (MAXIMA) amax[q] = fmaxf(amax[q], fabsf(f));
-                                const uint32_t hb = (uint32_t)__half_as_ushort(__float2half_rn(f));
+                                const uint32_t hb = (uint32_t)__half_as_ushort(__float2half_rn(FINE ? fminf(fmaxf(f, -65504.f), 65504.f) : f));
                                 wd[q][e >> 1] = (e & 1) ? ((word & 0x0000ffffu) | (hb << 16)) : ((word & 0xffff0000u) | hb);
                                 zd[q][e >> 1] &= (e & 1) ? 0x0000ffffu : 0xffff0000u;
                             }
@@ -372,6 +407,62 @@ act_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
         }
         if (ok) ok = pj_warp_wait(bar_acc, 0u, abort_flag, lane);
         tc_fence_after();
+        // ---- fine: what fp16 left of the quotients (x~ - fp16(x~), to fp16), times the same columns of L_A, gathered into the idle
+        // ring 64 at a time ----
+        if (FINE) named_bar_sync(1, kPConsumerWarps * 32);       // the list is there
+        for (int p = 0, n = FINE ? *n_rest : 0; n > 0; ++p, n -= 64) {
+            const uint16_t* col = rest_col + p * 64;
+            const int here = n < 64 ? n : 64, row = (tid - 64) & 127;
+            const bool there = row0 + row < M;
+            const __half *xr = X + (size_t)(there ? row0 + row : 0) * K + k0, *lr = LA + (size_t)row * K + k0;
+            for (int c8 = (tid - 64) >> 7; c8 * 8 < ((here + 15) & ~15); c8 += 2) {
+                const uint32_t at = sb + (uint32_t)row * 128u + (uint32_t)((c8 ^ (row & 7)) << 4);
+                unsigned short v[8], l[8];
+                float d[8];
+                int k[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const bool use = c8 * 8 + e < here;
+                    k[e] = use ? col[c8 * 8 + e] : 0;
+                    v[e] = use && there ? __half_as_ushort(xr[k[e]]) : (unsigned short)0;
+                    d[e] = use ? __ldg(s + k0 + k[e]) : 1.f;
+                    l[e] = use && row < r ? __half_as_ushort(__ldg(lr + k[e])) : (unsigned short)0;
+                }
+                uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float f = __fdiv_rn(__half2float(__ushort_as_half(v[e])), d[e]);
+                    const __half hi = __float2half_rn(fminf(fmaxf(f, -65504.f), 65504.f));
+                    w[e >> 1] |= (uint32_t)__half_as_ushort(__float2half_rn(f - __half2float(hi))) << (16 * (e & 1));
+                }
+                pj_sts128(at, make_uint4(w[0], w[1], w[2], w[3]));
+                for (int g = 0; g < groups; ++g) {
+                    pj_sts128(at + (uint32_t)((1 + g) * kPTileBytes),
+                              make_uint4(l[0] | (uint32_t)l[1] << 16, l[2] | (uint32_t)l[3] << 16, l[4] | (uint32_t)l[5] << 16, l[6] | (uint32_t)l[7] << 16));
+                    if (g + 1 < groups) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            l[e] = c8 * 8 + e < here && (g + 1) * 128 + row < r ? __half_as_ushort(__ldg(lr + (size_t)(g + 1) * 128 * K + k[e])) : (unsigned short)0;
+                    }
+                }
+            }
+            fence_proxy_async_smem();
+            named_bar_sync(1, kPConsumerWarps * 32);
+            if (tid == 64) {
+                if (ok) {
+                    tc_fence_after();
+                    const uint32_t idesc = make_idesc(1u, 0u, 128u, (uint32_t)kPTok);
+                    for (int g = 0; g < groups; ++g)
+                        for (int kk = 0; kk * 16 < here; ++kk)
+                            mma_f16_ss(tmem + g * 128, smem_desc_sw128(sb + (1 + g) * kPTileBytes) + 2 * kk, smem_desc_sw128(sb) + 2 * kk, idesc, 1u);
+                }
+                tc_commit(bar_acc);
+            }
+            __syncwarp();
+            const bool done = pj_warp_wait(bar_acc, (uint32_t)(p + 1) & 1u, abort_flag, lane);
+            ok = ok && done;
+            tc_fence_after();
+        }
         if (MAXIMA) {
             // ---- partial T: tensor memory -> shared memory as [token][128 rows of the group] -> one
             // bulk copy per group into the scratch, where a group's tile is contiguous.  The ring is idle by
@@ -840,10 +931,11 @@ int quant_act_ws_launches(int M, int K) { return M <= 32 ? 1 : 2; }
 
 int launch_quant_act_ws(const __half* X, const float* s, const __half* LA, int M, int K, int r,
                         int8_t* Xq, float* a_scale, __nv_bfloat16* T, void* scratch, size_t scratch_bytes,
-                        cudaStream_t st, int act_bits, bool t_pair, int M_pass) {
+                        cudaStream_t st, int act_bits, bool t_pair, int M_pass, bool fine) {
     const float qmax = (float)((1 << (act_bits - 1)) - 1);
     const int ldt = t_pair ? 2 * r : r, lo_off = t_pair ? r : 0;
     const int groups = (r + 127) / 128;
+    fine = fine && s != nullptr;
     if (groups > kPMaxGroups) return record_error(ASER_ERR_SHAPE, "quant_act: r beyond 512");
     if (M_pass == 0) M_pass = M;
     const bool beside = r > 0 && rows_beside(M_pass, K, r);
@@ -864,10 +956,10 @@ int launch_quant_act_ws(const __half* X, const float* s, const __half* LA, int M
         const int Kc = (K / kPCols + KS - 1) / KS * kPCols, NS = proj_stages(groups, K, beside);       // the longest slice
         // the ring (at least 128 KB: it later stages the partial T) and the tail
         const size_t smem = (size_t)NS * kPTileBytes * (1 + groups) + 256 + ((Kc / 8 + 15) & ~15) +
-                            kPCacheUnits * 8 * sizeof(float) + (beside ? 0 : kPConsumerWarps * kPTok * sizeof(float)) + 1024;
-        auto* kernel = beside ? act_proj_kernel<false> : act_proj_kernel<true>;
-        static size_t configured_all[2][kMaxDevices] = {{0}};
-        size_t* configured = configured_all[beside ? 0 : 1];
+                            kPCacheUnits * 8 * sizeof(float) + (fine ? kPRestBytes : 0) + (beside ? 0 : kPConsumerWarps * kPTok * sizeof(float)) + 1024;
+        auto* kernel = fine ? (beside ? act_proj_kernel<false, true> : act_proj_kernel<true, true>) : beside ? act_proj_kernel<false, false> : act_proj_kernel<true, false>;
+        static size_t configured_all[4][kMaxDevices] = {{0}};
+        size_t* configured = configured_all[(beside ? 0 : 1) + (fine ? 2 : 0)];
         int dev = 0;
         int rc = current_device(&dev);
         if (rc != ASER_OK) return rc;
@@ -892,7 +984,7 @@ int launch_quant_act_ws(const __half* X, const float* s, const __half* LA, int M
         pcfg.gridDim = dim3(KS, (M + kPTok - 1) / kPTok, 1);
         pcfg.blockDim = dim3(kPThreads, 1, 1);
         pcfg.dynamicSmemBytes = smem;
-        e = cudaLaunchKernelEx(&pcfg, kernel, mx, mla, s, M, K, r, amax_part, t_part, T, ldt, lo_off);
+        e = cudaLaunchKernelEx(&pcfg, kernel, mx, mla, X, LA, s, M, K, r, amax_part, t_part, T, ldt, lo_off);
         if (e != cudaSuccess) return record_cuda_error(e, "act_proj_kernel");
     }
     if (r > 0 && !beside) {

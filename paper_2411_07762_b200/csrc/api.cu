@@ -238,15 +238,18 @@ bool forward_act_uses_scratch(int M, int K, int r) {
 // the whole, so every token gets the same bits.
 int quant_with_workspace(const void* X_f16, const float* s, const void* LA_f16, int M, int M_pass, int K, int r,
                          int act_bits, bool t_pair, int8_t* Xq, float* a_scale, void* T_bf16,
-                         void* workspace, size_t workspace_bytes, void* stream) {
+                         void* workspace, size_t workspace_bytes, void* stream, bool fine = false) {
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (!forward_act_uses_scratch(M_pass, K, r))
+    // fine: the one-launch kernel for many tokens rounds the quotients, so only the other two are left
+    fine = fine && r > 0 && s != nullptr;
+    const bool scratch = fine ? M > 32 && !(r <= 128 && quant_act_mid_prefers(M, K, r)) : forward_act_uses_scratch(M_pass, K, r);
+    if (!scratch)
         return launch_quant_act(static_cast<const __half*>(X_f16), s, static_cast<const __half*>(LA_f16), M, K, r,
                                 Xq, a_scale, static_cast<__nv_bfloat16*>(T_bf16), st, act_bits, t_pair, M_pass);
     return launch_quant_act_ws(static_cast<const __half*>(X_f16), s, static_cast<const __half*>(LA_f16), M, K, r,
                                Xq, a_scale, static_cast<__nv_bfloat16*>(T_bf16),
                                static_cast<uint8_t*>(workspace) + kWsZeroedBytes,
-                               workspace_bytes - kWsZeroedBytes, st, act_bits, t_pair, M_pass);
+                               workspace_bytes - kWsZeroedBytes, st, act_bits, t_pair, M_pass, fine);
 }
 
 // ---- aser_forward_host: copies beside the computation ----
@@ -558,6 +561,26 @@ int aser_quant_act_ws(const void* X_f16, const float* s, const void* LA_f16, int
                                workspace_bytes - kWsZeroedBytes, st, act_bits, t_pair != 0);
 }
 
+int aser_quant_act_fine(const void* X_f16, const float* s, const void* LA_f16, int M, int K, int r, int8_t* Xq, float* a_scale,
+                        void* T_bf16, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!act_shape_ok(M, K, r) || r > 256) return fail(ASER_ERR_SHAPE, "unsupported M, K or r");
+    if (M == 0) return ASER_OK;
+    ASER_REQUIRE_PTR(X_f16);
+    ASER_OPTIONAL_PTR(s);
+    ASER_REQUIRE_PTR(Xq);
+    ASER_REQUIRE_PTR(a_scale);
+    if (r > 0) {
+        ASER_REQUIRE_PTR(LA_f16);
+        ASER_REQUIRE_PTR(T_bf16);
+    }
+    if (workspace == nullptr || misaligned16(workspace) || workspace_bytes < aser_quant_workspace_bytes(M, K, r))
+        return fail(ASER_ERR_WORKSPACE, "workspace missing, misaligned or too small");
+    const int rc = check_device();
+    if (rc != ASER_OK) return rc;
+    return quant_with_workspace(X_f16, s, r > 0 ? LA_f16 : nullptr, M, M, K, r, 8, false, Xq, a_scale, r > 0 ? T_bf16 : nullptr, workspace,
+                                workspace_bytes, stream, /*fine=*/true);
+}
+
 int aser_forward_act_launches(int M, int K, int r) {
     if (!act_shape_ok(M, K, r) || M == 0) return 0;
     return forward_act_uses_scratch(M, K, r) && r > 0 ? quant_act_ws_launches(M, K) : 1;
@@ -660,7 +683,7 @@ int aser_forward_ffn(const void* X_f16, const float* s, const void* LA_f16, cons
     float* a_scale = reinterpret_cast<float*>(ws + l.a_scale);
     void *T = ws + l.T, *H = ws + l.H;
     rc = quant_with_workspace(X_f16, s, r > 0 ? LA_f16 : nullptr, M, M, K, r, 8, false, Xq, a_scale, r > 0 ? T : nullptr,
-                              workspace, l.kernels, stream);
+                              workspace, l.kernels, stream, /*fine=*/true);
     if (rc != ASER_OK) return rc;
     rc = linear_common(Xq, a_scale, Wk_gu, w_scale_gu, r > 0 ? T : nullptr, r > 0 ? LB_gu_f16 : nullptr, M, 2 * F, K, r, H,
                        nullptr, workspace, l.kernels, stream, /*overlap_prev=*/true, 0, CatSplit(), &glu);

@@ -49,7 +49,7 @@ size_t quant_act_ws_scratch_bytes(int M, int K, int r);
 int quant_act_ws_launches(int M, int K);     // kernels one call enqueues
 int launch_quant_act_ws(const __half* X, const float* s, const __half* LA, int M, int K, int r,
                         int8_t* Xq, float* a_scale, __nv_bfloat16* T, void* scratch, size_t scratch_bytes,
-                        cudaStream_t st, int act_bits = 8, bool t_pair = false, int M_pass = 0);
+                        cudaStream_t st, int act_bits = 8, bool t_pair = false, int M_pass = 0, bool fine = false);
 // Device-side construction of a layer's factors (construct.cu); synchronises the stream.
 constexpr int kConstructIterations = 22;     // applications of A A^T unless the caller says otherwise
 size_t construct_workspace_bytes(int N, int K, int Tcal, int r, int n_split);

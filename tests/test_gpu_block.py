@@ -199,3 +199,30 @@ def test_projection_of_divided_columns(aser, M, K, r):
     ref, l1 = x @ LA.double().T, x.abs() @ LA.double().abs().T
     bound = 2.0 ** -16 * ref.abs() + (2.0 ** -22 + (K / 128 + 40) * 2.0 ** -21) * l1 + 2.0 ** -25 * LA.double().abs().sum(1)
     assert ((t - ref).abs() <= bound).all()
+
+
+@pytest.mark.parametrize("M,K,r,divided", [(20, 512, 16, 9), (100, 4096, 64, 41), (450, 4096, 64, 41), (500, 8192, 192, 82), (333, 8192, 48, 128), (700, 14336, 128, 143),
+                                           (1500, 4096, 256, 128), (4100, 1024, 32, 1), (129, 2048, 256, 100), (300, 128, 256, 128)])
+def test_fine_projection(aser, M, K, r, divided):
+    """T of any number of tokens with all weight on the divided columns: the bound of test_projection_of_divided_columns with T's one
+    rounding to bf16 (2^-8).  Quotients beyond fp16's range come through.  Codes and scales are those of the plain step."""
+    g = gen(M + K + r)
+    X = normal(g, M, K)
+    cols = torch.randperm(K, device="cuda", generator=g)[:divided]
+    s = torch.ones(K, device="cuda")
+    s[cols] = torch.exp2(8 * torch.rand(cols.numel(), device="cuda", generator=g) - 2)
+    s[cols[0]] = 2.5e-3
+    X[M - 1, cols[0]] = 200.0                        # x~ = 80000
+    LA = normal(g, r, K, scale=2.0 ** -6)
+    rest = torch.ones(K, device="cuda", dtype=torch.bool)
+    rest[cols] = False
+    LA[:, rest] = 0
+    Xq, sc, T = aser.quant_act_fine(X, s, LA)
+    plain = aser.quant_act(X, s, LA)
+    assert torch.equal(Xq, plain[0]) and torch.equal(sc, plain[1])
+    x = X.double() / s.double()
+    ref, l1 = x @ LA.double().T, x.abs() @ LA.double().abs().T
+    bound = 2.0 ** -8 * ref.abs() + 2 * ((2.0 ** -22 + (K / 128 + 40) * 2.0 ** -21) * l1 + 2.0 ** -25 * LA.double().abs().sum(1))
+    assert ((T.double() - ref).abs() <= bound).all()
+    again = aser.quant_act_fine(X, s, LA)
+    assert all(torch.equal(a, b) for a, b in zip((Xq, sc, T), again))

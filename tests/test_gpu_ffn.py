@@ -138,7 +138,7 @@ class Steps:
 
     def __call__(self, X, act):
         f, M = self.first, X.shape[0]
-        f.quant(X)
+        self.aser.quant_act_fine(X, f.s, f.L_A, f.ws, out=(f.Xq, f.a_scale, f.T))
         f.linear(M)
         H = self.aser.linear_w4a8_lr_glu(f.Xq[:M], f.a_scale, f.Wk, f.w_scale, f.T, f.L_B, 2 * self.F, f.ws, act)
         return f.Y[:M], H, self.down(H)

@@ -27,6 +27,15 @@ def test_gated_linear_is_refused(lib):
     assert call(ws=None) == WORKSPACE and call(nbytes=1000) == WORKSPACE and call(ws=ODD) == WORKSPACE
 
 
+def test_fine_activation_step_is_refused(lib):
+    def call(M=40, K=256, r=16, X=GOOD, s=GOOD, LA=GOOD, Xq=GOOD, T=GOOD, ws=GOOD, nbytes=1 << 26):
+        return lib.aser_quant_act_fine(X, s, LA, M, K, r, Xq, GOOD, T, ws, nbytes, None)
+    assert call(M=0, X=None, ws=None) == OK
+    assert call(K=200) == SHAPE and call(r=24) == SHAPE and call(r=272) == SHAPE and call(M=-1) == SHAPE
+    assert call(X=None) == NULL and call(LA=None) == NULL and call(T=None) == NULL and call(Xq=None) == NULL and call(s=ODD) == ALIGN
+    assert call(ws=None) == WORKSPACE and call(nbytes=1000) == WORKSPACE
+
+
 def test_feed_forward_is_refused(lib):
     def call(M=4, K=128, F=256, N=128, r=16, rd=16, act=0, X=GOOD, LA=GOOD, LAd=GOOD, sd=None, Y=GOOD, ws=GOOD, nbytes=1 << 26):
         return lib.aser_forward_ffn(X, None, LA, GOOD, GOOD, GOOD, sd, LAd, GOOD, GOOD, GOOD, M, K, F, N, r, rd, act, Y, ws,
