@@ -215,21 +215,19 @@ bool act_shape_ok(int M, int K, int r) {
 }
 
 // Which activation kernels a forward pass runs.  The two kernels with scratch are the only path above rank 128 (stacked down
-// projections of a shared-input group).  Below, one launch (quant_act_mid while its CTAs are about one wave, else the cluster
-// kernel) has less fixed cost; up to seven of the cluster kernel's 64-token clusters of 16 CTAs are resident at once,
-// and at the eighth its time steps up.  One launch | two kernels, us, rank 32: 448 / 449 x 4096 9.0 | 11.1 and 12.7 | 10.8, 448 / 449 x 8192 13.6 |
-// 16.1 and 18.5 | 15.8, 448 / 449 x 14336 18.5 | 20.7 and 26.2 | 21.0, 1024 x 4096 18.6 | 12.1; rank 128: 448 / 449 x 4096 11.1 | 12.0 and 15.8 |
-// 12.0, 448 / 449 x 8192 15.6 | 17.2 and 23.2 | 16.8, 448 / 449 x 14336 22.4 | 22.1 and 35.5 | 23.7.  Shorter rows step up later, but not all at the
-// same number of tokens: rank 32: 700 / 1024 x 3072 9.1 | 10.4 and 15.4 | 10.9, 1024 x 2048 9.1 | 9.4, 1023 x 1536 7.9 | 9.3, 1000 / 4096 x 1024
-// 7.7 | 8.8 and 13.6 | 11.5; rank 128: 700 / 1000 x 3072 12.6 | 11.5 and 18.7 | 12.2, 896 / 1000 x 2048 11.2 | 10.8 and 15.3 | 10.8, 1023 x
-// 1536 12.9 | 10.5, 1000 / 4096 x 1024 10.8 | 9.8 and 16.4 | 11.9, 448 x 5120 17.0 | 13.6, 448 x 7168 21.0 | 15.6: between these lines two kernels would
-// gain, most at rank 128.  Up to 32 tokens the few-token kernel serves every rank.
+// projections of a shared-input group).  Below, quant_act_mid has less fixed cost while its CTAs are about one wave.  Beyond
+// it the cluster kernel is left only where sixteen CTAs share a row's 128-column blocks evenly, up to seven of its clusters, which are
+// resident at once (one launch | two kernels, us, rank 64 or 128: 448 x 4096 10.6 | 11.9, 320 x 8192 15.4 | 18.0, 320 x 14336 19.3 |
+// 22.5; 449 x 4096 15.8 | 12.0, 449 x 14336 35.5 | 23.7; 700 x 2048 11.2 | 10.5), and for short rows (2000 x 256 9.4 | 10.5, 2000 x 1024 11.0 |
+// 9.6).  With fewer CTAs to a row it is the slower one everywhere: 448 x 4608 21.5 | 12.7, 448 x 5120 15.8 | 13.1, 230 x 6400 52.5 | 14.4, 230 x
+// 7168 20.6 | 14.6, 230 x 11008 82.6 | 20.7, 320 x 13824 56.7 | 23.3, 700 x 2432 32.7 | 11.2, 1000 x 1152 20.1 | 10.3.  Up to 32 tokens the
+// few-token kernel serves every rank.
 bool forward_act_uses_scratch(int M, int K, int r) {
     if (M <= 32) return false;
     if (r > 128) return true;
-    if (K >= 4096) return M > 448;
+    if (quant_act_mid_prefers(M, K, r)) return false;
     if (K <= 1024) return M > 4096;
-    return M >= 1024;
+    return K / 128 % 16 != 0 || M > (K < 4096 ? 1023 : 448);
 }
 
 // The activation step of a forward pass (the scratch of the two-kernel path sits behind the
