@@ -73,8 +73,8 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-// Which adapter a tile has is known one round trip later than where its rank stands: the whole list is asked for meanwhile (a
-// thread per 32 bytes), so that the look-up finds it near.
+// Which adapter a tile has is known one round trip later than where its rank stands: the list is asked for meanwhile (a
+// thread per 32 bytes: the first 2048 adapters), so that the look-up finds it near.
 __device__ __forceinline__ void warm_ranks(const AdapterParams& p) {
     const int i = (int)threadIdx.x * 8;
     int v;
