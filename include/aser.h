@@ -148,8 +148,8 @@ int aser_quant_act_ws(const void* X_f16, const float* s, const void* LA_f16,
 
 /*
  * aser_quant_act_fine -- the activation step for what feeds another quantized layer, as the first layer of a feed-forward block
- * does: aser_quant_act_ws with 8-bit codes, and with the quotients x~ in T to 22 bits at any number of tokens, as long as
- * at most 128 columns have a divisor other than 1 (with more, parts of K may fall back to fp16 quotients).  A quotient
+ * does: aser_quant_act_ws with 8-bit codes, and with the quotients x~ in T to 22 bits at any number of tokens and of divided
+ * columns (magnitudes from 131008 on become infinite; many divisors other than 1 cost a second pass over X).  A quotient
  * rounded to fp16 moves 2 % of T's values by a step of bf16: as little as T's own rounding in the layer's output, but
  * such a step also moves codes of the next layer's input.
  * r <= 256; workspace as for aser_quant_act_ws.

@@ -60,6 +60,21 @@ __device__ __forceinline__ void store_t2(__nv_bfloat16* row, int j, float t0, fl
 // every undivided element is zero (the smallest fp16 magnitude over 127 is 4.7e-10); what smoothing divided goes by exact codes.
 __device__ __forceinline__ float code_rcp(float sc) { return sc > 0x1p-127f ? __frcp_rn(sc) : 0.f; }
 
+// The reciprocal of a divisor as a double-length number (Dekker): x first + x second, the sum rounded once, is x / d but for one case in
+// millions next to a tie, for an fp16 x at a fraction of a division.  The first part is taken a little short, so that the second is never zero and has
+// its sign (an infinite x stays infinite).  Divisors are taken into the range where both parts are normal numbers: quotients by what lies
+// outside are 0 or infinite in fp16 all the same.
+struct Divisor { float first, second; };
+__device__ __forceinline__ Divisor divisor_parts(float d) {
+    d = copysignf(fminf(fmaxf(fabsf(d), 0x1p-100f), 0x1p100f), d);
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d));
+    r *= 1.f - 0x1p-21f;
+    const float rem = fmaf(-d, r, 1.f);
+    return {r, r * fmaf(rem, rem, rem)};
+}
+__device__ __forceinline__ float quotient(float x, const Divisor& d) { return fmaf(x, d.first, x * d.second); }
+
 // Exact codes for eight values (the definition: IEEE quotient, round half to even, clamp).
 static __device__ __noinline__ uint2 quant8_exact(float v0, float v1, float v2, float v3, float v4, float v5,
                                            float v6, float v7, float sc, float qmax) {

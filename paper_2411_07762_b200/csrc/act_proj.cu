@@ -2,8 +2,10 @@
 //
 //   act_proj_kernel    T.  A CTA owns 128 tokens and one slice of K; TMA streams the slice of X
 //                      through a shared-memory ring together with the matching columns of L_A.  The consumer
-//                      warps write x / s back as fp16 where s != 1 (fine: what that leaves of the quotients of up to 128 columns of a
-//                      slice is multiplied at the end), one thread issues tcgen05.mma
+//                      warps write x / s back as fp16 where s != 1 (fine: what that leaves of the quotients is multiplied behind them,
+//                      up to 128 columns of a slice gathered, more in a second turn of the slice through the ring: rank 64, 1 % of the
+//                      columns / all of them divided, us: 600 x 4096 13.6 / 32.5, 4096 x 4096 27 / 87, 600 x 14336, rank 128, 32 /
+//                      110), one thread issues tcgen05.mma
 //                      (kind::f16) with L_A on the M side (up to four groups of 128 rows, so the
 //                      down projections of several layers that share X are computed in one pass)
 //                      and the 128 tokens on the N side.  The slices' partial T are summed in order and rounded to bf16.
@@ -57,7 +59,7 @@ constexpr bool rows_beside(int M, int K, int r) { return M >= beside_from(K, r);
 constexpr int kPMaxCluster = 8;             // CTAs of a cluster
 constexpr int kPCacheUnits = 254;           // 8-column units with a divisor whose divisors are kept in shared memory
 constexpr int kPUncached = 255;             // tag of such a unit beyond the cache: its divisors are read from global memory
-// fine: columns of a slice with a divisor whose quotients are multiplied as the sum of two fp16 numbers (more: as one, all of them).
+// fine: columns with a divisor that are gathered 64 at a time; a slice with more goes through the ring again.
 constexpr int kPRest = 128;
 constexpr int kPRestBytes = kPRest * 2 + 16;
 
@@ -138,6 +140,8 @@ act_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
     // rows; in shared memory the rows follow one another, 128 bytes each, so group g is the 16 KB
     // at g * 16 KB whatever the boxes.  Where r is not a multiple of 128 the last group's MMA also
     // reads the stale rows behind row r; their accumulator rows are never read.
+    // (exact quotients where their maximum is taken, or where they are rounded to fp16 as in the other kernels)
+    constexpr bool kParts = FINE && !MAXIMA;
     const int la_boxes = r <= 256 ? 1 : 2;
     const int la_box_rows = r / la_boxes;
     const uint32_t la_stage_bytes = (uint32_t)r * 128u;
@@ -175,6 +179,7 @@ act_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
     int* n_rest = reinterpret_cast<int*>(rest_col + kPRest);
     float* amax_w = s_cache + kPCacheUnits * 8 + (FINE ? kPRestBytes / 4 : 0);   // MAXIMA: [8 warps][128 rows]
     int* n_cached = reinterpret_cast<int*>(tail + 25 * 8 + 16);
+    int* n_divided = n_cached + 1;                                  // fine: columns of the slice with a divisor
     const uint32_t tmem_cols = groups <= 1 ? 128u : groups == 2 ? 256u : 512u;
 
     if (warp == 0) {
@@ -207,7 +212,7 @@ act_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
         // The smoothing divisors are 1 on all but the few outlier channels.  A unit that has one
         // keeps its eight divisors in shared memory, so that the streaming loop below never waits
         // for global memory.
-        if (tid == 64) *n_cached = 0;
+        if (tid == 64) *n_cached = *n_divided = 0;
         named_bar_sync(1, kPConsumerWarps * 32);
         for (int g = tid - 64; g < Kc / 8; g += kPConsumerWarps * 32) {
             int tag = 0;
@@ -217,6 +222,8 @@ act_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
                 const bool one = a.x == 1.f && a.y == 1.f && a.z == 1.f && a.w == 1.f &&
                                  b.x == 1.f && b.y == 1.f && b.z == 1.f && b.w == 1.f;
                 if (!one) {
+                    if (FINE)
+                        atomicAdd(n_divided, (a.x != 1.f) + (a.y != 1.f) + (a.z != 1.f) + (a.w != 1.f) + (b.x != 1.f) + (b.y != 1.f) + (b.z != 1.f) + (b.w != 1.f));
                     const int at = atomicAdd(n_cached, 1);
                     tag = kPUncached;
                     if (at < kPCacheUnits) {
@@ -233,18 +240,21 @@ act_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
+    // fine: the slice goes through the ring a second time, with the second fp16 numbers of the quotients
+    auto twice = [&] { return FINE && *reinterpret_cast<volatile int*>(n_divided) > kPRest; };
 
     if (warp == 0) {
         // ================= TMA producer =================
         if (lane == 0) {
             bool ok = true;
+            const int turns = twice() ? 2 * nst : nst;
             int issued = (NS < nst) ? NS : nst;
-            for (int i = issued; i < nst && ok; ++i) {
+            for (int i = issued; i < turns && ok; ++i) {
                 const int st = i % NS;
-                ok = pj_wait(bar_free(st), (uint32_t)(i / NS - 1) & 1u, abort_flag);
+                if (i >= NS) ok = pj_wait(bar_free(st), (uint32_t)(i / NS - 1) & 1u, abort_flag);
                 if (!ok) break;
                 const uint32_t dst = sb + st * stage_bytes;
-                const int kblk = (k0 + i * kPCols) / kPCols;
+                const int kblk = k0 / kPCols + (i < nst ? i : i - nst);
                 mbar_arrive_expect_tx(bar_full(st), (uint32_t)kPTileBytes);
                 tma_load_3d(dst, &map_x, 0, row0, kblk, bar_full(st));
                 ++issued;
@@ -258,13 +268,14 @@ act_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
         // ================= L_A producer: one box of up to 256 rows (two groups) per copy =================
         if (lane == 0) {
             bool ok = true;
+            const int turns = twice() ? 2 * nst : nst;
             int issued = 0;
-            for (int i = 0; i < nst && ok; ++i) {
+            for (int i = 0; i < turns && ok; ++i) {
                 const int st = i % NS;
                 if (i >= NS) ok = pj_wait(bar_free(st), (uint32_t)(i / NS - 1) & 1u, abort_flag);
                 if (!ok) break;
                 const uint32_t dst = sb + st * stage_bytes + kPTileBytes;
-                const int kblk = (k0 + i * kPCols) / kPCols;
+                const int kblk = k0 / kPCols + (i < nst ? i : i - nst);
                 mbar_arrive_expect_tx(bar_full(st), la_stage_bytes);
                 for (int b = 0; b < la_boxes; ++b)
                     tma_load_3d(dst + b * la_box_rows * 128, &map_la, 0, b * la_box_rows, kblk, bar_full(st));
@@ -279,8 +290,9 @@ act_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
         // ================= MMA issuer =================
         if (lane == 0) {
             const uint32_t idesc = make_idesc(1u, 0u, 128u, (uint32_t)kPTok);
+            const int turns = twice() ? 2 * nst : nst;
             bool ok = true;
-            for (int i = 0; i < nst && ok; ++i) {
+            for (int i = 0; i < turns && ok; ++i) {
                 const int st = i % NS;
                 ok = pj_wait(bar_ready(st), (uint32_t)(i / NS) & 1u, abort_flag);
                 if (!ok) break;
@@ -334,13 +346,16 @@ act_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
 #pragma unroll
         for (int q = 0; q < 4; ++q) hmax[q] = __float2half2_rn(0.f);
         bool ok = true;
-        for (int i = 0; i < nst; ++i) {
+        // (fine: where the slice has a second turn, it is of what fp16 left of the quotients, and of zeros in the other columns)
+        const int turns = twice() ? 2 * nst : nst;
+        for (int i = 0; i < turns; ++i) {
             const int st = i % NS;
+            const bool rest = FINE && i >= nst;
             ok = pj_warp_wait(bar_full(st), (uint32_t)(i / NS) & 1u, abort_flag, lane);
             if (!ok) break;
             const uint32_t base = sb + st * stage_bytes;
-            const int tag = unit_tag[i * 8 + cw];
-            if (MAXIMA || tag != 0) {
+            const int unit = (rest ? i - nst : i) * 8 + cw, tag = unit_tag[unit];
+            if (MAXIMA || tag != 0 || rest) {
                 uint32_t addr[4], wd[4][4];
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
@@ -353,10 +368,10 @@ act_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
 #pragma unroll
-                    for (int w = 0; w < 4; ++w) zd[q][w] = wd[q][w];
+                    for (int w = 0; w < 4; ++w) zd[q][w] = rest ? 0u : wd[q][w];          // (second turn: what is written back)
                 if (tag != 0) {
                     const float4* sp = (tag != kPUncached) ? reinterpret_cast<const float4*>(s_cache + (tag - 1) * 8)
-                                                           : reinterpret_cast<const float4*>(s + k0 + i * kPCols + cw * 8);
+                                                           : reinterpret_cast<const float4*>(s + k0 + unit * 8);
                     const float4 s0 = sp[0], s1 = sp[1];
                     const float sv[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
                     // Only the columns with a divisor (the same for every lane: lanes are rows) are divided and
@@ -364,23 +379,32 @@ act_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         if (sv[e] != 1.f) {
+                            const Divisor d = kParts ? divisor_parts(sv[e]) : Divisor();
 #pragma unroll
                             for (int q = 0; q < 4; ++q) {
                                 const uint32_t word = wd[q][e >> 1];
                                 const __half hv = __ushort_as_half((unsigned short)((e & 1) ? (word >> 16) : (word & 0xffffu)));
-                                const float f = __fdiv_rn(__half2float(hv), sv[e]);
+                                const float f = kParts ? quotient(__half2float(hv), d) : __fdiv_rn(__half2float(hv), sv[e]);
                                 if (MAXIMA) amax[q] = fmaxf(amax[q], fabsf(f));
-                                const uint32_t hb = (uint32_t)__half_as_ushort(__float2half_rn(FINE ? fminf(fmaxf(f, -65504.f), 65504.f) : f));
+                                const __half hi = __float2half_rn(FINE ? fminf(fmaxf(f, -65504.f), 65504.f) : f);
+                                if (rest) {
+                                    zd[q][e >> 1] |= (uint32_t)__half_as_ushort(__float2half_rn(f - __half2float(hi))) << (16 * (e & 1));
+                                    continue;
+                                }
+                                const uint32_t hb = (uint32_t)__half_as_ushort(hi);
                                 wd[q][e >> 1] = (e & 1) ? ((word & 0x0000ffffu) | (hb << 16)) : ((word & 0xffff0000u) | hb);
                                 zd[q][e >> 1] &= (e & 1) ? 0x0000ffffu : 0xffff0000u;
                             }
                         }
                     }
+                }
+                if (tag != 0 || rest) {
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) pj_sts128(addr[q], make_uint4(wd[q][0], wd[q][1], wd[q][2], wd[q][3]));
+                    for (int q = 0; q < 4; ++q)
+                        pj_sts128(addr[q], rest ? make_uint4(zd[q][0], zd[q][1], zd[q][2], zd[q][3]) : make_uint4(wd[q][0], wd[q][1], wd[q][2], wd[q][3]));
                     fence_proxy_async_smem();       // the MMA reads these through the async proxy
                 }
-                if (MAXIMA) {
+                if (MAXIMA && !rest) {
 #pragma unroll
                     for (int q = 0; q < 4; ++q)
 #pragma unroll
@@ -431,7 +455,7 @@ act_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
                 uint32_t w[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float f = __fdiv_rn(__half2float(__ushort_as_half(v[e])), d[e]);
+                    const float x = __half2float(__ushort_as_half(v[e])), f = kParts ? quotient(x, divisor_parts(d[e])) : __fdiv_rn(x, d[e]);
                     const __half hi = __float2half_rn(fminf(fmaxf(f, -65504.f), 65504.f));
                     w[e >> 1] |= (uint32_t)__half_as_ushort(__float2half_rn(f - __half2float(hi))) << (16 * (e & 1));
                 }
