@@ -521,7 +521,7 @@ int likely_tiles(const AdapterParams& p) { return (p.M + kTok - 1) / kTok + (p.n
 
 // Boxes of `box` rows by 64 columns, 128 bytes a row, of an fp16 matrix.
 int rows_map(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint64_t ld, uint32_t box) {
-    return encode_map_2d_ld(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, base, rows, cols, ld, box, kCols, CU_TENSOR_MAP_SWIZZLE_128B, /*keep=*/false);
+    return encode_map_2d_ld(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, base, rows, cols, ld, box, kCols, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
 template <typename Kernel>

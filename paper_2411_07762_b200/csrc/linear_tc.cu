@@ -977,7 +977,7 @@ int make_map_2d(CUtensorMap* map, CUtensorMapDataType dt, int esize, const void*
 // tokens x 128 bytes, 128-byte swizzle.  In shared memory each block's BT x 128-byte tile is
 // contiguous, which is the K-major operand layout the MMA descriptor expects.
 int make_map_x(CUtensorMap* map, const void* base, uint64_t M, uint64_t K, uint32_t BT, uint32_t KS) {
-    MapKey k = make_key(base, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, CU_TENSOR_MAP_SWIZZLE_128B);
+    MapArgs k = map_args(base, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, CU_TENSOR_MAP_SWIZZLE_128B);
     k.dims[0] = 128; k.dims[1] = M; k.dims[2] = K / 128;
     k.strides[0] = K; k.strides[1] = 128;
     k.box[0] = 128; k.box[1] = BT; k.box[2] = KS;

