@@ -215,7 +215,13 @@ int launch_small(const __half* X, const float* s, const __half* LA, int M, int K
     const int tok = (M > 2 && ctas(4) >= 128) ? 4 : (M > 1 && ctas(2) >= 128) ? 2 : 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(M + ctas(tok), 1, 1);
-    cfg.blockDim = dim3(tok == 4 ? PT : TH, 1, 1);
+    // The wider CTAs only while each has an SM of its own (of 1024 / 512 threads, us: 24 x 14336, rank 32, 7.7 / 6.3; 9 x 14336, rank 64, 7.5 / 6.3;
+    // 8 x 14336, rank 64, 5.3 / 6.3).  T has the same bits either way: the same threads make it.
+    int num_sms = 0;
+    const int rc = device_sm_count(&num_sms);
+    if (rc != ASER_OK) return rc;
+    const bool narrow = TH != PT && (tok == 4 || M + ctas(tok) > num_sms);
+    cfg.blockDim = dim3(narrow ? PT : TH, 1, 1);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -223,7 +229,10 @@ int launch_small(const __half* X, const float* s, const __half* LA, int M, int K
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     cudaError_t e;
-    if (tok == 4) e = cudaLaunchKernelEx(&cfg, quant_act_small_kernel<PT, PT, CPT * (TH / PT), 4>, X, s, LA, M, K, r, Xq, a_scale, T, ldt, lo_off, qmax);
+    constexpr int kNarrow = CPT * (TH / PT);        // chunks of a thread of PT
+    if (tok == 4) e = cudaLaunchKernelEx(&cfg, quant_act_small_kernel<PT, PT, kNarrow, 4>, X, s, LA, M, K, r, Xq, a_scale, T, ldt, lo_off, qmax);
+    else if (narrow && tok == 2) e = cudaLaunchKernelEx(&cfg, quant_act_small_kernel<PT, PT, kNarrow, 2>, X, s, LA, M, K, r, Xq, a_scale, T, ldt, lo_off, qmax);
+    else if (narrow) e = cudaLaunchKernelEx(&cfg, quant_act_small_kernel<PT, PT, kNarrow, 1>, X, s, LA, M, K, r, Xq, a_scale, T, ldt, lo_off, qmax);
     else if (tok == 2) e = cudaLaunchKernelEx(&cfg, quant_act_small_kernel<TH, PT, CPT, 2>, X, s, LA, M, K, r, Xq, a_scale, T, ldt, lo_off, qmax);
     else e = cudaLaunchKernelEx(&cfg, quant_act_small_kernel<TH, PT, CPT, 1>, X, s, LA, M, K, r, Xq, a_scale, T, ldt, lo_off, qmax);
     if (e != cudaSuccess) return record_cuda_error(e, "quant_act_small_kernel");
