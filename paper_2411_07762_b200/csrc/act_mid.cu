@@ -9,8 +9,13 @@
 //    an inner product does not care about the order of k, so a thread's k positions are the 8 columns that one 16-byte
 //    load brings, the same for X and L_A, and neither goes through shared memory.  X is divided where the divisor is
 //    not 1 (fp32), and the quotient multiplied as the sum of two fp16 numbers: rounded to one, 2 % of T's bf16 values came out a
-//    step off, and in a feed-forward block a step of T moves codes of H (a few tokens' outputs by 2 %).  The warps' sums meet in shared memory, the CTAs' in distributed
-//    shared memory, both in a fixed order; the order depends on K alone, not on the number of tokens.
+//    step off, and in a feed-forward block a step of T moves codes of H (a few tokens' outputs by 2 %).  Code that runs once is bound by
+//    the fetching of its instructions: pairs of columns are divided by a few (double-length reciprocals, and the second numbers by an mma of
+//    eight columns), without divisors there is an instance of its own (96 x 8192, rank 128, 1 % of the columns / all of them divided / no divisors, us:
+//    8.0 / 12.0 / 6.3; with a division and two mma of sixteen columns for each column 8.4 / 19.2 / 7.1).  The warps' sums meet in shared memory,
+//    the CTAs' in distributed shared memory, both in a fixed order; the order depends on K alone, not on the number of tokens.
+#include <type_traits>
+
 #include "act_math.cuh"
 #include "aser_common.cuh"
 #include "sm100_ptx.cuh"
@@ -30,10 +35,76 @@ __device__ __forceinline__ void mid_mma(float (&d)[4], uint32_t a0, uint32_t a1,
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
+// (eight columns of k: a word of a token against a word of L_A)
+__device__ __forceinline__ void mid_mma8(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t b0) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k8.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5}, {%6}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(b0));
+}
+
+// 32 columns of 32 tokens and of 32 rows of L_A, a thread's share: 8 columns of the tokens and rows g + 8 i.
+template <bool DIV>
+struct MidUnit {
+    uint32_t x[4][4];
+    uint4 l[4];
+    unsigned tags = 0;                       // pairs of columns with a divisor
+
+    __device__ __forceinline__ void load(const __half* xp, const __half* lp, const float* s, int K, int c, int t, const bool (&x_ok)[4], const bool (&l_ok)[4]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint4 v = x_ok[i] ? *reinterpret_cast<const uint4*>(xp + 8 * i * K + c) : make_uint4(0, 0, 0, 0);
+            x[i][0] = v.x; x[i][1] = v.y; x[i][2] = v.z; x[i][3] = v.w;
+            l[i] = l_ok[i] ? __ldg(reinterpret_cast<const uint4*>(lp + 8 * i * K + c)) : make_uint4(0, 0, 0, 0);
+        }
+        if (DIV) {
+            const float4 a = __ldg(reinterpret_cast<const float4*>(s + c + t * 8)), b = __ldg(reinterpret_cast<const float4*>(s + c + t * 8) + 1);
+            tags = (a.x != 1.f || a.y != 1.f ? 1u : 0u) | (a.z != 1.f || a.w != 1.f ? 2u : 0u) |
+                   (b.x != 1.f || b.y != 1.f ? 4u : 0u) | (b.z != 1.f || b.w != 1.f ? 8u : 0u);
+        }
+    }
+    // all: pairs where any lane has a divisor (the others divide by 1).
+    __device__ __forceinline__ void multiply(float (&acc)[2][4][4], const float* sp, unsigned all) {
+#pragma unroll
+        for (int w = 0; DIV && w < 4; ++w) {
+            if (!(all >> w & 1)) continue;
+            const float2 d = __ldg(reinterpret_cast<const float2*>(sp) + w);         // (again: eight registers fewer all along)
+            const Divisor d0 = divisor_parts(d.x), d1 = divisor_parts(d.y);
+            const float2 first = make_float2(d0.first, d1.first), second = make_float2(d0.second, d1.second);
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt) {
+                uint32_t lo[2];              // what fp16 leaves of the quotients
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    uint32_t& word = x[2 * mt + i][w];
+                    const float2 x2 = __half22float2(*reinterpret_cast<const __half2*>(&word));
+                    const float2 q = __ffma2_rn(x2, first, __fmul2_rn(x2, second));
+                    const __half2 hi = __hmin2(__hmax2(__floats2half2_rn(q.x, q.y), __float2half2_rn(-65504.f)), __float2half2_rn(65504.f));
+                    const float2 h = __half22float2(hi);
+                    const __half2 rest = __floats2half2_rn(q.x - h.x, q.y - h.y);
+                    word = *reinterpret_cast<const uint32_t*>(&hi);
+                    lo[i] = *reinterpret_cast<const uint32_t*>(&rest);
+                }
+#pragma unroll
+                for (int nt = 0; nt < 4; ++nt)
+                    mid_mma8(acc[mt][nt], lo[0], lo[1], w == 0 ? l[nt].x : w == 1 ? l[nt].y : w == 2 ? l[nt].z : l[nt].w);
+            }
+        }
+#pragma unroll
+        for (int nt = 0; nt < 4; ++nt)
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt) {
+                mid_mma(acc[mt][nt], x[2 * mt][0], x[2 * mt + 1][0], x[2 * mt][1], x[2 * mt + 1][1], l[nt].x, l[nt].y);
+                mid_mma(acc[mt][nt], x[2 * mt][2], x[2 * mt + 1][2], x[2 * mt][3], x[2 * mt + 1][3], l[nt].z, l[nt].w);
+            }
+    }
+};
+
 // Grid: t_tiles * CL projecting CTAs (clusters of CL along K), then the quantizing CTAs, R rows each.
 // A sum (register 4 (4 mt + nt) + e of lane 4 g + t) is token 16 mt + g + 8 (e / 2), L_A row 8 nt + 2 t + e % 2.
 // TH threads: 256, or 512 for rows that would fill a thread's registers; the projection takes eight warps of them either way.
-template <int CPT, int R, int TH = kMThreads>
+// DIV: there are divisors.
+template <bool DIV, int CPT, int R, int TH = kMThreads>
 __global__ void __launch_bounds__(TH, 512 / TH)
 quant_act_mid_kernel(const __half* __restrict__ X, const float* __restrict__ s, const __half* __restrict__ LA, int M, int K,
                      int r, int t_tiles, int CL, int8_t* __restrict__ Xq, float* __restrict__ a_scale,
@@ -49,7 +120,7 @@ quant_act_mid_kernel(const __half* __restrict__ X, const float* __restrict__ s, 
     if ((int)blockIdx.x >= t_tiles * CL) {
         const int row0 = ((int)blockIdx.x - t_tiles * CL) * R, nrows = M - row0 < R ? M - row0 : R;
         if (nrows > 0)
-            quantize_rows<CPT, R>(X + (size_t)row0 * K, s, nrows, K, Xq + (size_t)row0 * K, a_scale + row0, qmax, sh.rows);
+            quantize_rows<CPT, R>(X + (size_t)row0 * K, DIV ? s : nullptr, nrows, K, Xq + (size_t)row0 * K, a_scale + row0, qmax, sh.rows);
         return;         // clusters take one role or the other, so no peer waits for this CTA
     }
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
@@ -71,67 +142,12 @@ quant_act_mid_kernel(const __half* __restrict__ X, const float* __restrict__ s, 
         l_ok[i] = j0 + g + 8 * i < r;
     }
     for (int u = warp < kMWarps ? rank * kMWarps + warp : K; u < K / 64; u += CL * kMWarps) {
-        uint4 xv[2][4], lv[2][4];
-        float4 s0[2], s1[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int c = u * 64 + h * 32;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                xv[h][i] = x_ok[i] ? *reinterpret_cast<const uint4*>(xp + 8 * i * K + c) : make_uint4(0, 0, 0, 0);
-                lv[h][i] = l_ok[i] ? __ldg(reinterpret_cast<const uint4*>(lp + 8 * i * K + c)) : make_uint4(0, 0, 0, 0);
-            }
-            s0[h] = s1[h] = make_float4(1.f, 1.f, 1.f, 1.f);
-            if (s) {
-                s0[h] = __ldg(reinterpret_cast<const float4*>(s + c + t * 8));
-                s1[h] = __ldg(reinterpret_cast<const float4*>(s + c + t * 8) + 1);
-            }
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const float sv[8] = {s0[h].x, s0[h].y, s0[h].z, s0[h].w, s1[h].x, s1[h].y, s1[h].z, s1[h].w};
-            uint32_t xw[4][4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) { xw[i][0] = xv[h][i].x; xw[i][1] = xv[h][i].y; xw[i][2] = xv[h][i].z; xw[i][3] = xv[h][i].w; }
-            unsigned tags = 0;               // columns where a lane has a divisor
-#pragma unroll
-            for (int e = 0; e < 8; ++e) tags |= sv[e] != 1.f ? 1u << e : 0u;
-            tags = __reduce_or_sync(0xffffffffu, tags);
-            if (tags) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    if (!(tags >> e & 1)) continue;
-                    uint32_t lo[4];          // what fp16 leaves of the quotients, multiplied at once: in the place of its word, zeros beside it
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t word = xw[i][e >> 1];
-                        const __half hv = __ushort_as_half((unsigned short)((e & 1) ? (word >> 16) : (word & 0xffffu)));
-                        const float q = __fdiv_rn(__half2float(hv), sv[e]);
-                        const __half hi = __float2half_rn(fminf(fmaxf(q, -65504.f), 65504.f));
-                        const uint32_t hb = (uint32_t)__half_as_ushort(hi), lb = (uint32_t)__half_as_ushort(__float2half_rn(q - __half2float(hi)));
-                        xw[i][e >> 1] = (e & 1) ? ((word & 0x0000ffffu) | (hb << 16)) : ((word & 0xffff0000u) | hb);
-                        lo[i] = (e & 1) ? lb << 16 : lb;
-                    }
-#pragma unroll
-                    for (int nt = 0; nt < 4; ++nt) {
-                        const uint32_t l0 = e < 4 ? lv[h][nt].x : lv[h][nt].z, l1 = e < 4 ? lv[h][nt].y : lv[h][nt].w;
-#pragma unroll
-                        for (int mt = 0; mt < 2; ++mt)
-                            if (e & 2) mid_mma(acc[mt][nt], 0u, 0u, lo[2 * mt], lo[2 * mt + 1], l0, l1);
-                            else mid_mma(acc[mt][nt], lo[2 * mt], lo[2 * mt + 1], 0u, 0u, l0, l1);
-                    }
-                }
-            }
-#pragma unroll
-            for (int nt = 0; nt < 4; ++nt) {
-                const uint4 l = lv[h][nt];
-#pragma unroll
-                for (int mt = 0; mt < 2; ++mt) {
-                    mid_mma(acc[mt][nt], xw[2 * mt][0], xw[2 * mt + 1][0], xw[2 * mt][1], xw[2 * mt + 1][1], l.x, l.y);
-                    mid_mma(acc[mt][nt], xw[2 * mt][2], xw[2 * mt + 1][2], xw[2 * mt][3], xw[2 * mt + 1][3], l.z, l.w);
-                }
-            }
-        }
+        MidUnit<DIV> now, next;
+        now.load(xp, lp, s, K, u * 64, t, x_ok, l_ok);
+        next.load(xp, lp, s, K, u * 64 + 32, t, x_ok, l_ok);
+        const unsigned all = DIV ? __reduce_or_sync(0xffffffffu, now.tags | next.tags << 4) : 0u;
+        now.multiply(acc, s + u * 64 + t * 8, all);
+        next.multiply(acc, s + u * 64 + 32 + t * 8, all >> 4);
     }
     if (warp < kMWarps) {
 #pragma unroll
@@ -200,11 +216,12 @@ int mid_rows(int M, int K) { return K > 8192 || M <= 128 ? 1 : M > 512 && K <= 2
 }  // namespace
 
 // The CTAs of this kernel are short and two are resident on an SM; the cluster kernel's step hardly depends on the
-// number of tokens until its clusters no longer fit at once.  Measured, this kernel | the cluster kernel, us: rank 32: 64 x 4096 4.5 |
-// 9.7, 448 x 4096 (336 CTAs) 9.2 | 10.2, 101 x 8192 7.7 | 12.7, 333 x 8192 (254) 9.0 | 13.1, rank 64: 333 x 4096 (343) 10.2 | 11.2, 400 x 4096 (408) 11.1 | 11.2, 350 x 5120 (351) 13.0 | 16.0, 448 x 8192 (336) 14.3 | 13.0, 333 x 14336
-// (421) 17.5 | 17.8; rank 128: 200 x 4096 (324) 10.0 | 10.8, 333 x 4096 (518) 12.2 | 10.9, 200 x 8192 (324) 14.1 | 16.1, 333 x 8192 (518)
-// 17.0 | 16.4, 200 x 14336 (424) 19.2 | 23.3; short rows: 1000 x 1024, rank 128 (506, four rows each) 10.0 | 10.1, rank 32 (314) 7.2 |
-// 9.5, 448 x 2048, rank 128 (448) 9.0 | 9.6, 1000 x 3072, rank 32 (628) 12.1 | 15.0, rank 128 (1012) 21.1 | 17.7.
+// number of tokens until its clusters no longer fit at once.  Measured with 1 % of the columns divided, this kernel (its CTAs) | the cluster kernel, us:
+// rank 32: 64 x 4096 (80) 4.4 | 9.9, 448 x 4096 (336) 9.4 | 10.8, 101 x 8192 (133) 7.2 | 13.0, 333 x 8192 (255) 9.4 | 13.7, 448 x 8192 (336) 14.1 |
+// 13.6, 333 x 14336 (421) 17.6 | 18.2; rank 64: 64 x 4096 (96) 4.5 | 10.1, 333 x 4096 (343) 9.8 | 11.2, 384 x 4096 (384) 10.9 | 10.8, 350 x 5120 (351)
+// 12.6 | 18.4; rank 128: 200 x 4096 (324) 10.2 | 11.3, 333 x 4096 (519) 11.4 | 11.5, 200 x 8192 (324) 14.7 | 16.5, 333 x 8192 (519) 16.8 | 16.7,
+// 200 x 14336 (424) 20.2 | 22.8; short rows: 1000 x 1024, rank 128 (506, four rows each) 10.8 | 10.7, rank 32 (314) 7.9 | 9.9, 448 x 2048,
+// rank 128 (448) 9.4 | 9.8, 1000 x 2560, rank 32 (628) 12.6 | 15.6, rank 128 (1012) 17.2 | 17.1.
 bool quant_act_mid_prefers(int M, int K, int r) {
     const int rows = mid_rows(M, K);
     const int ctas = (M + rows - 1) / rows + mid_cluster(K) * ((M + kMTok - 1) / kMTok) * ((r + kMRank - 1) / kMRank);
@@ -216,12 +233,16 @@ int launch_quant_act_mid(const __half* X, const float* s, const __half* LA, int 
     // chunks of eight columns per thread by the row length, one, two or four rows per quantizing CTA
     const int chunks = (K / 8 + kMThreads - 1) / kMThreads, rows = mid_rows(M, K);
     auto go = [&](auto* kernel, int threads = kMThreads) { return launch_mid_cfg(kernel, threads, rows, X, s, LA, M, K, r, Xq, a_scale, T, ldt, lo_off, qmax, st); };
-    if (rows == 4) return go(quant_act_mid_kernel<1, 4>);        // up to 2048 columns
-    if (chunks <= 1) return rows == 2 ? go(quant_act_mid_kernel<1, 2>) : go(quant_act_mid_kernel<1, 1>);
-    if (chunks <= 2) return rows == 2 ? go(quant_act_mid_kernel<2, 2>) : go(quant_act_mid_kernel<2, 1>);
-    if (chunks <= 4) return rows == 2 ? go(quant_act_mid_kernel<4, 2>) : go(quant_act_mid_kernel<4, 1>);
-    if (chunks <= 8) return go(quant_act_mid_kernel<8, 1>);
-    return go(quant_act_mid_kernel<8, 1, 512>, 512);
+    auto pick = [&](auto div) {
+        constexpr bool DIV = decltype(div)::value;
+        if (rows == 4) return go(quant_act_mid_kernel<DIV, 1, 4>);        // up to 2048 columns
+        if (chunks <= 1) return rows == 2 ? go(quant_act_mid_kernel<DIV, 1, 2>) : go(quant_act_mid_kernel<DIV, 1, 1>);
+        if (chunks <= 2) return rows == 2 ? go(quant_act_mid_kernel<DIV, 2, 2>) : go(quant_act_mid_kernel<DIV, 2, 1>);
+        if (chunks <= 4) return rows == 2 ? go(quant_act_mid_kernel<DIV, 4, 2>) : go(quant_act_mid_kernel<DIV, 4, 1>);
+        if (chunks <= 8) return go(quant_act_mid_kernel<DIV, 8, 1>);
+        return go(quant_act_mid_kernel<DIV, 8, 1, 512>, 512);
+    };
+    return s ? pick(std::true_type()) : pick(std::false_type());
 }
 
 }  // namespace aser
