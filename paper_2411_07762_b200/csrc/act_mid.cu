@@ -222,10 +222,15 @@ int mid_rows(int M, int K) { return K > 8192 || M <= 128 ? 1 : M > 512 && K <= 2
 // 12.6 | 18.4; rank 128: 200 x 4096 (324) 10.2 | 11.3, 333 x 4096 (519) 11.4 | 11.5, 200 x 8192 (324) 14.7 | 16.5, 333 x 8192 (519) 16.8 | 16.7,
 // 200 x 14336 (424) 20.2 | 22.8; short rows: 1000 x 1024, rank 128 (506, four rows each) 10.8 | 10.7, rank 32 (314) 7.9 | 9.9, 448 x 2048,
 // rank 128 (448) 9.4 | 9.8, 1000 x 2560, rank 32 (628) 12.6 | 15.6, rank 128 (1012) 17.2 | 17.1.
-bool quant_act_mid_prefers(int M, int K, int r) {
+// two_kernels: the alternative is the step of two kernels, as in a forward pass.  Between 341 and 400 CTAs at 4096 to 5120 columns it is then faster at
+// high ranks and without a projection, where rows do not have 4096 columns (105 points; a pass, this kernel | two kernels, us: 4608 columns:
+// 225 tokens, rank 128, 25.1 | 22.7, 449, rank 16, 24.5 | 25.8, 681 without 31.3 | 28.4; 5120: 256, rank 128, 26.3 | 23.6, 343, rank 64, 26.1 | 26.5, 700
+// without 33.2 | 30.4; 4096: 225, rank 128, 22.1 | 23.2, 343, rank 64, 22.3 | 23.6, 771 without 29.0 | 28.3).
+bool quant_act_mid_prefers(int M, int K, int r, bool two_kernels) {
     const int rows = mid_rows(M, K);
     const int ctas = (M + rows - 1) / rows + mid_cluster(K) * ((M + kMTok - 1) / kMTok) * ((r + kMRank - 1) / kMRank);
-    return ctas <= (rows == 4 ? 450 : K < 4096 ? 630 : K <= 5120 ? 400 : K <= 8192 ? 340 : 424);
+    const bool high = two_kernels && (r == 0 || (r > 64 && K > 4096));
+    return ctas <= (rows == 4 ? 450 : K < 4096 ? 630 : K <= 5120 && !high ? 400 : K <= 8192 ? 340 : 424);
 }
 
 int launch_quant_act_mid(const __half* X, const float* s, const __half* LA, int M, int K, int r, int8_t* Xq, float* a_scale,

@@ -225,7 +225,7 @@ bool act_shape_ok(int M, int K, int r) {
 bool forward_act_uses_scratch(int M, int K, int r) {
     if (M <= 32) return false;
     if (r > 128) return true;
-    if (quant_act_mid_prefers(M, K, r)) return false;
+    if (quant_act_mid_prefers(M, K, r, /*two_kernels=*/true)) return false;
     if (K <= 1024) return M > 4096;
     return K / 128 % 16 != 0 || M > (K < 4096 ? 1023 : 448);
 }
@@ -240,7 +240,7 @@ int quant_with_workspace(const void* X_f16, const float* s, const void* LA_f16, 
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     // fine: the one-launch kernel for many tokens rounds the quotients, so only the other two are left
     fine = fine && r > 0 && s != nullptr;
-    const bool scratch = fine ? M > 32 && !(r <= 128 && quant_act_mid_prefers(M, K, r)) : forward_act_uses_scratch(M_pass, K, r);
+    const bool scratch = fine ? M > 32 && !(r <= 128 && quant_act_mid_prefers(M, K, r, /*two_kernels=*/true)) : forward_act_uses_scratch(M_pass, K, r);
     if (!scratch)
         return launch_quant_act(static_cast<const __half*>(X_f16), s, static_cast<const __half*>(LA_f16), M, K, r,
                                 Xq, a_scale, static_cast<__nv_bfloat16*>(T_bf16), st, act_bits, t_pair, M_pass);
