@@ -3,26 +3,26 @@
 //
 // With so few tokens the layer is a stream of packed weights through HBM (4 M operations per
 // byte) and what matters is how many bytes are in flight and how short the dependent chain of a
-// CTA is, not the tensor-core rate.  So this kernel has no shared-memory pipeline, no
-// barriers and no cross-CTA reduction:
-//   * a CTA owns 16 or 32 output channels for the WHOLE of K, its eight warps take every eighth
-//     128-column block; the only exchange is one shared-memory sum over the eight warps;
-//   * every thread keeps 128 bytes of packed weights in flight as 8-byte loads into registers
+// CTA is, not the tensor-core rate.  So this kernel has no shared-memory pipeline, and no more exchange between threads than it must:
+//   * in the plain form a CTA of eight warps owns 16 or 32 output channels for the whole of K, its warps take every eighth
+//     128-column block, and the only exchange is one shared-memory sum over the warps.  With more tiles than CTAs are resident a CTA takes
+//     several, and asks for the next one's first weights while it finishes the sums of this one (28672 x 4096, one token 14.7 -> 13.7 us).
+//     Long rows are split over clusters of two to four CTAs of four warps: they send their sums to the cluster's first CTA, which finishes the
+//     tile (launch_nt has the rules);
+//   * every thread keeps 128 bytes of packed weights in flight as loads into registers
 //     (issued before anything else, refilled as they are consumed).  What bounds the kernel beside HBM is the
 //     number of lines that the lanes of a load touch in L1, half a warp at a time: a thread takes 16 neighbouring columns
-//     of either half of a block (two lines per half warp; its activations are then 16 contiguous bytes twice, 64 a row),
+//     of either half of a block by 8-byte loads (two lines per half warp; its activations are then 16 contiguous bytes twice, 64 a row),
 //     not the 32 of one sub-block (16-byte loads, four lines per quarter warp: 16 cycles for 512 bytes instead of 8, L1 83 %
-//     busy; 28672 x 4096, 8 / 16 tokens 15.4 / 20.6 -> 13.6 / 17.8 us, 14336 x 4096 9.4 / 12.2 -> 8.0 / 10.5, 4096 x 4096, one token 5.2 ->
-//     4.7);  A per-thread cp.async ring in shared memory (twice the bytes in flight) was
-//     measured 20-50 % slower: the shared memory it takes is L1 capacity that the activation
+//     busy; 28672 x 4096, 8 / 16 tokens 15.4 / 20.6 -> 13.6 / 17.8 us, 14336 x 4096 9.4 / 12.2 -> 8.0 / 10.5).  Where a warp has a block or two the
+//     chain counts, and the fewer loads are the faster ones (launch_cfg has the rule).  A per-thread cp.async ring in shared memory (twice the
+//     bytes in flight) was measured 20-50 % slower: the shared memory it takes is L1 capacity that the activation
 //     fragments then miss;
 //   * the packed word is turned into two int8x4 registers (16 * q) by two logic operations and
 //     fed to mma.sync m16n8k32 (weights on the 16-row side, tokens on the 8-column side).  An
 //     integer dot product does not care about the order of k, so a thread's k positions are
 //     simply the 32 columns it loaded; the activation fragment reads the same 32 columns of
 //     its token's row of Xq (served by L1/L2: Xq is at most 16 x K bytes);
-//   * more tiles than CTAs are resident: a CTA takes several, and asks for the next one's first weights while it finishes
-//     the sums of this one (28672 x 4096, one token 14.7 -> 13.7 us);
 //   * the low-rank term is a (16 or 32) x M x r product per CTA: warp w takes the 16-wide slices
 //     w and w + 8 of r on mma.sync m16n8k16 (L_B rows from global memory, T converted bf16 ->
 //     fp16 in registers); its few loads are issued right behind the first weight loads and it is
@@ -46,9 +46,15 @@ constexpr int kDecThreads = kDecWarps * 32;
 // low-rank term's slices w and w + 8 by warp w of the cluster's first eight.
 constexpr int kSplitThreads = 128, kSplitCtas = 7;
 
-// A row's 32 columns of a thread: 8 bytes of a block's first half (words 2 (t & 1) and + 1 of sub-block t / 2) and 8 of its second.
-__device__ __forceinline__ uint4 ld_stream16(const uint8_t* p) {
+// A row's 32 columns of a thread.  WIDE: the 16 bytes of sub-block t.  Else 8 bytes of a block's first half (words 2 (t & 1) and + 1 of
+// sub-block t / 2) and 8 of its second.
+template <bool WIDE>
+__device__ __forceinline__ uint4 ld_row(const uint8_t* p) {
     uint4 v;
+    if constexpr (WIDE) {
+        asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+        return v;
+    }
     asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
     asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(v.z), "=r"(v.w) : "l"(p + 2 * kWkRows * 16));
     return v;
@@ -100,7 +106,7 @@ struct DecCfg {
 // GLU: the channels are gate and up in turn, a lane of an even channel stores the product with its neighbour's (no dump).
 // STREAM: more tiles than CTAs are resident; a CTA takes every gridDim.x-th tile, and its weights keep coming from one tile to the next.
 // CL > 1: a cluster of CTAs of four warps shares a tile's K.  Its first CTA gets the others' sums and finishes the tile.
-template <int NT, int R, int B, bool GROUP, bool GLU, bool STREAM, int CL = 1>
+template <int NT, int R, int B, bool GROUP, bool GLU, bool STREAM, int CL = 1, bool WIDE = false>
 __global__ void __launch_bounds__(CL > 1 ? kSplitThreads : kDecThreads, CL > 1 ? kSplitCtas : DecCfg<NT, R, B>::MinCtas)
 linear_decode_kernel(const int8_t* Xq, const float* a_scale, const __nv_bfloat16* T, int M, int K, int ldt,
                      int32_t* __restrict__ acc_debug, const CatSplit cat, const __grid_constant__ LinearGroup group, const GluForm glu, int tiles) {
@@ -129,11 +135,11 @@ linear_decode_kernel(const int8_t* Xq, const float* a_scale, const __nv_bfloat16
         }
         n0 = (tile - first) * C::Rows;
     };
-    // Rows n0 + 16 rt + g and + 8, columns 16 t .. 16 t + 15 of either half of a block.  The
+    // Rows n0 + 16 rt + g and + 8, columns 16 t .. 16 t + 15 of either half of a block (WIDE: 32 t .. 32 t + 31).  The
     // blocked layout pads the last 128-row tile with zero codes, so rows past N inside that tile
     // read as zeros; a CTA never reaches past the tile (16 R divides 128).
     auto weights = [&](int layer, int n0) {
-        return group.Wk[layer] + ((size_t)(n0 >> 7) * KB) * kWkBlockBytes + (t >> 1) * (kWkRows * 16) + ((n0 & 127) + g) * 16 + (t & 1) * 8;
+        return group.Wk[layer] + ((size_t)(n0 >> 7) * KB) * kWkBlockBytes + (WIDE ? t * (kWkRows * 16) : (t >> 1) * (kWkRows * 16) + (t & 1) * 8) + ((n0 & 127) + g) * 16;
     };
     int layer, n0;
     find(first_tile, layer, n0);
@@ -146,8 +152,8 @@ linear_decode_kernel(const int8_t* Xq, const float* a_scale, const __nv_bfloat16
         if (kbi < KB) {
 #pragma unroll
             for (int rt = 0; rt < R; ++rt) {
-                wa[i][rt][0] = ld_stream16(wbase + (size_t)kbi * kWkBlockBytes + rt * 256);
-                wa[i][rt][1] = ld_stream16(wbase + (size_t)kbi * kWkBlockBytes + rt * 256 + 128);
+                wa[i][rt][0] = ld_row<WIDE>(wbase + (size_t)kbi * kWkBlockBytes + rt * 256);
+                wa[i][rt][1] = ld_row<WIDE>(wbase + (size_t)kbi * kWkBlockBytes + rt * 256 + 128);
             }
         }
     }
@@ -236,7 +242,7 @@ linear_decode_kernel(const int8_t* Xq, const float* a_scale, const __nv_bfloat16
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         x_ok[nt] = g + 8 * nt < M;
-        xrow[nt] = Xq + (size_t)(x_ok[nt] ? g + 8 * nt : 0) * K + t * 16;
+        xrow[nt] = Xq + (size_t)(x_ok[nt] ? g + 8 * nt : 0) * K + t * (WIDE ? 32 : 16);
     }
     for (int kb0 = warp; kb0 < KB; kb0 += kAll * BATCH) {
 #pragma unroll
@@ -250,7 +256,7 @@ linear_decode_kernel(const int8_t* Xq, const float* a_scale, const __nv_bfloat16
                     if (x_ok[nt]) {
                         const uint4* xp = reinterpret_cast<const uint4*>(xrow[nt] + kbi * kWkCols);
                         lo = xp[0];
-                        hi = xp[4];
+                        hi = xp[WIDE ? 1 : 4];
                     }
                     b[nt][0] = lo.x; b[nt][1] = lo.y; b[nt][2] = lo.z; b[nt][3] = lo.w;
                     b[nt][4] = hi.x; b[nt][5] = hi.y; b[nt][6] = hi.z; b[nt][7] = hi.w;
@@ -270,11 +276,11 @@ linear_decode_kernel(const int8_t* Xq, const float* a_scale, const __nv_bfloat16
                             mma_s8_16x8x32(c[rt][nt], a0, a1, a2, a3, b[nt][2 * j], b[nt][2 * j + 1]);
                     }
                     if (kbn < KB) {
-                        wa[i][rt][0] = ld_stream16(wbase + (size_t)kbn * kWkBlockBytes + rt * 256);
-                        wa[i][rt][1] = ld_stream16(wbase + (size_t)kbn * kWkBlockBytes + rt * 256 + 128);
+                        wa[i][rt][0] = ld_row<WIDE>(wbase + (size_t)kbn * kWkBlockBytes + rt * 256);
+                        wa[i][rt][1] = ld_row<WIDE>(wbase + (size_t)kbn * kWkBlockBytes + rt * 256 + 128);
                     } else if (STREAM && wnext) {
-                        wa[i][rt][0] = ld_stream16(wnext + (size_t)(warp + i * kAll) * kWkBlockBytes + rt * 256);
-                        wa[i][rt][1] = ld_stream16(wnext + (size_t)(warp + i * kAll) * kWkBlockBytes + rt * 256 + 128);
+                        wa[i][rt][0] = ld_row<WIDE>(wnext + (size_t)(warp + i * kAll) * kWkBlockBytes + rt * 256);
+                        wa[i][rt][1] = ld_row<WIDE>(wnext + (size_t)(warp + i * kAll) * kWkBlockBytes + rt * 256 + 128);
                     }
                 }
             }
@@ -377,8 +383,20 @@ int launch_cfg(const int8_t* Xq, const float* a_scale, const __nv_bfloat16* T, i
     // One layer of 9 to 16 tokens and few rows has an instance without the search for the layer, which the compiler makes
     // faster (alone / as a group of one, us: 12 x 4096 x 14336 9.6 / 10.5, 16 x 4096 x 14336 11.0 / 11.7); for the others the opposite
     // holds (1 x 4096 x 14336 8.9 / 8.2, 16 x 8192 x 8192 11.2 / 10.9, 8 x 8192 x 8192 8.9 / 8.7).
+    // 16-row tiles with 16-byte weight loads where a warp has one or two blocks, and for 9 to 12 tokens or little of a low-rank term (a pass on 336
+    // points, 16-byte / two 8-byte loads, us: 16 x 4096 x 4096, rank 0, 7.1 / 7.8, rank 64 8.5 / 8.3, rank 128 9.6 / 9.0; 12 x 4096 x 4096, rank 128, 8.8 /
+    // 9.1; 9 x 1024 x 4096, rank 32, 7.3 / 7.8; 16 x 2048 x 2048, rank 64, 5.9 / 6.1; 8 x 7168 x 4096, rank 128, 0.6 more, rank 0 0.3 less).
+    int top = 0;
+    for (int l = 0; l < group.layers; ++l) top = group.r[l] > top ? group.r[l] : top;
+    const bool wide = R == 1 && (K <= 2048 || (NT == 2 && (M <= 12 || top <= 16)));
     cudaError_t e;
-    if (tiles > resident)
+    if (wide && tiles <= resident) {
+        constexpr bool kWide = R == 1;
+        if (NT == 2 && group.layers == 1)
+            e = cudaLaunchKernelEx(&cfg, linear_decode_kernel<NT, R, B, NT != 2 || R != 1, GLU, false, 1, kWide>, Xq, a_scale, T, M, K, ldt, acc_debug, cat, group, glu, tiles);
+        else
+            e = cudaLaunchKernelEx(&cfg, linear_decode_kernel<NT, R, B, true, GLU, false, 1, kWide>, Xq, a_scale, T, M, K, ldt, acc_debug, cat, group, glu, tiles);
+    } else if (tiles > resident)
         e = cudaLaunchKernelEx(&cfg, linear_decode_kernel<NT, R, B, true, GLU, true>, Xq, a_scale, T, M, K, ldt, acc_debug, cat, group, glu, tiles);
     else if (NT == 2 && R == 1 && group.layers == 1)
         e = cudaLaunchKernelEx(&cfg, linear_decode_kernel<NT, R, B, NT != 2 || R != 1, GLU, false>, Xq, a_scale, T, M, K, ldt, acc_debug, cat, group, glu, tiles);
