@@ -319,15 +319,16 @@ int aser_forward_ffn(const void* X_f16, const float* s, const void* LA_f16, cons
  * n_slots) bytes (0 for bad sizes), contents irrelevant.
  *
  * aser_adapters_add -- the update above.  Y [M, N] and out [M, N] may be one matrix (in place: rows without an adapter are then
- * not touched; else they are copied); other overlaps of out with Y, X or the adapters are not allowed.  ldx, ldy, ldo: elements between rows,
+ * not touched; else they are copied); other overlaps of out with Y or X are refused (ASER_ERR_SHAPE; column ranges of one matrix beside each
+ * other are none), those with the adapters not allowed.  ldx, ldy, ldo: elements between rows,
  * multiples of 8 (0: K, N, N), so a projection of a fused group is a column range.  plan must be one of these M and
  * n_slots, made by work that precedes the call on `stream` (a plan of other sizes makes the call write nothing).  Where
  * there are many tokens to an adapter the call is two launches with a workspace between them, of aser_adapters_workspace_bytes(M, N, K,
  * r, n_slots) bytes, contents irrelevant (else one launch and 0 bytes: workspace may be NULL); calls that overlap in time need one
  * each.
  *
- * aser_forward_adapters -- aser_forward, then the adapters of its tokens added to Y in place, enqueued together.  All
- * arguments are checked before anything is.  adapter_workspace: that of aser_adapters_add, apart from the layer's own.
+ * aser_forward_adapters -- aser_forward, then the adapters of its tokens added to Y in place, enqueued together.  Y may not overlap X,
+ * which is read twice.  All arguments are checked before anything is enqueued.  adapter_workspace: that of aser_adapters_add, apart from the layer's own.
  */
 size_t aser_adapters_plan_bytes(int M, int n_slots);
 int aser_adapters_plan(const int32_t* slot, int M, int n_slots, void* plan, size_t plan_bytes, void* stream);

@@ -442,7 +442,8 @@ class AserLinear:
     def __call__(self, X: torch.Tensor, lowrank: bool = True, adapters: "AserAdapters | None" = None,
                  plan: "AdapterPlan | None" = None) -> torch.Tensor:
         """One forward pass through aser_forward (quantization and linear kernel overlapped); with `adapters` and the
-        `plan` of the batch through aser_forward_adapters."""
+        `plan` of the batch through aser_forward_adapters (X may then not be the layer's own output, which is written before
+        the adapters read X)."""
         M = X.shape[0]
         if adapters is not None:
             return adapters._forward(self, X, plan, lowrank)
@@ -654,7 +655,7 @@ class AserAdapters:
 
     def add(self, X: torch.Tensor, Y: torch.Tensor, plan: AdapterPlan, out: torch.Tensor | None = None) -> torch.Tensor:
         """out = Y + scale B (A x) by each token's adapter; X fp16 [M, K], Y and out fp16 [M, N], rows of which may be apart
-        (a column range of a fused projection).  Without `out` in place."""
+        (a column range of a fused projection).  Without `out` in place; what is written may not overlap X."""
         # (a call of a few tokens is shorter on the GPU than from here, as everywhere in this file)
         M, device = X.shape[0], torch._C._cuda_getDevice()
         ldx = _rows(X, (M, self.K), "X", device)

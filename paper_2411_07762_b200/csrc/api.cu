@@ -197,6 +197,23 @@ int adapters_check(const void* X_f16, int ldx, const void* A_f16, const void* B_
     return ASER_OK;
 }
 
+// Whether any of M rows of two fp16 matrices share memory; matrices of one row distance may be column ranges beside each other.
+bool rows_overlap(const void* a, int lda, int cols_a, const void* b, int ldb, int cols_b, int M) {
+    const long long d = ((long long)reinterpret_cast<uintptr_t>(b) - (long long)reinterpret_cast<uintptr_t>(a)) / 2;
+    const long long end_a = (long long)(M - 1) * lda + cols_a, end_b = (long long)(M - 1) * ldb + cols_b;
+    if (d >= end_a || -d >= end_b) return false;
+    if (lda != ldb || M == 1) return true;
+    const long long column = (d % lda + lda) % lda;          // of b's first element, counted from a's
+    return column < cols_a || column + cols_b > lda;
+}
+
+// What a call writes lies over what it reads (the last check: an update in place is one matrix).
+int adapters_overlap(const void* X, int ldx, const void* Y, int ldy, const void* out, int ldo, int M, int N, int K, int r) {
+    if (r > 0 && rows_overlap(X, ldx, K, out, ldo, N, M)) return fail(ASER_ERR_SHAPE, "X and the matrix that is written overlap");
+    if (Y != out && rows_overlap(Y, ldy, N, out, ldo, N, M)) return fail(ASER_ERR_SHAPE, "Y and out overlap without being one matrix");
+    return ASER_OK;
+}
+
 AdapterParams adapter_params(const void* X_f16, int ldx, const void* A_f16, const void* B_f16, const int32_t* ranks,
                              const float* scale, const void* plan, int M, int N, int K, int r, int n_slots, const void* Y_f16,
                              int ldy, void* out_f16, int ldo) {
@@ -633,7 +650,8 @@ int aser_adapters_add(const void* X_f16, int ldx, const void* A_f16, const void*
     int rc = adapters_check(X_f16, ldx, A_f16, B_f16, ranks, scale, plan, plan_bytes, M, N, K, r, n_slots, Y_f16, ldy, out_f16, ldo,
                             workspace, workspace_bytes);
     if (rc != ASER_OK || M == 0 || N == 0) return rc;
-    rc = check_device();
+    rc = adapters_overlap(X_f16, ldx, Y_f16, ldy, out_f16, ldo, M, N, K, r);
+    if (rc == ASER_OK) rc = check_device();
     if (rc != ASER_OK) return rc;
     return launch_adapters(adapter_params(X_f16, ldx, A_f16, B_f16, ranks, scale, plan, M, N, K, r, n_slots, Y_f16, ldy, out_f16, ldo),
                            workspace, static_cast<cudaStream_t>(stream));
@@ -948,12 +966,18 @@ int aser_forward_adapters(const void* X_f16, const float* s, const void* LA_f16,
                           void* workspace, size_t workspace_bytes, const void* A_f16, const void* B_f16, const int32_t* ranks,
                           const float* scale, const void* plan, size_t plan_bytes, int r_adapter, int n_slots, void* adapter_workspace,
                           size_t adapter_workspace_bytes, void* stream) {
-    // the adapters' arguments are checked before the layer is enqueued (M == 0: nothing is)
+    // the adapters' arguments and the layer's are checked before anything is enqueued (M == 0: nothing is)
     int rc = adapters_check(X_f16, K, A_f16, B_f16, ranks, scale, plan, plan_bytes, M, N, K, r_adapter, n_slots, Y_f16, N, Y_f16, N,
                             adapter_workspace, adapter_workspace_bytes);
     if (rc != ASER_OK) return rc;
-    rc = aser_forward(X_f16, s, LA_f16, Wk, w_scale, LB_f16, M, N, K, r, Xq, a_scale, T_bf16, Y_f16, workspace, workspace_bytes, stream);
-    if (rc != ASER_OK || M == 0 || N == 0) return rc;
+    if (!shape_ok(M, N, K, r)) return fail(ASER_ERR_SHAPE, "unsupported M, N, K or r");
+    if (M == 0 || N == 0) return ASER_OK;
+    rc = forward_validate(X_f16, s, LA_f16, Wk, w_scale, LB_f16, M, N, K, r, Xq, a_scale, T_bf16, Y_f16, workspace, workspace_bytes);
+    // (the layer alone may write Y over X, which it has read by then; the adapters read X again)
+    if (rc == ASER_OK) rc = adapters_overlap(X_f16, K, Y_f16, N, Y_f16, N, M, N, K, r_adapter);
+    if (rc == ASER_OK)
+        rc = forward_tokens(X_f16, s, LA_f16, Wk, w_scale, LB_f16, M, M, N, K, r, Xq, a_scale, T_bf16, Y_f16, workspace, workspace_bytes, stream);
+    if (rc != ASER_OK) return rc;
     return launch_adapters(adapter_params(X_f16, K, A_f16, B_f16, ranks, scale, plan, M, N, K, r_adapter, n_slots, Y_f16, N, Y_f16, N),
                            adapter_workspace, static_cast<cudaStream_t>(stream));
 }
