@@ -700,16 +700,27 @@ class AserAdapters:
         return layer.Y[:M]
 
 
+def _on_current_gpu(**tensors):
+    """Tensors that a kernel launched now would read lie on the GPU that it would run on."""
+    device = torch._C._cuda_getDevice()
+    for name, v in tensors.items():
+        if v is not None and v.get_device() != device:
+            raise ValueError("%s needs to be on the current GPU" % name)
+
+
 class AserGatedFFN:
     """Gated feed-forward block of three ASER-quantized layers, Y = down(act(gate(X)) * up(X)), through
     aser_forward_ffn; device-resident operands and a workspace for up to `max_tokens` tokens.
 
     W_gate, W_up fp16 [F,K] with one smoothing vector s [K] (or None) and one pair of factors for both: L_A [r,K], L_B [2F,r]
     whose first F rows are gate's (None for no low-rank term); W_down fp16 [N,F] with s_down [F], L_A_down [r',F],
-    L_B_down [N,r'].  The packed gate and up channels are stored in turn."""
+    L_B_down [N,r'].  The packed gate and up channels are stored in turn.  A block has one workspace and one output buffer: calls that
+    overlap in time, and graphs that may run at the same time, need a block each."""
 
     def __init__(self, W_gate, W_up, s, L_A, L_B, W_down, s_down, L_A_down, L_B_down, max_tokens: int,
                  activation: str = "silu"):
+        _on_current_gpu(W_gate=W_gate, W_up=W_up, s=s, L_A=L_A, L_B=L_B, W_down=W_down, s_down=s_down, L_A_down=L_A_down,
+                        L_B_down=L_B_down)
         self.F, self.K = W_gate.shape
         self.N = W_down.shape[0]
         if W_up.shape != W_gate.shape or W_down.shape[1] != self.F:
