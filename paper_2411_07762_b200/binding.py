@@ -743,12 +743,12 @@ class AserGatedFFN:
             raise ValueError("unsupported shapes for a feed-forward block")
         dev = W_gate.device
         self.s, self.s_down = s, s_down
-        self.Wq, self.w_scale = pack_w4(interleave_gate_up(W_gate, W_up), s)
-        self.Wk = repack_w4(self.Wq)
+        Wq, self.w_scale = pack_w4(interleave_gate_up(W_gate, W_up), s)         # (the canonical form is not kept: no call reads it)
+        self.Wk = repack_w4(Wq)
         self.L_A = None if L_A is None else _dev(L_A, torch.float16, "L_A")
         self.L_B = None if L_B is None else interleave_gate_up(*_dev(L_B, torch.float16, "L_B").chunk(2))
-        self.Wq_down, self.w_scale_down = pack_w4(_dev(W_down, torch.float16, "W_down"), s_down)
-        self.Wk_down = repack_w4(self.Wq_down)
+        Wq, self.w_scale_down = pack_w4(_dev(W_down, torch.float16, "W_down"), s_down)
+        self.Wk_down = repack_w4(Wq)
         self.L_A_down = None if L_A_down is None else _dev(L_A_down, torch.float16, "L_A_down")
         self.L_B_down = None if L_B_down is None else _dev(L_B_down, torch.float16, "L_B_down")
         self.Y = torch.empty((max_tokens, self.N), dtype=torch.float16, device=dev)
