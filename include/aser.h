@@ -337,6 +337,12 @@ int aser_adapters_add(const void* X_f16, int ldx, const void* A_f16, const void*
                       const void* Y_f16, int ldy, void* out_f16, int ldo, void* workspace, size_t workspace_bytes,
                       void* stream);
 size_t aser_adapters_workspace_bytes(int M, int N, int K, int r, int n_slots);
+/*
+ * aser_adapters_check_status -- aser_check_status of the adapter calls made with a plan: synchronises `stream` and returns ASER_OK, or
+ * ASER_ERR_DEVICE_TIMEOUT if a bounded wait of one of them gave up since the plan was made or last checked (what such a wait was for has been
+ * written as NaN).  Debugging aid, not part of the hot path.
+ */
+int aser_adapters_check_status(void* plan, void* stream);
 int aser_forward_adapters(const void* X_f16, const float* s, const void* LA_f16, const void* Wk, const float* w_scale,
                           const void* LB_f16, int M, int N, int K, int r, int8_t* Xq, float* a_scale, void* T_bf16,
                           void* Y_f16, void* workspace, size_t workspace_bytes, const void* A_f16, const void* B_f16,

@@ -17,7 +17,7 @@ EXPORTED_SYMBOLS = (
     "aser_forward_shared_workspace_bytes", "aser_construct", "aser_construct_workspace_bytes", "aser_linear_w4a8_lr", "aser_linear_w4a8", "aser_linear_w4a8_lr_simt", "aser_linear_w4a8_lr_static",
     "aser_workspace_bytes", "aser_workspace_init", "aser_check_status", "aser_forward",
     "aser_forward_host", "aser_linear_w4a8_lr_glu", "aser_forward_ffn_workspace_bytes", "aser_forward_ffn",
-    "aser_adapters_plan_bytes", "aser_adapters_plan", "aser_quant_act_fine", "aser_adapters_add", "aser_adapters_workspace_bytes", "aser_forward_adapters",
+    "aser_adapters_plan_bytes", "aser_adapters_plan", "aser_quant_act_fine", "aser_adapters_add", "aser_adapters_workspace_bytes", "aser_forward_adapters", "aser_adapters_check_status",
     "aser_last_error", "aser_version",
 )
 
@@ -75,6 +75,7 @@ lib.aser_adapters_plan.argtypes = [_P, _I, _I, _P, _Z, _P]
 lib.aser_adapters_workspace_bytes.argtypes = [_I, _I, _I, _I, _I]
 lib.aser_adapters_workspace_bytes.restype = _Z
 lib.aser_adapters_add.argtypes = [_P, _I, _P, _P, _P, _P, _P, _Z, _I, _I, _I, _I, _I, _P, _I, _P, _I, _P, _Z, _P]
+lib.aser_adapters_check_status.argtypes = [_P, _P]
 lib.aser_forward_adapters.argtypes = [_P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _P, _P, _P, _P, _P, _Z,
                                       _P, _P, _P, _P, _P, _Z, _I, _I, _P, _Z, _P]
 lib.aser_construct_workspace_bytes.argtypes = [_I, _I, _I, _I, _I]
@@ -612,6 +613,11 @@ class AdapterPlan:
         _chk(lib.aser_adapters_plan(_ptr(slot), self.M, self.n_slots, _ptr(self.data), self.nbytes, _stream()),
              "aser_adapters_plan")
         return self
+
+    def check_status(self) -> None:
+        """Raises if a bounded wait of an adapter call with this plan gave up (aser_adapters_check_status; synchronises)."""
+        if self.M:
+            _chk(lib.aser_adapters_check_status(_ptr(self.data), _stream()), "aser_adapters_check_status")
 
 
 class AserAdapters:

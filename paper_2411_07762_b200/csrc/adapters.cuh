@@ -1,6 +1,6 @@
 // The plan of a batch's adapters (adapters.cu): tokens by adapter, cut into tiles of one adapter each.
 //   words 0 .. 7   M, n_slots, tiles of kTileFew tokens, tiles of kTileMany tokens, those of the latter with an
-//                  adapter, tokens with an adapter, 0, 0
+//                  adapter, tokens with an adapter, status (not 0: a wait of a call since the plan was made gave up), 0
 //   tiles of 16    {adapter or -1, first place in the list of tokens, tokens, 0, their numbers [16]}: one round of loads
 //   tiles of 128   {adapter or -1, first place, tokens, the first token's number if they follow one another, else -1}
 //   tokens         [M] token numbers by adapter, those without one last
@@ -11,7 +11,7 @@ namespace aser {
 
 constexpr int kTileFew = 16, kTileMany = 128;
 
-constexpr int kFewWords = 4 + kTileFew;
+constexpr int kFewWords = 4 + kTileFew, kPlanStatusWord = 6;
 
 struct PlanView {
     int32_t* tiles_few;       // kFewWords each
@@ -61,6 +61,8 @@ int launch_adapters_down(const AdapterParams& p, cudaStream_t st);
 int launch_adapters_up(const AdapterParams& p, cudaStream_t st);
 
 #ifdef __CUDACC__
+// (by any number of threads: all write the same)
+__device__ __forceinline__ void report_give_up(const AdapterParams& p) { const_cast<volatile int32_t*>(p.plan)[kPlanStatusWord] = 1; }
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile(
         "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"

@@ -14,7 +14,7 @@
 // bound both kernels (4096 tokens of 6 adapters, ranks to 64, 4096 x 4096: 47 us, now 31.2, where the bytes take 16.2; 2048 tokens of
 // 5, ranks to 128, 14336 -> 4096: 43.9, bytes 14.9; 501 tokens of 8, ranks to 32, 4096 -> 28672: 27.6, bytes 11.3).
 //
-// Every wait is bounded; a warp that gives up leaves NaN in what it would have written.
+// Every wait is bounded; a warp that gives up leaves NaN in what it would have written, and its CTA sets the plan's status word.
 #include "adapters.cuh"
 #include "sm100_ptx.cuh"
 
@@ -190,7 +190,11 @@ adapters_down_kernel(const __grid_constant__ DownMaps maps, const AdapterParams 
         bool ok = true;
         if (n > 0) ok = warp_wait(smem_u32(done), 0u, stop, lane);
         __syncthreads();                  // the ring is free
-        if (*stop) { ok = false; let_copies_land(); }
+        if (*stop) {
+            ok = false;
+            if (threadIdx.x == 0) report_give_up(p);
+            let_copies_land();
+        }
         tc_fence_after();
         // partial sums [128 tokens][rk + 4]
         float* part = reinterpret_cast<float*>(smem);
@@ -512,7 +516,10 @@ adapters_up_kernel(const __grid_constant__ UpMaps maps, const AdapterParams p, i
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (*stop) let_copies_land();
+    if (*stop) {
+        if (threadIdx.x == 0) report_give_up(p);
+        let_copies_land();
+    }
     if (warp == 0) tmem_free(tmem, kUpTmem);
 }
 

@@ -641,6 +641,21 @@ size_t aser_adapters_workspace_bytes(int M, int N, int K, int r, int n_slots) {
     return adapters_workspace_bytes(M, N, K, r, n_slots);
 }
 
+int aser_adapters_check_status(void* plan, void* stream) {
+    ASER_REQUIRE_PTR(plan);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    int32_t* at = static_cast<int32_t*>(plan) + kPlanStatusWord;
+    int32_t word = 0;
+    cudaError_t e = cudaMemcpyAsync(&word, at, sizeof(word), cudaMemcpyDeviceToHost, st);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+    if (e == cudaSuccess && word != 0) {
+        e = cudaMemsetAsync(at, 0, sizeof(word), st);
+        if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+    }
+    if (e != cudaSuccess) return record_cuda_error(e, "aser_adapters_check_status");
+    return word == 0 ? ASER_OK : fail(ASER_ERR_DEVICE_TIMEOUT, "a bounded device-side wait of an adapter call gave up");
+}
+
 int aser_adapters_add(const void* X_f16, int ldx, const void* A_f16, const void* B_f16, const int32_t* ranks, const float* scale,
                       const void* plan, size_t plan_bytes, int M, int N, int K, int r, int n_slots, const void* Y_f16, int ldy,
                       void* out_f16, int ldo, void* workspace, size_t workspace_bytes, void* stream) {
