@@ -109,13 +109,22 @@ __device__ __forceinline__ void pj_sts128(uint32_t addr, uint4 v) {
 
 // A group's partial sums, tensor memory -> `buf` as [token][128 rows of the group].  A warp reaches the 32 lanes (rows j) of
 // its quarter, warp % 4; the two warps of a quarter take 64 tokens each.  gave_up: NaN instead.
-__device__ __forceinline__ void pj_stage_t(uint32_t tmem, int g, uint32_t buf, int cw, int warp, int lane, bool gave_up) {
+// sets: so many accumulators, `apart` columns from each other, are added up.
+__device__ __forceinline__ void pj_stage_t(uint32_t tmem, int g, uint32_t buf, int cw, int warp, int lane, bool gave_up, int sets = 1, int apart = 0) {
     const int q = warp & 3, half = cw >> 2;
 #pragma unroll 1
     for (int c0 = half * 64; c0 < half * 64 + 64; c0 += 16) {
         uint32_t v[16];
         tmem_ld16(tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(g * 128 + c0), v);
         tmem_wait_ld(v);
+#pragma unroll 1
+        for (int a = 1; a < sets; ++a) {
+            uint32_t w[16];
+            tmem_ld16(tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(a * apart + g * 128 + c0), w);
+            tmem_wait_ld(w);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) + __uint_as_float(w[e]));
+        }
 #pragma unroll
         for (int e = 0; e < 16; ++e)
             asm volatile("st.shared.b32 [%0], %1;" ::"r"(buf + (uint32_t)(c0 + e) * 512u + (uint32_t)(q * 32 + lane) * 4u), "r"(gave_up ? 0x7fc00000u : v[e]) : "memory");
@@ -180,7 +189,11 @@ act_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
     float* amax_w = s_cache + kPCacheUnits * 8 + (FINE ? kPRestBytes / 4 : 0);   // MAXIMA: [8 warps][128 rows]
     int* n_cached = reinterpret_cast<int*>(tail + 25 * 8 + 16);
     int* n_divided = n_cached + 1;                                  // fine: columns of the slice with a divisor
-    const uint32_t tmem_cols = groups <= 1 ? 128u : groups == 2 ? 256u : 512u;
+    const uint32_t tmem_cols = FINE ? 512u : groups <= 1 ? 128u : groups == 2 ? 256u : 512u;
+    // fine: the slice's stages in two or four sums, as many as tensor memory holds, which are added up in fp32.  The tensor cores' additions are truncated,
+    // and their errors grow with the sum: 4096 x 4096, rank 128, 0.08 % of T a step of bf16 off with one sum, 0.026 % with four (a product in
+    // fp32 0.07 %), for 0.3 % of a gated block's time (674 -> 676 us).
+    auto sums = [&](int turns) { const int n = groups <= 1 ? 4 : groups == 2 ? 2 : 1; return !FINE ? 1 : n < turns ? n : turns; };
 
     if (warp == 0) {
         if (lane == 0) {
@@ -291,9 +304,11 @@ act_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
         if (lane == 0) {
             const uint32_t idesc = make_idesc(1u, 0u, 128u, (uint32_t)kPTok);
             const int turns = twice() ? 2 * nst : nst;
+            const int sets = sums(turns);
             bool ok = true;
             for (int i = 0; i < turns && ok; ++i) {
-                const int st = i % NS;
+                const int st = i % NS, set = FINE ? i * sets / turns : 0;
+                const bool first = i == 0 || (FINE && (i - 1) * sets / turns != set);
                 ok = pj_wait(bar_ready(st), (uint32_t)(i / NS) & 1u, abort_flag);
                 if (!ok) break;
                 tc_fence_after();
@@ -302,7 +317,7 @@ act_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
                     const uint64_t adesc = smem_desc_sw128(sb + st * stage_bytes + (1 + g) * kPTileBytes);
 #pragma unroll
                     for (int kk = 0; kk < kPCols / 16; ++kk)
-                        mma_f16_ss(tmem + g * 128, adesc + 2 * kk, bdesc + 2 * kk, idesc, (i != 0 || kk != 0) ? 1u : 0u);
+                        mma_f16_ss(tmem + (set * groups + g) * 128, adesc + 2 * kk, bdesc + 2 * kk, idesc, (!first || kk != 0) ? 1u : 0u);
                 }
                 tc_commit(bar_free(st));
             }
@@ -498,7 +513,7 @@ act_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
                     if (tid == 64) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
                     named_bar_sync(1, kPConsumerWarps * 32);
                 }
-                pj_stage_t(tmem, g, buf, cw, warp, lane, false);
+                pj_stage_t(tmem, g, buf, cw, warp, lane, false, sums(twice() ? 2 * nst : nst), groups * 128);
                 fence_proxy_async_smem();
                 named_bar_sync(1, kPConsumerWarps * 32);
                 float* dst = t_part + (((size_t)ks * groups + g) * M + row0) * 128;
@@ -521,7 +536,7 @@ act_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
         const int cw = warp - 2;
         const int share0 = kPTok * 32 * ks / (int)gridDim.x, share1 = kPTok * 32 * (ks + 1) / (int)gridDim.x;   // float4s of a group
         for (int g = 0; g < groups; ++g) {
-            if (warp >= 2 && warp < kPWarpLa) pj_stage_t(tmem, g, sb, cw, warp, lane, *abort_flag != 0);
+            if (warp >= 2 && warp < kPWarpLa) pj_stage_t(tmem, g, sb, cw, warp, lane, *abort_flag != 0, sums(twice() ? 2 * nst : nst), groups * 128);
             cluster_arrive();
             cluster_wait();
             for (int e = share0 + tid; e < share1; e += kPThreads) {

@@ -58,3 +58,19 @@ def test_many_divided_columns(aser, M, K, r, divided, first):
     assert not bad.any(), "%d wrong, worst error / bound %.3f" % (int(bad.sum()), float(((T.double() - ref).abs() / bound).max()))
     again = aser.quant_act_fine(X, s, LA)
     assert all(torch.equal(a, b) for a, b in zip((Xq, sc, T), again))
+
+
+@pytest.mark.parametrize("M,K,r", [(4096, 4096, 128), (1000, 8192, 64), (600, 14336, 96), (1500, 2048, 256)])
+def test_few_values_a_step_off(aser, M, K, r):
+    """T is the rounded exact sum but where the sum's own error carries it over the middle between two bf16 numbers: seldomer than for a
+    product in fp32, whose additions are rounded one by one."""
+    g = gen(M + K)
+    X, LA = normal(g, M, K), normal(g, r, K, scale=0.02)
+    s = torch.ones(K, device="cuda")
+    s[torch.randperm(K, device="cuda", generator=g)[:K // 100]] = 7.0
+    exact = ((X.double() / s.double()) @ LA.double().T).to(torch.bfloat16)
+    assert not torch.backends.cuda.matmul.allow_tf32
+    plain = ((X.float() / s) @ LA.float().T).to(torch.bfloat16)
+    T = aser.quant_act_fine(X, s, LA)[2]
+    off, off_plain = int((T != exact).sum()), int((plain != exact).sum())
+    assert off <= off_plain, "%d of %d values off, of a product in fp32 %d" % (off, T.numel(), off_plain)
