@@ -79,8 +79,11 @@ int aser_unrepack_w4(const void* Wk, int N, int K, uint8_t* Wq, void* stream);
  *   x~ = fp32(X[m,k]) / s[k]                       (fp32 division; s == NULL means ones)
  *   a_scale[m] = max_k |x~| / 127                  (fp32 division; zero row -> 0, codes 0)
  *   Xq[m,k] = clamp(rne(x~ / a_scale[m]), -127, 127)
- *   T[m,j]  = bf16( sum_k L_A[j,k] * x~[m,k] )     (fp32 accumulation; from a few hundred tokens
- *                                                   on x~ may be rounded to fp16 first)
+ *   T[m,j]  = bf16( sum_k L_A[j,k] * x~[m,k] )     (fp32 accumulation)
+ * Where the divisor is not 1, x~ enters T in fp32 up to 32 tokens; as the sum of two fp16 numbers (22 bits) while one launch for
+ * a few hundred tokens serves the call, which ends sooner the higher the rank (with 8192 columns at 97 tokens for r = 256, at 449 for r = 16);
+ * else rounded to fp16.  In a pass with scratch (aser_quant_act_ws, and aser_forward where it runs that step, as for every r > 128) the last holds
+ * from 33 tokens on.
  * Xq and a_scale are bit-exact with the definition.  r == 0: LA_f16 and T_bf16 are ignored.
  */
 int aser_quant_act(const void* X_f16, const float* s, const void* LA_f16,

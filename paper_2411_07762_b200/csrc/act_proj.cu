@@ -19,8 +19,8 @@
 // has L2 15 % and HBM 20 % busy: latency of the loads in flight).  Rows of more than 8192 columns exceed L2 at a few thousand tokens and both streams come from
 // HBM; many rows of L_A at 8192 columns are bound by their own traffic already.  Few tokens: beside, a tile has at most eight
 // slices of K, so with few tiles the projection is the longer chain the more rows of L_A there are.  The activation step, us, beside |
-// after each other: rank 128: 33 x 4096 12.4 | 11.9, 64 x 4096 12.3 | 12.5, 600 x 4096 12.7 | 14.1, 4096 x 4096 24.3 | 28.9, 33 x 3072 11.0 |
-// 12.3, 64 x 6144 14.8 | 13.9, 128 x 6144 14.0 | 14.8; rank 64: 300 x 8192 16.7 | 16.6, 449 x 8192 16.6 | 17.3, 4096 x 8192 45.8 | 46.7; rank 128:
+// after each other: rank 128: 33 x 4096 12.4 | 11.9, 64 x 4096 12.3 | 12.5, 600 x 4096 12.7 | 14.1, 4096 x 4096 24.3 | 28.9,
+// 64 x 6144 14.8 | 13.9, 128 x 6144 14.0 | 14.8; rank 64: 300 x 8192 16.7 | 16.6, 449 x 8192 16.6 | 17.3, 4096 x 8192 45.8 | 46.7; rank 128:
 // 1500 x 14336 46 | 41, 4096 x 14336 100 | 85; rank 256: 64 x 4096 17.3 | 15.5, 449 x 4096 17.8 | 17.0, 800 x 4096 18.7 | 19.3, 4096 x 4096 30.6 |
 // 36.7, 100 x 2048 14.2 | 14.2, 600 x 2048 14.9 | 15.4, 600 x 8192 28.2 | 22.2; rank 384: 64 x 4096 22.3 | 17.6, 800 x 4096 24.1 | 22.8, 1600 x 4096 26.4 |
 // 26.4, 4096 x 4096 36.8 | 43.3, 600 x 2048 19.7 | 18.2, 300 x 512 17.8 | 18.0, 200 x 3584 22.0 | 23.9.  (Rank 512 would gain from 2500 tokens on.)

@@ -3,7 +3,6 @@
 // Shared by the kernels that use them; everything here is inline.
 #pragma once
 #include <cuda.h>
-#include <string.h>
 
 #include "aser_common.cuh"
 
