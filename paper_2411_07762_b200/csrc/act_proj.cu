@@ -4,7 +4,7 @@
 //                      through a shared-memory ring together with the matching columns of L_A.  The consumer
 //                      warps write x / s back as fp16 where s != 1 (fine: what that leaves of the quotients is multiplied behind them,
 //                      up to 128 columns of a slice gathered, more in a second turn of the slice through the ring: rank 64, 1 % of the
-//                      columns / all of them divided, us: 600 x 4096 13.6 / 32.5, 4096 x 4096 27 / 87, 600 x 14336, rank 128, 32 /
+//                      columns / all of them divided, us: 600 x 4096 14.6 / 33.6, 4096 x 4096 30 / 88, 600 x 14336, rank 128, 33 /
 //                      110), one thread issues tcgen05.mma
 //                      (kind::f16) with L_A on the M side (up to four groups of 128 rows, so the
 //                      down projections of several layers that share X are computed in one pass)
@@ -109,8 +109,10 @@ __device__ __forceinline__ void pj_sts128(uint32_t addr, uint4 v) {
 
 // A group's partial sums, tensor memory -> `buf` as [token][128 rows of the group].  A warp reaches the 32 lanes (rows j) of
 // its quarter, warp % 4; the two warps of a quarter take 64 tokens each.  gave_up: NaN instead.
-// sets: so many accumulators, `apart` columns from each other, are added up.
-__device__ __forceinline__ void pj_stage_t(uint32_t tmem, int g, uint32_t buf, int cw, int warp, int lane, bool gave_up, int sets = 1, int apart = 0) {
+// FINE: `sets` accumulators, `apart` columns from each other, are added up (one after the other: with two or three loads in flight the registers
+// that the kernel may have are too few, 600 x 4096, rank 64, 14.6 -> 16.6 us).
+template <bool FINE>
+__device__ __forceinline__ void pj_stage_t(uint32_t tmem, int g, uint32_t buf, int cw, int warp, int lane, bool gave_up, int sets, int apart) {
     const int q = warp & 3, half = cw >> 2;
 #pragma unroll 1
     for (int c0 = half * 64; c0 < half * 64 + 64; c0 += 16) {
@@ -118,7 +120,7 @@ __device__ __forceinline__ void pj_stage_t(uint32_t tmem, int g, uint32_t buf, i
         tmem_ld16(tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(g * 128 + c0), v);
         tmem_wait_ld(v);
 #pragma unroll 1
-        for (int a = 1; a < sets; ++a) {
+        for (int a = 1; FINE && a < sets; ++a) {
             uint32_t w[16];
             tmem_ld16(tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(a * apart + g * 128 + c0), w);
             tmem_wait_ld(w);
@@ -190,10 +192,10 @@ act_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
     int* n_cached = reinterpret_cast<int*>(tail + 25 * 8 + 16);
     int* n_divided = n_cached + 1;                                  // fine: columns of the slice with a divisor
     const uint32_t tmem_cols = FINE ? 512u : groups <= 1 ? 128u : groups == 2 ? 256u : 512u;
-    // fine: the slice's stages in two or four sums, as many as tensor memory holds, which are added up in fp32.  The tensor cores' additions are truncated,
-    // and their errors grow with the sum: 4096 x 4096, rank 128, 0.08 % of T a step of bf16 off with one sum, 0.026 % with four (a product in
-    // fp32 0.07 %), for 0.3 % of a gated block's time (674 -> 676 us).
-    auto sums = [&](int turns) { const int n = groups <= 1 ? 4 : groups == 2 ? 2 : 1; return !FINE ? 1 : n < turns ? n : turns; };
+    // fine: the slice's stages by turns in four sums (above rank 128 two), as many as tensor memory holds, which are added up in fp32.  The tensor cores'
+    // additions are truncated, and their errors grow with the sum: 4096 x 4096, rank 128, 0.08 % of T a step of bf16 off with one sum, 0.026 % with
+    // four (a product in fp32 0.07 %), for 2 us (28.1 -> 30.0 at rank 64; two divisions to find a stage's sum, rather than turns, took 2.5 more).
+    auto sums = [&](int turns) { const int n = groups <= 1 ? 4 : groups == 2 ? 2 : 1; return !FINE ? 1 : n <= turns ? n : turns >= 2 ? 2 : 1; };
 
     if (warp == 0) {
         if (lane == 0) {
@@ -307,8 +309,8 @@ act_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
             const int sets = sums(turns);
             bool ok = true;
             for (int i = 0; i < turns && ok; ++i) {
-                const int st = i % NS, set = FINE ? i * sets / turns : 0;
-                const bool first = i == 0 || (FINE && (i - 1) * sets / turns != set);
+                const int st = i % NS, set = FINE ? i & (sets - 1) : 0;
+                const bool first = FINE ? i < sets : i == 0;
                 ok = pj_wait(bar_ready(st), (uint32_t)(i / NS) & 1u, abort_flag);
                 if (!ok) break;
                 tc_fence_after();
@@ -513,7 +515,7 @@ act_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
                     if (tid == 64) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
                     named_bar_sync(1, kPConsumerWarps * 32);
                 }
-                pj_stage_t(tmem, g, buf, cw, warp, lane, false, sums(twice() ? 2 * nst : nst), groups * 128);
+                pj_stage_t<FINE>(tmem, g, buf, cw, warp, lane, false, sums(twice() ? 2 * nst : nst), groups * 128);
                 fence_proxy_async_smem();
                 named_bar_sync(1, kPConsumerWarps * 32);
                 float* dst = t_part + (((size_t)ks * groups + g) * M + row0) * 128;
@@ -536,7 +538,7 @@ act_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
         const int cw = warp - 2;
         const int share0 = kPTok * 32 * ks / (int)gridDim.x, share1 = kPTok * 32 * (ks + 1) / (int)gridDim.x;   // float4s of a group
         for (int g = 0; g < groups; ++g) {
-            if (warp >= 2 && warp < kPWarpLa) pj_stage_t(tmem, g, sb, cw, warp, lane, *abort_flag != 0, sums(twice() ? 2 * nst : nst), groups * 128);
+            if (warp >= 2 && warp < kPWarpLa) pj_stage_t<FINE>(tmem, g, sb, cw, warp, lane, *abort_flag != 0, sums(twice() ? 2 * nst : nst), groups * 128);
             cluster_arrive();
             cluster_wait();
             for (int e = share0 + tid; e < share1; e += kPThreads) {
